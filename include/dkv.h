@@ -32,6 +32,7 @@ extern "C" {
  * accumulation, softmax, the residual stream and confidences are always fp32 */
 #define DKV_BF16 0
 #define DKV_FP32 1
+#define DKV_E4M3 2        /* paged caches only (dkv_paged_cache): 8 bits per element, a scale per position and K/V head */
 
 /* cache variants (Sec. 3.3 "dKV-Cache-Decode", "dKV-Cache-Prefill and dKV-Cache-PD"; Sec. 3.4) */
 #define DKV_DECODE  0
@@ -272,6 +273,63 @@ int dkv_attn_update_static(void *k_cache, void *v_cache, const void *q, const vo
 int dkv_concat_reorder(const void *k_cached, const void *v_cached, const void *k_new, const void *v_new,
                        const int32_t *take, void *k_out, void *v_out, int32_t batch, int32_t n_kv_heads,
                        int32_t n_cached, int32_t n_new, int32_t head_dim, int32_t dtype, void *stream);
+
+/* A K/V cache in pages, for sequences of different lengths that grow and leave: position p of sequence b lives in page
+ * page_table[b][p / page_size] at slot p % page_size. An entry outside [0, n_pages) says that there is no page: rows are not
+ * stored there, loads give zeros, attention leaves those positions out (a table can be wider than what is in use, and a
+ * page can be given back before its sequence ends). Pages may be shared by sequences that only read them.
+ *   k_pages, v_pages (dev) [n_pages][n_kv_heads][page_size][head_dim], elements of `dtype`, 16-byte aligned
+ *   k_scale, v_scale (dev) [n_pages][n_kv_heads][page_size], DKV_E4M3 only: scale of a row as the biased exponent of a
+ *                    power of two (E8M0): element = code * 2^(scale - 127)
+ *   page_table (dev) [batch][max_pages]
+ *   seq_len (dev) [batch] positions of each sequence (attention only; taken as 0 below 0, as max_pages * page_size above)
+ * page_size: a power of two, 16 to 65536; max_pages * page_size at most 2^30; head_dim 32, 64 or 128; dtype DKV_BF16, DKV_FP32 or
+ * DKV_E4M3. Nothing in the structure is kept by a call; the structure itself is host memory. Table, lengths, positions
+ * and row offsets are read on the device, so a captured call follows them. */
+typedef struct {
+    void *k_pages, *v_pages;
+    uint8_t *k_scale, *v_scale;
+    const int32_t *page_table, *seq_len;
+    int32_t batch, n_pages, max_pages, page_size, n_kv_heads, head_dim, dtype;
+} dkv_paged_cache;
+
+/* Write rows into the cache: row r of sequence b, i.e. row_off[b] <= r < row_off[b + 1], goes to position positions[r] of that
+ * sequence. Rows whose position is negative, beyond the table or on no page are not stored, nor are rows from
+ * min(rows, row_off[batch]) on. Positions are distinct within a sequence, and no page that two sequences share is written.
+ *   k_new, v_new (dev) [rows] rows of [n_kv_heads][head_dim], `row_stride` elements apart (at least n_kv_heads * head_dim),
+ *                elements of `dtype` (DKV_BF16 or DKV_FP32)
+ *   positions (dev) [rows]; row_off (dev) [batch + 1] ascending from 0, or null for one row per sequence (rows == batch)
+ * DKV_BF16 and DKV_FP32 caches hold the nearest value of their type. A DKV_E4M3 cache holds x * 2^-e rounded to the nearest e4m3
+ * value, ties to even, with the smallest e >= -110 that brings the largest finite magnitude of the row to at most 448: an
+ * error of at most 2^-4 of the element or 2^(e - 10), whichever is larger. Infinities and NaN become NaN, and count for nothing in e. (e is at
+ * most 120, and then magnitudes end at 240 * 2^120, so that no finite element is read back as infinity.) */
+int dkv_paged_store(const dkv_paged_cache *cache, const void *k_new, const void *v_new, int64_t row_stride,
+                    const int32_t *positions, const int32_t *row_off, int32_t rows, int32_t dtype, void *stream);
+
+/* The inverse: k_out[r], v_out[r] (dev, [rows][n_kv_heads][head_dim] of `dtype`, DKV_BF16 or DKV_FP32) = the rows at positions[r],
+ * zeros where the position is outside the table or on no page. Rows from min(rows, row_off[batch]) on are left as they
+ * are. Exact, but for a DKV_FP32 cache read as DKV_BF16 (nearest value). */
+int dkv_paged_load(const dkv_paged_cache *cache, void *k_out, void *v_out, const int32_t *positions,
+                   const int32_t *row_off, int32_t rows, int32_t dtype, void *stream);
+
+/* Attention of new rows over the cache (Eq. 4 with lengths of their own): for row r of sequence b and query head h
+ *   out[r][h] = softmax(q[r][h] . K[b][h / group]^T / sqrt(head_dim)) V[b][h / group]
+ * over the positions below seq_len[b] that lie on a page, no further mask. Where the sum of the exponentials is zero (no such position,
+ * or all scores -infinity) the result is zero. What lies behind a sequence's end or on pages that the table does not name is
+ * never used, whatever it holds.
+ *   q (dev) [rows] rows of [n_q_heads][head_dim], `q_stride` elements apart (at least n_q_heads * head_dim); out (dev)
+ *     [rows][n_q_heads][head_dim]; elements of `dtype`
+ *   row_off as above; max_rows_per_seq (host) bounds the rows of any one sequence (rows of a sequence beyond it are left out)
+ *   workspace (dev), 16-byte aligned, of dkv_paged_attn_workspace_bytes for the same cache, heads, rows and bound; calls that may
+ *     overlap need one each
+ * Rows from min(rows, row_off[batch]) on are left as they are. dtype DKV_BF16 reads DKV_BF16 and DKV_E4M3 caches (products of bf16
+ * operands, probabilities among them, sums in fp32; e4m3 elements with their scales are exact in bf16); DKV_FP32 reads
+ * DKV_FP32 and DKV_E4M3 caches, in fp32 throughout. */
+size_t dkv_paged_attn_workspace_bytes(const dkv_paged_cache *cache, int32_t n_q_heads, int32_t rows, int32_t max_rows_per_seq,
+                                      int32_t dtype);
+int dkv_paged_attn(const dkv_paged_cache *cache, const void *q, int64_t q_stride, const int32_t *row_off, void *out,
+                   int32_t rows, int32_t max_rows_per_seq, int32_t n_q_heads, int32_t dtype, void *workspace,
+                   size_t workspace_bytes, void *stream);
 
 /* y[M, N] (fp32, dev) = x[M, K] * w[N, K]^T with x, w of `dtype` (dev): the projection kernel of
  * the path on its own, for parity tests and roofline measurements. workspace as returned by

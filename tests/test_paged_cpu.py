@@ -1,0 +1,144 @@
+"""Paged K/V cache without a GPU: the oracle's quantiser against another one, and what the calls refuse."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2505_15781_amd as P
+from oracle import paged as O
+from paper_2505_15781_amd import binding as B
+
+
+def test_e4m3_values_and_rounding_of_the_oracle_are_those_of_the_type():
+    codes = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).double().numpy()
+    assert np.array_equal(O.e4m3_values(), codes, equal_nan=True)
+    g = np.random.default_rng(1)
+    x = np.concatenate([g.standard_normal(4000) * 2.0 ** g.integers(-12, 7, 4000), codes[~np.isnan(codes)],
+                        (codes[:126] + codes[1:127]) / 2, -(codes[:126] + codes[1:127]) / 2, [448.0, -448.0, 0.0, 2.0 ** -10, 3 * 2.0 ** -11]])
+    x = x.astype(np.float32)
+    assert np.array_equal(O.round_e4m3(x.astype(np.float64)), torch.from_numpy(x).to(torch.float8_e4m3fn).double().numpy())
+
+
+@pytest.mark.parametrize("top,e", [(448.0, 0), (449.0, 1), (224.0, -1), (224.5, 0), (1.0, -8), (1.75, -8), (1.7500001, -7), (0.0, -110),
+                                   (1e-38, -110), (448 * 2.0 ** -110, -110), (449 * 2.0 ** -110, -109), (3.3895e38, 120), (np.inf, -8), (np.nan, -8)])
+def test_scale_of_the_oracle(top, e):
+    x = np.array([np.float32(top), -1.0 if not np.isfinite(top) else 0.0])
+    held, got = O.quantise(x)
+    assert got == e
+    assert np.isnan(held[0]) if not np.isfinite(top) else abs(held[0] - x[0]) <= max(2.0 ** -4 * abs(x[0]), 2.0 ** (e - 10))
+    assert np.isfinite(held.astype(np.float32))[1] and (not np.isfinite(top) or np.isfinite(held.astype(np.float32)[0]))
+
+
+def desc(**changes):
+    d = B.PagedCacheDesc(16, 16, 16, 16, 16, 16, 2, 4, 3, 16, 2, 64, B.E4M3)
+    for k, v in changes.items():
+        setattr(d, "dtype" if k == "cache_dtype" else k, v)
+    return d
+
+
+def store(d=None, k=16, v=16, stride=128, pos=16, off=16, rows=3, dtype=0, **changes):
+    return B.lib.dkv_paged_store(C.byref(d or desc(**changes)), k, v, stride, pos, off, rows, dtype, None)
+
+
+def load(d=None, k=16, v=16, pos=16, off=16, rows=3, dtype=0, **changes):
+    return B.lib.dkv_paged_load(C.byref(d or desc(**changes)), k, v, pos, off, rows, dtype, None)
+
+
+def attn(q=16, stride=256, off=16, out=16, rows=3, most=2, heads=4, dtype=0, ws=16, nbytes=1 << 40, **changes):
+    return B.lib.dkv_paged_attn(C.byref(desc(**changes)), q, stride, off, out, rows, most, heads, dtype, ws, nbytes, None)
+
+
+CACHE_FAULTS = [(dict(k_pages=None), -1), (dict(v_pages=None), -1), (dict(page_table=None), -1), (dict(k_scale=None), -1),
+                (dict(v_scale=None), -1), (dict(cache_dtype=3), -1), (dict(cache_dtype=-1), -1), (dict(batch=0), -1), (dict(n_pages=0), -1),
+                (dict(max_pages=0), -1), (dict(n_kv_heads=0), -1), (dict(head_dim=48), -3), (dict(head_dim=256), -3), (dict(page_size=8), -3),
+                (dict(page_size=48), -3), (dict(page_size=131072), -3), (dict(page_size=0), -3), (dict(page_size=65536, max_pages=16385), -3),
+                (dict(k_pages=24), -1), (dict(v_pages=17), -1)]
+
+
+@pytest.mark.parametrize("fault,code", CACHE_FAULTS)
+def test_every_call_refuses_a_bad_cache(fault, code):
+    for call in (store, load, attn):
+        assert call(**fault) == code and B.last_error()
+    assert B.lib.dkv_paged_attn_workspace_bytes(C.byref(desc(**fault)), 4, 3, 2, 0) == 0
+
+
+def test_refused_arguments():
+    for call in (store, load):
+        assert call(k=None) == call(v=None) == call(pos=None) == -1
+        assert call(rows=-1) == call(dtype=2) == -1
+        assert call(off=None, rows=3) == -1                          # one row per sequence: two sequences
+        assert call(rows=1 << 24) == -3
+        assert call(rows=0, k=None, v=None, pos=None) == 0
+    assert store(stride=127) == -1
+    assert attn(q=None) == attn(out=None) == attn(seq_len=None) == attn(rows=-1) == attn(dtype=2) == -1
+    assert attn(heads=3) == attn(heads=0) == attn(most=-1) == attn(rows=5) == attn(off=None) == attn(stride=255) == -1
+    assert attn(rows=0, q=None, out=None, ws=None, nbytes=0) == 0
+    assert B.lib.dkv_paged_store(None, 16, 16, 128, 16, 16, 3, 0, None) == -1
+    assert attn(dtype=B.BF16, cache_dtype=B.FP32) == attn(dtype=B.FP32, cache_dtype=B.BF16) == -3
+
+
+def tensors(dtype=torch.float8_e4m3fn):
+    scale = torch.zeros((5, 2, 16), dtype=torch.uint8).view(torch.float8_e8m0fnu)
+    pages = torch.zeros((5, 2, 16, 64), dtype=torch.uint8).view(dtype) if dtype == torch.float8_e4m3fn else torch.zeros((5, 2, 16, 64), dtype=dtype)
+    f8 = dtype == torch.float8_e4m3fn
+    return P.PagedCache(pages, pages.clone(), torch.zeros((3, 4), dtype=torch.int32), torch.zeros(3, dtype=torch.int32),
+                        scale if f8 else None, scale.clone() if f8 else None)
+
+
+def calls(cache, k=None, pos=None, off="given", q=None, out=None, ws=None):
+    k = torch.zeros((6, 2, 64), dtype=torch.bfloat16) if k is None else k
+    pos = torch.zeros(6, dtype=torch.int32) if pos is None else pos
+    off = torch.zeros(4, dtype=torch.int32) if isinstance(off, str) else off
+    q = torch.zeros((6, 4, 64), dtype=torch.bfloat16) if q is None else q
+    out = torch.zeros((6, 4, 64), dtype=torch.bfloat16) if out is None else out
+    return {"store": lambda: P.paged_store(cache, k, k, pos, off), "load": lambda: P.paged_load(cache, k, k, pos, off),
+            "attn": lambda: P.paged_attn(cache, q, off, out, 6, ws)}
+
+
+def refused(which, cache, text, **kw):
+    for name, call in calls(cache, **kw).items():
+        if name in which:
+            with pytest.raises(ValueError, match=text):
+                call()
+
+
+ALL = ("store", "load", "attn")
+
+
+def test_the_binding_refuses_tensors_that_are_not_what_a_call_reads():
+    c = tensors()
+    refused(ALL, c, "not on a GPU")                                  # everything else is as it should be
+    refused(ALL, c._replace(k_pages=c.k_pages[:, :, :, :32]), "k_pages")
+    refused(ALL, c._replace(v_pages=c.v_pages[:4]), "v_pages")
+    refused(ALL, c._replace(k_pages=c.k_pages[0], v_pages=c.v_pages[0]), "four dimensions")
+    refused(ALL, c._replace(k_pages=c.k_pages.view(torch.uint8), v_pages=c.v_pages.view(torch.uint8)), "not supported")
+    refused(ALL, c._replace(k_scale=None), "need k_scale")
+    refused(ALL, c._replace(v_scale=c.v_scale.view(torch.uint8)), "v_scale")
+    refused(ALL, c._replace(k_scale=c.k_scale[:, :1]), "k_scale")
+    refused(ALL, tensors(torch.bfloat16)._replace(k_scale=c.k_scale), "scales go with")
+    refused(ALL, c._replace(page_table=c.page_table.long()), "page_table")
+    refused(ALL, c._replace(page_table=c.page_table[:, ::2]), "page_table")
+    refused(ALL, c._replace(seq_len=c.seq_len[:2]), "seq_len")
+    refused(ALL, c, "row_off", off=torch.zeros(5, dtype=torch.int32))
+    refused(ALL, c, "row_off", off=torch.zeros(4, dtype=torch.int64))
+    refused(ALL, c, "one row per sequence", off=None)
+    refused(("attn",), c._replace(seq_len=None), "seq_len")
+    refused(("store", "load"), c, "positions", pos=torch.zeros(5, dtype=torch.int32))
+    refused(("store", "load"), c, "positions", pos=torch.zeros(6, dtype=torch.int64))
+    refused(("store", "load"), c, "k_", k=torch.zeros((6, 2, 32), dtype=torch.bfloat16))
+    refused(("store", "load"), c, "k_", k=torch.zeros((6, 3, 64), dtype=torch.bfloat16))
+    refused(("store", "load"), c, "k_", k=torch.zeros((6, 2, 64), dtype=torch.float16))
+    refused(("store",), c, "k_new", k=torch.zeros((6, 64, 2), dtype=torch.bfloat16).transpose(1, 2))
+    refused(("store",), c, "k_new", k=torch.zeros((1, 2, 64), dtype=torch.bfloat16).expand(6, 2, 64))
+    refused(("load",), c, "k_out", k=torch.zeros((6, 3, 64), dtype=torch.bfloat16)[:, :2])
+    refused(("attn",), c, "out", out=torch.zeros((6, 4, 64)))
+    refused(("attn",), c, "out", out=torch.zeros((6, 5, 64), dtype=torch.bfloat16)[:, :4])
+    refused(("attn",), c, "q", q=torch.zeros((6, 4, 32), dtype=torch.bfloat16))
+    refused(("attn",), c, "workspace", ws=torch.zeros(8)[::2])
+
+
+def test_rows_that_are_parts_of_longer_ones_are_taken():
+    """Slices of a fused projection's rows pass every check but the last (these tensors are not on a GPU)."""
+    qkv = torch.zeros((6, 8, 64), dtype=torch.bfloat16)
+    refused(("store", "attn"), tensors(), "not on a GPU", k=qkv[:, 4:6], q=qkv[:, :4])
