@@ -95,6 +95,9 @@ lib.dkv_paged_load.argtypes = [C.POINTER(PagedCacheDesc), c_vp, c_vp, c_vp, c_vp
 lib.dkv_paged_attn_workspace_bytes.restype = c_sz
 lib.dkv_paged_attn_workspace_bytes.argtypes = [C.POINTER(PagedCacheDesc), c_i32, c_i32, c_i32, c_i32]
 lib.dkv_paged_attn.argtypes = [C.POINTER(PagedCacheDesc), c_vp, C.c_int64, c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_vp, c_sz, c_vp]
+_marshal.bind_paged(*(C.cast(f, c_vp).value for f in (lib.dkv_paged_store, lib.dkv_paged_load, lib.dkv_paged_attn_workspace_bytes,
+                                                      lib.dkv_paged_attn)),
+                    torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.int32)
 lib.dkv_peak_copy.argtypes = [c_vp, c_vp, c_sz, c_vp]
 lib.dkv_peak_read.argtypes = [c_vp, c_vp, c_sz, c_vp]
 lib.dkv_peak_mfma.argtypes = [c_vp, c_i32, C.POINTER(C.c_double), c_vp]
@@ -359,112 +362,32 @@ class PagedCache(NamedTuple):
     v_scale: Optional[torch.Tensor] = None
 
 
-_PAGE_DTYPES = {torch.bfloat16: BF16, torch.float32: FP32, torch.float8_e4m3fn: E4M3}
-
-
-def _want(ok, text):
-    if not ok:
-        raise ValueError(text)
-
-
-def _whole(t, name, shape, dtype, device):
-    """A contiguous tensor of this shape and type, where the cache is."""
-    _want(t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous(),
-          f"{name}: a contiguous {dtype} tensor of shape {list(shape)} is expected, not {t.dtype} {list(t.shape)}")
-    _want(t.device == device, f"{name} is on {t.device}, the cache on {device}")
-
-
-def _paged_desc(cache):
-    k, v, table, seq_len, ks, vs = cache
-    _want(k.dim() == 4, "pages have four dimensions: pages, kv heads, slots, head_dim")
-    _want(k.dtype in _PAGE_DTYPES, f"pages of {k.dtype} are not supported")
-    _whole(k, "k_pages", k.shape, k.dtype, k.device)
-    _whole(v, "v_pages", k.shape, k.dtype, k.device)
-    _want(table.dim() == 2, "page_table has two dimensions: sequences, pages")
-    _whole(table, "page_table", table.shape, torch.int32, k.device)
-    if seq_len is not None:
-        _whole(seq_len, "seq_len", table.shape[:1], torch.int32, k.device)
-    if k.dtype == torch.float8_e4m3fn:
-        _want(ks is not None and vs is not None, "pages of torch.float8_e4m3fn need k_scale and v_scale")
-        _whole(ks, "k_scale", k.shape[:3], torch.float8_e8m0fnu, k.device)
-        _whole(vs, "v_scale", k.shape[:3], torch.float8_e8m0fnu, k.device)
-    else:
-        _want(ks is None and vs is None, "scales go with pages of torch.float8_e4m3fn only")
-    return PagedCacheDesc(_ptr(k), _ptr(v), _ptr(ks), _ptr(vs), _ptr(table), _ptr(seq_len), table.shape[0], k.shape[0],
-                          table.shape[1], k.shape[2], k.shape[1], k.shape[3], _PAGE_DTYPES[k.dtype])
-
-
-def _paged_rows(t, name, heads, head_dim, device, whole):
-    """[rows, heads, head_dim] of bfloat16 or float32; the rows may be apart from each other unless `whole`."""
-    _want(t.dim() == 3 and t.shape[1] == heads and t.shape[2] == head_dim and t.dtype in (torch.bfloat16, torch.float32),
-          f"{name}: [rows, {heads}, {head_dim}] of bfloat16 or float32 is expected, not {list(t.shape)} of {t.dtype}")
-    rows, dense = t.shape[0], heads * head_dim
-    _want(t.is_contiguous() or (not whole and t.stride(2) == 1 and (heads == 1 or t.stride(1) == head_dim) and (rows < 2 or t.stride(0) >= dense)),
-          f"{name}: " + ("a contiguous tensor" if whole else "rows of heads one behind the other") + " is expected")
-    _want(t.device == device, f"{name} is on {t.device}, the cache on {device}")
-    return dense if t.is_contiguous() or rows < 2 else t.stride(0)
-
-
-def _paged_offsets(row_off, batch, rows, device):
-    if row_off is None:
-        _want(rows == batch, f"without row offsets there is one row per sequence: {rows} rows, {batch} sequences")
-    else:
-        _whole(row_off, "row_off", (batch + 1,), torch.int32, device)
-
-
-def _paged_on_gpu(device):
-    _want(device.type == "cuda", f"the cache is on {device}, not on a GPU")
-    _want(device.index == torch.cuda.current_device(), f"the cache is on {device}, the current device is {torch.cuda.current_device()}")
+def _place(cache):
+    """(current device, its stream) for a cache on a GPU; the marshalling refuses a cache that is elsewhere."""
+    return (-1, 0) if cache[0].get_device() < 0 else (torch.cuda.current_device(), _stream())
 
 
 def paged_store(cache, k_new, v_new, positions, row_off=None):
     """Write rows of new K and V to their positions, quantised where the cache holds e4m3: row r of sequence b, i.e.
     row_off[b] <= r < row_off[b + 1], goes to position positions[r]; without row_off, row r belongs to sequence r.
     k_new, v_new [rows, n_kv_heads, head_dim], bfloat16 or float32; the rows may be parts of longer ones."""
-    d, dev = _paged_desc(cache), cache.k_pages.device
-    stride = _paged_rows(k_new, "k_new", d.n_kv_heads, d.head_dim, dev, False)
-    rows = k_new.shape[0]
-    _want(v_new.dtype == k_new.dtype and v_new.shape == k_new.shape and _paged_rows(v_new, "v_new", d.n_kv_heads, d.head_dim, dev, False) == stride,
-          "k_new and v_new have the same shape, type and distance between rows")
-    _whole(positions, "positions", (rows,), torch.int32, dev)
-    _paged_offsets(row_off, d.batch, rows, dev)
-    _paged_on_gpu(dev)
-    _check(lib.dkv_paged_store(C.byref(d), _ptr(k_new), _ptr(v_new), stride, _ptr(positions), _ptr(row_off), rows,
-                               _PAGE_DTYPES[k_new.dtype], _stream()))
+    _check(_marshal.paged_store(cache, k_new, v_new, positions, row_off, *_place(cache)))
 
 
 def paged_load(cache, k_out, v_out, positions, row_off=None):
     """The rows at these positions, as paged_store takes them; zeros where there is no page."""
-    d, dev = _paged_desc(cache), cache.k_pages.device
-    _paged_rows(k_out, "k_out", d.n_kv_heads, d.head_dim, dev, True)
-    rows = k_out.shape[0]
-    _whole(v_out, "v_out", k_out.shape, k_out.dtype, dev)
-    _whole(positions, "positions", (rows,), torch.int32, dev)
-    _paged_offsets(row_off, d.batch, rows, dev)
-    _paged_on_gpu(dev)
-    _check(lib.dkv_paged_load(C.byref(d), _ptr(k_out), _ptr(v_out), _ptr(positions), _ptr(row_off), rows,
-                              _PAGE_DTYPES[k_out.dtype], _stream()))
+    _check(_marshal.paged_load(cache, k_out, v_out, positions, row_off, *_place(cache)))
 
 
 def paged_attn_workspace_bytes(cache, n_q_heads, rows, max_rows_per_seq, dtype=BF16):
-    """Bytes of workspace paged_attn needs at most for this many rows (0 where it would refuse them)."""
-    return lib.dkv_paged_attn_workspace_bytes(C.byref(_paged_desc(cache)), n_q_heads, rows, max_rows_per_seq, dtype)
+    """Bytes of workspace that paged_attn needs for this many rows of `dtype` (0 where it would refuse them)."""
+    return _marshal.paged_attn_workspace_bytes(cache, n_q_heads, rows, max_rows_per_seq, dtype)
 
 
 def paged_attn(cache, q, row_off, out, max_rows_per_seq, workspace):
     """Attention of the rows of q [rows, n_q_heads, head_dim] over all positions of their sequences (below seq_len, on a
     page) into `out`; row_off as in paged_store (None: one row per sequence)."""
-    d, dev = _paged_desc(cache), cache.k_pages.device
-    _want(cache.seq_len is not None, "attention needs seq_len")
-    _want(q.dim() == 3, "q has three dimensions: rows, heads, head_dim")
-    rows, heads = q.shape[0], q.shape[1]
-    stride = _paged_rows(q, "q", heads, d.head_dim, dev, False)
-    _whole(out, "out", q.shape, q.dtype, dev)
-    _paged_offsets(row_off, d.batch, rows, dev)
-    _want(workspace is None or (workspace.device == dev and workspace.is_contiguous()), "the workspace is a contiguous tensor where the cache is")
-    _paged_on_gpu(dev)
-    _check(lib.dkv_paged_attn(C.byref(d), _ptr(q), stride, _ptr(row_off), _ptr(out), rows, max_rows_per_seq, heads,
-                              _PAGE_DTYPES[q.dtype], _ptr(workspace), 0 if workspace is None else workspace.nbytes, _stream()))
+    _check(_marshal.paged_attn(cache, q, row_off, out, max_rows_per_seq, workspace, *_place(cache)))
 
 
 GEMM_OPT_STAGGER, GEMM_OPT_XCD_GROUP, GEMM_OPT_SWIGLU, GEMM_OPT_STREAM_W = 1, 2, 4, 8
