@@ -100,26 +100,27 @@ def attn(cache, q, off):
     R, Hq, dh = q.shape
     out, spread, most = np.full(q.shape, np.nan), np.full(q.shape, np.nan), 0.0
     group = Hq // cache["k"].shape[1]
-    held = {}
+    mine = {}
     for r, b in rows_of(cache, off, R):
-        if b not in held:
-            at = seen(cache, b)
-            pages, slots = [a[0] for a in at], [a[1] for a in at]
-            held[b] = (cache["k"][pages, :, slots], cache["v"][pages, :, slots])          # [keys, kv heads, dh]
-        K, V = held[b]
-        if len(K) == 0:
+        mine.setdefault(b, []).append(r)
+    for b, r in mine.items():
+        at = seen(cache, b)
+        pages, slots = [a[0] for a in at], [a[1] for a in at]
+        if not at:
             out[r] = spread[r] = 0.0
             continue
+        K, V = cache["k"][pages, :, slots], cache["v"][pages, :, slots]          # [keys, kv heads, dh]
         for h in range(Hq):
             k, v = K[:, h // group], V[:, h // group]
-            s = k @ q[r, h] / np.sqrt(dh)
-            m = s.max()
-            if m == -np.inf:
-                out[r, h] = spread[r, h] = 0.0
-                continue
-            p = np.exp(s - m)
-            out[r, h], spread[r, h] = p @ v / p.sum(), p @ np.abs(v) / p.sum()
+            s = q[r, h] @ k.T / np.sqrt(dh)
+            m = s.max(-1, keepdims=True)
+            nothing = m == -np.inf
+            p = np.where(nothing, 0.0, np.exp(s - np.where(nothing, 0.0, m)))
+            total = p.sum(-1, keepdims=True)
+            total = np.where(nothing, 1.0, total)
+            out[r, h] = np.where(nothing, 0.0, p @ v / total)
+            spread[r, h] = np.where(nothing, 0.0, p @ np.abs(v) / total)
             finite = np.abs(k).max(-1) < np.inf
             if finite.any():
-                most = max(most, float((np.abs(k[finite]) @ np.abs(q[r, h])).max() / np.sqrt(dh)))
+                most = max(most, float((np.abs(q[r, h]) @ np.abs(k[finite]).T).max() / np.sqrt(dh)))
     return out, spread, most

@@ -95,7 +95,7 @@ __device__ __forceinline__ void dma16_at_nt(uint32_t voff, const void *base, uin
 }
 
 static inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-static inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
+static inline __host__ __device__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 // ---- internal launchers (host side) --------------------------------------------------------
 

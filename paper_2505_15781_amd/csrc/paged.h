@@ -23,6 +23,22 @@ struct PagedCache {
     __device__ __forceinline__ int keys(int b) const { return max(0, min(seq_len[b], capacity())); }
 };
 
+// Division by a number that the host knows: x / d = x * mul >> (31 + l) for 0 <= x < 2^31, with 2^(l - 1) < d <= 2^l and mul = 2^(31 + l) / d
+// rounded up: the excess of mul * d over 2^(31 + l) is less than 2^l, so that x times it stays below 2^(31 + l).
+struct Divisor {
+    int d;
+    uint32_t mul;
+    int shift;
+    __host__ explicit Divisor(int d_ = 1) : d(d_) {
+        int l = 0;
+        while ((1ll << l) < d) ++l;
+        shift = 31 + l;
+        mul = (uint32_t)(((1ull << shift) + d - 1) / d);
+    }
+    __device__ __forceinline__ int div(int x) const { return (int)((uint64_t)(uint32_t)x * mul >> shift); }
+    __device__ __forceinline__ int mod(int x) const { return x - div(x) * d; }
+};
+
 typedef uint8_t e4m3_t;      // a code; its row's scale is a biased exponent
 
 // Value of a scale: a normal number for the exponents that a store writes (-110 to 120).

@@ -20,34 +20,45 @@ __device__ __forceinline__ void store_result(bf16_t *p, f32x4 o, float l) {
 }
 
 #include "paged_split.h"
+#include "paged_wide.h"
 
 struct Plan {
     int nq, q_groups;       // query tiles of 16 rows per workgroup, groups of them
     int cap;                // slices of the whole batch at most
     bool split;             // whether a sequence can have several
+    int wide;               // paged_wide.h: workgroups of an XCD, or 0
     SlicePlan slices;
 };
 
-constexpr int kWorkgroups = 512;      // slices are made up to this many workgroups
-constexpr int kLeast = 16;            // key tiles of a slice at least: two for each wavefront
+// One workgroup of 8 wavefronts holds a compute unit (its LDS): slices make up to that many, a second round costs what the first does
+// (two sequences of 131072 keys: 56 us with 256 workgroups, 67 with 512). A slice has 32 tiles of keys at least, four for each wavefront:
+// 512 keys in one slice take 8.6 us, in two with the launch that joins them 10.8.
+constexpr int kWorkgroups = 256, kLeast = 32;
 
-Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int dtype) {
+Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int dtype, int head_dim) {
     Plan p;
     max_rows = max_rows < rows ? max_rows : rows;
+    const int G = n_q_heads / c.n_kv_heads, pairs = ceil_div(c.batch * c.n_kv_heads, 8);      // of the fullest XCD
+    const int64_t blocks = (int64_t)pairs + (int64_t)ceil_div(c.n_kv_heads, 8) * ceil_div(rows * G, 128);
+    const int64_t bound = (int64_t)pairs * ceil_div(max_rows * G, 128);
+    p.wide = (int)(blocks < bound ? blocks : bound);
+    if (dtype != DKV_BF16 || head_dim != 128 || max_rows * G <= 64 || p.wide < 24) p.wide = 0;
     const int tiles = ceil_div(max_rows > 0 ? max_rows * (n_q_heads / c.n_kv_heads) : 1, 16), key_tiles = ceil_div(c.max_pages << c.page_shift, PKT);
     p.nq = dtype == DKV_BF16 && tiles > 1 ? 2 : 1;
     p.q_groups = ceil_div(tiles, p.nq);
     const int64_t whole = (int64_t)c.n_kv_heads * p.q_groups;       // workgroups of one slice for each sequence: batch times this
     p.split = key_tiles > kLeast && c.batch * whole < kWorkgroups;
-    p.slices.want = p.split ? (int)(kWorkgroups / whole) : 1;
-    p.slices.least = p.split ? kLeast : key_tiles;
-    const int64_t most = (int64_t)c.batch * ceil_div(key_tiles, p.slices.least), cap = (int64_t)c.batch + p.slices.want + 1;
-    p.cap = (int)(most < cap ? most : cap);
+    p.slices.split = p.split;
+    p.slices.want = Divisor(p.split ? (int)(kWorkgroups / whole) : 1);
+    p.slices.least = kLeast;
+    // at most `want` slices where that is twice the sequences or more (see slice_length), else `want` and one for each sequence
+    const int64_t most = (int64_t)c.batch * ceil_div(key_tiles, kLeast), cap = (int64_t)c.batch + p.slices.want.d + 1;
+    p.cap = !p.split ? c.batch : (int)(most < cap ? most : cap);
     return p;
 }
 
 size_t partial_bytes(const Plan &p, const PagedCache &c, int head_dim) {
-    return p.split ? (size_t)p.cap * c.n_kv_heads * (p.q_groups * p.nq * 16) * (head_dim + 4) * sizeof(float) : 0;
+    return p.split && !p.wide ? align_up(c.batch * sizeof(int2), 16) + (size_t)p.cap * c.n_kv_heads * (p.q_groups * p.nq * 16) * (head_dim + 4) * sizeof(float) : 0;
 }
 
 template <typename T, typename C, int DH, int NQ, int NW>
@@ -55,6 +66,8 @@ int launch_split(const PagedCache &c, const Plan &p, const void *q, int64_t q_st
                  int max_rows, int Hq, hipStream_t s) {
     constexpr int smem = NW * SplitSmem<T, DH>::WAVE_BYTES;
     const float scale_log2e = 1.4426950408889634f / sqrtf((float)DH);
+    int2 *meta = static_cast<int2 *>(part);
+    float *records = reinterpret_cast<float *>(static_cast<char *>(part) + align_up(c.batch * sizeof(int2), 16));
     const unsigned grid = (unsigned)(ceil_div(p.cap * c.n_kv_heads, 8) * 8 * p.q_groups);
 #define SPLIT(ONCE)                                                                                                              \
     do {                                                                                                                         \
@@ -65,17 +78,33 @@ int launch_split(const PagedCache &c, const Plan &p, const void *q, int64_t q_st
             lds_ok.store(true, std::memory_order_release);                                                                       \
         }                                                                                                                        \
         hipLaunchKernelGGL((paged_attn_split<T, C, DH, NQ, NW, ONCE>), dim3(grid), dim3(64 * NW), smem, s, c, p.slices, (const T *)q, \
-                           q_stride, row_off, (T *)out, (float *)part, rows, max_rows, Hq, p.q_groups, scale_log2e);             \
+                           q_stride, row_off, (T *)out, meta, records, rows, max_rows, Divisor(p.q_groups), Divisor(c.n_kv_heads), \
+                           Divisor(Hq / c.n_kv_heads), scale_log2e);                                                             \
     } while (0)
     if (p.q_groups == 1) SPLIT(true);
     else SPLIT(false);
 #undef SPLIT
     DKV_LAUNCH_CHECK();
     if (p.split) {
-        hipLaunchKernelGGL((paged_merge<T, DH>), dim3((unsigned)ceil_div(rows * Hq, 4)), dim3(256), 0, s, c, p.slices, row_off,
-                           (const float *)part, (T *)out, rows, max_rows, Hq, p.q_groups * NQ * 16);
+        hipLaunchKernelGGL((paged_merge<T, DH>), dim3((unsigned)ceil_div(rows * Hq, 4)), dim3(256), 0, s, row_off, c.batch,
+                           (const int2 *)meta, (const float *)records, (T *)out, rows, max_rows, Divisor(Hq), Divisor(Hq / c.n_kv_heads),
+                           p.q_groups * NQ * 16);
         DKV_LAUNCH_CHECK();
     }
+    return DKV_OK;
+}
+
+template <typename C>
+int launch_wide(const PagedCache &c, const Plan &p, const void *q, int64_t q_stride, const int *row_off, void *out, int rows, int max_rows,
+                int Hq, hipStream_t s) {
+    static std::atomic<bool> lds_ok{false};
+    if (!lds_ok.load(std::memory_order_acquire)) {
+        DKV_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(&paged_attn_wide<C>), hipFuncAttributeMaxDynamicSharedMemorySize, WIDE_LDS_BYTES));
+        lds_ok.store(true, std::memory_order_release);
+    }
+    hipLaunchKernelGGL(paged_attn_wide<C>, dim3((unsigned)p.wide * 8), dim3(256), WIDE_LDS_BYTES, s, c, (const bf16_t *)q, q_stride, row_off,
+                       (bf16_t *)out, rows, max_rows, Hq, 1.4426950408889634f / sqrtf(128.f));
+    DKV_LAUNCH_CHECK();
     return DKV_OK;
 }
 
@@ -83,6 +112,7 @@ template <typename T, typename C, int DH>
 int launch_heads(const PagedCache &c, const Plan &p, const void *q, int64_t q_stride, const int *row_off, void *out, void *part, int rows,
                  int max_rows, int Hq, hipStream_t s) {
     if constexpr (sizeof(T) == 4) return launch_split<T, C, DH, 1, 4>(c, p, q, q_stride, row_off, out, part, rows, max_rows, Hq, s);
+    else if (DH == 128 && p.wide) return launch_wide<C>(c, p, q, q_stride, row_off, out, rows, max_rows, Hq, s);
     else if (p.nq == 1) return launch_split<T, C, DH, 1, 8>(c, p, q, q_stride, row_off, out, part, rows, max_rows, Hq, s);
     else return launch_split<T, C, DH, 2, 8>(c, p, q, q_stride, row_off, out, part, rows, max_rows, Hq, s);
 }
@@ -102,9 +132,10 @@ int attn_call(const dkv_paged_cache *cache, PagedCache &view, Plan &plan, int32_
     }
     if (dtype != DKV_BF16 && dtype != DKV_FP32) { dkv_set_error("unknown dtype"); return DKV_E_INVALID_ARG; }
     if (cache->dtype != dtype && cache->dtype != DKV_E4M3) { dkv_set_error("rows of dtype %d do not read a cache of dtype %d", dtype, cache->dtype); return DKV_E_UNSUPPORTED; }
-    if ((int64_t)rows * n_q_heads < 1 << 24) {
-        plan = make_plan(view, n_q_heads, rows, max_rows_per_seq, dtype);
-        if ((int64_t)plan.cap * cache->n_kv_heads * plan.q_groups < 1 << 22) return DKV_OK;
+    if ((int64_t)rows * n_q_heads < 1 << 24 && (int64_t)cache->batch * cache->n_kv_heads < 1 << 22 &&
+        (int64_t)cache->batch * cache->max_pages * cache->page_size <= 1ll << 35) {
+        plan = make_plan(view, n_q_heads, rows, max_rows_per_seq, dtype, cache->head_dim);
+        if (plan.wide ? plan.wide < 1 << 20 : (int64_t)plan.cap * cache->n_kv_heads * plan.q_groups < 1 << 22) return DKV_OK;
     }
     dkv_set_error("%d rows of %d heads in %d sequences are too many for one call", rows, n_q_heads, cache->batch);
     return DKV_E_UNSUPPORTED;

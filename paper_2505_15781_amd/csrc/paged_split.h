@@ -18,19 +18,19 @@
 
 constexpr int PKT = 32;                // keys per tile
 
-// How the keys of a batch are cut: about `want` slices for one K/V head and query group over the whole batch, none
-// shorter than `least` tiles (before they are evened out within their sequence).
+// How the keys of a batch are cut: into at most `want` slices for one K/V head and query group over the whole batch where that
+// is possible (each sequence with rows has one at least), none shorter than `least` tiles before they are evened
+// out within their sequence. want = 0: one slice for each sequence.
 struct SlicePlan {
-    int want, least;
+    int least;
+    Divisor want;
+    bool split;
 };
 struct Slices {
-    int first, n, tiles;               // slices of the sequences before, slices and key tiles of this one
+    int first, n;                      // slices of the sequences before, and of this one
+    int b, r0, rows, keys;             // the sequence
 };
 
-__device__ __forceinline__ int key_tiles(const PagedCache &c, const int *row_off, int b) {
-    const int rows = row_off ? row_off[b + 1] - row_off[b] : 1;
-    return rows > 0 ? max(1, (c.keys(b) + PKT - 1) / PKT) : 0;
-}
 __device__ __forceinline__ int wave_prefix(int x) {        // inclusive: within rows of 16 lanes, then across the rows
     x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);
     x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
@@ -40,26 +40,59 @@ __device__ __forceinline__ int wave_prefix(int x) {        // inclusive: within 
     x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
     return x;
 }
-// Whole wavefronts. Finds the sequence that slice `at` of the batch belongs to (b < 0 on entry; false if there are fewer slices) or
-// the slices of sequence b.
-__device__ __forceinline__ bool find_slices(const PagedCache &c, const int *row_off, const SlicePlan &plan, int at, int &b, Slices &s) {
+// x / d rounded up for 0 <= x < 2^25, from an approximate quotient that is off by one at most
+__device__ __forceinline__ int ceil_div_fast(int x, int d) {
+    int q = (int)((float)x * __builtin_amdgcn_rcpf((float)d)), r = x - q * d;
+    if (r < 0) --q, r += d;
+    return q + (r > 0) + (r > d);
+}
+// Key tiles of a sequence: at least one where there are rows, which makes the slice that writes their zeros.
+__device__ __forceinline__ int key_tiles(int keys, int rows) { return rows > 0 ? max(1, (keys + PKT - 1) / PKT) : 0; }
+__device__ __forceinline__ int key_tiles(const PagedCache &c, const int *row_off, int b) {
+    return key_tiles(c.keys(b), row_off ? row_off[b + 1] - row_off[b] : 1);
+}
+// Key tiles of a slice: the least that makes at most `want` slices of the whole batch, or (where rounding up within the sequences
+// makes more than that) a length that surely does. Whole wavefronts; `tiles`: of sequence `lane`.
+__device__ __forceinline__ int slice_length(const PagedCache &c, const int *row_off, const SlicePlan &plan, int tiles) {
     const int lane = threadIdx.x & 63;
-    int tiles = lane < c.batch ? key_tiles(c, row_off, lane) : 0;
-    float total = (float)tiles;                            // the same sum in every wavefront: it need not be exact
-    for (int i = 64 + lane; i < c.batch; i += 64) total += (float)key_tiles(c, row_off, i);
-    total = wave_sum(total);
-    const int slice = __builtin_amdgcn_readfirstlane(max(plan.least, (int)ceilf(total / (float)plan.want)));
-    int before = 0;
+    auto sum = [&](auto f) {
+        int x = f(tiles);
+        for (int i = 64 + lane; i < c.batch; i += 64) x += f(key_tiles(c, row_off, i));
+        return __builtin_amdgcn_readlane(wave_prefix(x), 63);
+    };
+    const int total = sum([](int x) { return x; });
+    int slice = max(plan.least, plan.want.div(total + plan.want.d - 1));
+    if (sum([&](int x) { return ceil_div_fast(x, slice); }) > plan.want.d) slice = max(plan.least, ceil_div(total, max(plan.want.d - c.batch, 1)));
+    return slice;
+}
+// Whole wavefronts. Finds slice `at` of the batch; false if there are fewer.
+__device__ __forceinline__ bool find_slice(const PagedCache &c, const int *row_off, const SlicePlan &plan, int at, Slices &s) {
+    const int lane = threadIdx.x & 63;
+    if (!plan.split) {
+        if (at >= c.batch) return false;
+        s.b = s.first = at;
+        s.n = 1;
+        rows_of_sequence(row_off, at, s.r0, s.rows);
+        s.keys = c.keys(at);
+        return true;
+    }
+    int slice = 0, before = 0;
     for (int i = 0; i < c.batch; i += 64) {
-        if (i > 0) tiles = i + lane < c.batch ? key_tiles(c, row_off, i + lane) : 0;
-        const int n = (tiles + slice - 1) / slice, upto = before + wave_prefix(n);
-        const unsigned long long hit = b < 0 ? __builtin_amdgcn_ballot_w64(upto > at) : b < i + 64 ? 1ull << (b - i) : 0ull;
+        const int b = min(i + lane, c.batch - 1), keys = c.keys(b);
+        int r0, rows;
+        rows_of_sequence(row_off, b, r0, rows);
+        const int tiles = i + lane < c.batch ? key_tiles(keys, rows) : 0;
+        if (i == 0) slice = slice_length(c, row_off, plan, tiles);
+        const int n = ceil_div_fast(tiles, slice), upto = before + wave_prefix(n);
+        const unsigned long long hit = __builtin_amdgcn_ballot_w64(upto > at);
         if (hit) {
             const int l = __builtin_ctzll(hit);
-            b = i + l;
+            s.b = i + l;
             s.n = __builtin_amdgcn_readlane(n, l);
             s.first = __builtin_amdgcn_readlane(upto, l) - s.n;
-            s.tiles = __builtin_amdgcn_readlane(tiles, l);
+            s.r0 = __builtin_amdgcn_readlane(r0, l);
+            s.rows = __builtin_amdgcn_readlane(rows, l);
+            s.keys = __builtin_amdgcn_readlane(keys, l);
             return true;
         }
         before = __builtin_amdgcn_readlane(upto, 63);
@@ -125,9 +158,9 @@ __device__ __forceinline__ void softmax_step_f32(f32x4 (&st)[NT], float &m_run, 
 // T: rows (and LDS), C: cache, ONCE: one query group, so that nobody else reads these keys (non-temporal loads)
 template <typename T, typename C, int DH, int NQ, int NW, bool ONCE>
 __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c, SlicePlan plan, const T *__restrict__ Q, int64_t q_stride,
-                                                                    const int *__restrict__ row_off, T *__restrict__ out,
-                                                                    float *__restrict__ part, int rows, int max_rows, int Hq, int q_groups,
-                                                                    float scale_log2e) {
+                                                                    const int *__restrict__ row_off, T *__restrict__ out, int2 *__restrict__ meta,
+                                                                    float *__restrict__ part, int rows, int max_rows, Divisor groups, Divisor heads,
+                                                                    Divisor G, float scale_log2e) {
     using SM = SplitSmem<T, DH>;
     constexpr bool BF = sizeof(T) == 2;
     constexpr int REC = DH + 4;                       // floats per record: m, l, pad, pad, o[DH]
@@ -137,17 +170,17 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
     unsigned char *ksm = smem_raw + wave * SM::WAVE_BYTES, *vsm = ksm + SM::K_BYTES;
 
     // the query groups of a (slice, K/V head) read the same keys: consecutive workgroups of one XCD (id mod 8)
-    const int unit = (int)(blockIdx.x >> 3) / q_groups * 8 + (int)(blockIdx.x & 7), qg = (int)(blockIdx.x >> 3) % q_groups;
-    const int kvh = unit % c.n_kv_heads, at = unit / c.n_kv_heads;
-    int b = -1;
+    const int slot = (int)(blockIdx.x >> 3), unit = groups.div(slot) * 8 + (int)(blockIdx.x & 7), qg = groups.mod(slot);
+    const int at = heads.div(unit), kvh = heads.mod(unit);
     Slices sl;
-    if (!find_slices(c, row_off, plan, at, b, sl)) return;
-    const int G = Hq / c.n_kv_heads, len = c.keys(b);
-    int r0, nrows;
-    rows_of_sequence(row_off, b, r0, nrows);
-    const int nq = min(nrows, max_rows) * G, m0 = qg * NQ * 16;       // query rows of this (sequence, K/V head), first one here
+    if (!find_slice(c, row_off, plan, at, sl)) return;
+    const int b = sl.b, r0 = sl.r0, len = sl.keys;
+    const int nq = min(sl.rows, max_rows) * G.d, m0 = qg * NQ * 16;   // query rows of this (sequence, K/V head), first one here
     if (m0 >= nq) return;                                             // uniform for the workgroup
-    const int per = (sl.tiles + sl.n - 1) / sl.n, t_begin = (at - sl.first) * per, t_end = min(sl.tiles, t_begin + per);
+    const int tiles = key_tiles(len, 1), per = plan.split ? ceil_div_fast(tiles, sl.n) : tiles;
+    const int t_begin = (at - sl.first) * per, t_end = min(tiles, t_begin + per);
+    if (plan.split && tid == 0 && at == sl.first && kvh == 0 && qg == 0) meta[b] = make_int2(sl.first, sl.n);
+    const int64_t q_rows = groups.d * (NQ * 16);
 
     // Pages of this wavefront's tiles t_begin + wave + NW j: lane i has half i & 1 of tile j0 + i / 2. -1: none, or behind the end.
     auto load_pages = [&](int j0) {
@@ -210,22 +243,22 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
     int t = t_begin + wave, j = 0;
     pages = load_pages(0);
     pages_ahead = load_pages(32);
-    if (t < t_end) load_tile(t, 0);
-
     // Query operands. bf16: dims 32 ks + 8 g + [0, 8); fp32: dims 16 ks + 4 g + [0, 4), one of the four for each product
     constexpr int QS = BF ? DH / 32 : DH / 16;
     u32x4 qf[NQ][QS];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         const int mq = m0 + 16 * n + qi;
-        const bool ok = mq < nq && (unsigned)(r0 + mq / G) < (unsigned)rows;
-        const T *qp = Q + (ok ? (int64_t)(r0 + mq / G) * q_stride + (kvh * G + mq % G) * DH : 0) + (BF ? 8 : 4) * g;
+        const int r = r0 + G.div(mq);
+        const bool ok = mq < nq && (unsigned)r < (unsigned)rows;
+        const T *qp = Q + (ok ? r * q_stride + (kvh * G.d + G.mod(mq)) * DH : 0) + (BF ? 8 : 4) * g;
 #pragma unroll
         for (int ks = 0; ks < QS; ++ks) {
             const u32x4 x = *reinterpret_cast<const bf16x8_el *>(qp + (BF ? 32 : 16) * ks);
             qf[n][ks] = ok ? x : u32x4{0, 0, 0, 0};
         }
     }
+    if (t < t_end) load_tile(t, 0);
     const bf16x8 ones = row_sum_operand(lane);
     const unsigned char *vrow0 = vsm + (4 * g + (qi >> 2)) * SM::V_STRIDE + (qi & 3) * 8;      // bf16: see vt_operand
 
@@ -321,8 +354,8 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
 
     constexpr int CHUNKS = DH / 4;                    // a thread joins 4 output dims of a query row
     for (int idx = tid; idx < NQ * 16 * CHUNKS; idx += 64 * NW) {
-        const int qr = idx / CHUNKS, ch = idx % CHUNKS, mq = m0 + qr;
-        if (mq >= nq || (unsigned)(r0 + mq / G) >= (unsigned)rows) continue;
+        const int qr = idx / CHUNKS, ch = idx % CHUNKS, mq = m0 + qr, r = r0 + G.div(mq);
+        if (mq >= nq || (unsigned)r >= (unsigned)rows) continue;
         float mw[NW], M = -3.0e38f, lsum = 0.f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
@@ -338,9 +371,9 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
             o += wgt * *reinterpret_cast<const f32x4 *>(rec + 4 + 4 * ch);
         }
         if (sl.n == 1) {
-            store_result(out + ((size_t)(r0 + mq / G) * Hq + kvh * G + mq % G) * DH + 4 * ch, o, lsum);
+            store_result(out + (((size_t)r * c.n_kv_heads + kvh) * G.d + G.mod(mq)) * DH + 4 * ch, o, lsum);
         } else {
-            float *rec = part + ((size_t)unit * (q_groups * NQ * 16) + mq) * REC;
+            float *rec = part + (unit * q_rows + mq) * REC;
             if (ch == 0) {
                 rec[0] = M;
                 rec[1] = lsum;
@@ -352,29 +385,27 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
 
 // Joins the slices of one (row, query head): one wavefront each. Rows of sequences with one slice have their result already.
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void paged_merge(PagedCache c, SlicePlan plan, const int *__restrict__ row_off, const float *__restrict__ part,
-                                                   T *__restrict__ out, int rows, int max_rows, int Hq, int q_rows) {
+__global__ __launch_bounds__(256) void paged_merge(const int *__restrict__ row_off, int batch, const int2 *__restrict__ meta,
+                                                   const float *__restrict__ part, T *__restrict__ out, int rows, int max_rows, Divisor Hq,
+                                                   Divisor G, int q_rows) {
     constexpr int REC = DH + 4, CH = DH / 4, LANES = 64 / CH;      // CH lanes hold a record's output, LANES records at a time
-    const int lane = threadIdx.x & 63, pair = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6);
-    const int r = pair / Hq, h = pair % Hq;
+    const int lane = threadIdx.x & 63, pair = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int r = Hq.div(pair), h = Hq.mod(pair);
     if (r >= rows) return;
-    int b = sequence_of_row(row_off, c.batch, r);
-    if (b >= c.batch) return;
-    int r0, n;
-    rows_of_sequence(row_off, b, r0, n);
-    if (r - r0 >= max_rows) return;
-    Slices sl;
-    find_slices(c, row_off, plan, 0, b, sl);
-    if (sl.n <= 1) return;
-    const int G = Hq / c.n_kv_heads, mq = (r - r0) * G + h % G;
-    const size_t step = (size_t)c.n_kv_heads * q_rows * REC;
-    const float *rec = part + (((size_t)sl.first * c.n_kv_heads + h / G) * q_rows + mq) * REC;
+    const int b = sequence_of_row(row_off, batch, r);
+    if (b >= batch) return;
+    const int in = row_off ? r - row_off[b] : 0;
+    const int2 sl = meta[b];                                       // first slice, slices
+    if (in >= max_rows || sl.y <= 1) return;
+    const int kvh = G.div(h), mq = in * G.d + G.mod(h), heads = G.div(Hq.d);
+    const size_t step = (size_t)heads * q_rows * REC;
+    const float *rec = part + (((size_t)sl.x * heads + kvh) * q_rows + mq) * REC;
     float M = -3.0e38f;
-    for (int s = lane; s < sl.n; s += 64) M = fmaxf(M, rec[s * step]);
+    for (int s = lane; s < sl.y; s += 64) M = fmaxf(M, rec[s * step]);
     M = wave_max(M);
     float l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = lane / CH; s < sl.n; s += LANES) {
+    for (int s = lane / CH; s < sl.y; s += LANES) {
         const float *x = rec + s * step, w = __builtin_amdgcn_exp2f(x[0] - M);
         l += w * x[1];
         o += w * *reinterpret_cast<const f32x4 *>(x + 4 + 4 * (lane % CH));

@@ -168,7 +168,8 @@ ATTN = [  # lens, rows, page, kv heads, group, dh
     ([1], [1], 16, 1, 1, 128), ([0], [1], 16, 2, 2, 64), ([512], [1], 16, 4, 1, 128), ([31, 32, 33, 0, 1], [1, 2, 1, 3, 1], 16, 2, 4, 128),
     ([63, 64, 65, 127, 129], [3, 0, 17, 1, 16], 32, 2, 1, 64), ([1300, 7], [1, 5], 64, 2, 7, 128), ([5000], [2], 128, 1, 7, 128),
     ([333, 1000, 16], [40, 70, 16], 16, 3, 1, 128), ([769, 100, 257], [65, 129, 33], 32, 2, 7, 128), ([300, 513], [130, 257], 256, 2, 1, 64),
-    ([200, 40], [17, 23], 16, 4, 1, 32), ([2100], [1], 16, 1, 16, 32), ([640, 448], [300, 64], 64, 8, 4, 128), ([1, 2, 3], [130, 1, 140], 16, 26, 1, 128)]
+    ([200, 40], [17, 23], 16, 4, 1, 32), ([2100], [1], 16, 1, 16, 32), ([640, 448], [300, 64], 64, 8, 4, 128), ([1, 2, 3], [130, 1, 140], 16, 26, 1, 128),
+    ([1333, 64, 333, 0], [200, 100, 400, 70], 16, 8, 4, 128), ([63, 129, 1024], [300, 5, 900], 128, 32, 1, 128)]
 
 
 @pytest.mark.parametrize("types", ["bf16 bf16", "bf16 e4m3", "fp32 fp32", "fp32 e4m3"])
