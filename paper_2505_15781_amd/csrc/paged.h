@@ -16,9 +16,9 @@ struct PagedCache {
         const int id = table[(size_t)b * max_pages + (p >> page_shift)];
         return (unsigned)id < (unsigned)n_pages ? id : -1;
     }
-    // index of a (page, head, slot) row: times head_dim elements, or itself in the scales
-    __device__ __forceinline__ size_t row(int page, int head, int slot) const {
-        return (((size_t)page * n_kv_heads + head) << page_shift) + slot;
+    // index of a (page, head, slot) row: times head_dim elements, or itself in the scales. A cache has at most 2^32 rows.
+    __device__ __forceinline__ uint32_t row(int page, int head, int slot) const {
+        return (((uint32_t)page * n_kv_heads + head) << page_shift) + slot;
     }
     __device__ __forceinline__ int keys(int b) const { return max(0, min(seq_len[b], capacity())); }
 };

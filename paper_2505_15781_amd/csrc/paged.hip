@@ -64,9 +64,9 @@ __global__ __launch_bounds__(256) void paged_store_kernel(PagedCache c, const T 
     const int p = positions[r], page = c.page(b, p);
     if (page < 0 || i >= 2 * P * c.n_kv_heads) return;
     const int head = i / (2 * P), is_v = i / P % 2, piece = i % P;
-    const size_t at = c.row(page, head, p & (c.page_size() - 1));
+    const uint32_t at = c.row(page, head, p & (c.page_size() - 1));
     const f32x8 x = load8((is_v ? v_new : k_new) + r * row_stride + head * DH + 8 * piece);
-    store_piece<DH>(reinterpret_cast<C *>(is_v ? c.v : c.k) + at * DH, (is_v ? c.vs : c.ks) + at, piece, x);
+    store_piece<DH>(reinterpret_cast<C *>(is_v ? c.v : c.k) + (size_t)at * DH, (is_v ? c.vs : c.ks) + at, piece, x);
 }
 
 template <typename T, typename C, int DH>
@@ -81,8 +81,8 @@ __global__ __launch_bounds__(256) void paged_load_kernel(PagedCache c, T *__rest
     const int p = positions[r], page = c.page(b, p);
     f32x8 x = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (page >= 0) {
-        const size_t at = c.row(page, head, p & (c.page_size() - 1));
-        x = load8(reinterpret_cast<const C *>(is_v ? c.v : c.k) + at * DH + 8 * piece);
+        const uint32_t at = c.row(page, head, p & (c.page_size() - 1));
+        x = load8(reinterpret_cast<const C *>(is_v ? c.v : c.k) + (size_t)at * DH + 8 * piece);
         if (sizeof(C) == 1) x *= scale_value((is_v ? c.vs : c.ks)[at]);
     }
     store8((is_v ? v_out : k_out) + ((size_t)r * c.n_kv_heads + head) * DH + 8 * piece, x);
@@ -113,6 +113,7 @@ int dkv_paged_view(const dkv_paged_cache *c, PagedCache &view) {
         dkv_set_error("page_size %d not supported (a power of two, 16 to 65536)", c->page_size); return DKV_E_UNSUPPORTED;
     }
     if ((int64_t)c->max_pages * c->page_size > 1 << 30) { dkv_set_error("the table covers more than 2^30 positions"); return DKV_E_UNSUPPORTED; }
+    if ((int64_t)c->n_pages * c->n_kv_heads > (1ll << 32) / c->page_size) { dkv_set_error("more than 2^32 rows of keys in one cache"); return DKV_E_UNSUPPORTED; }
     if ((reinterpret_cast<uintptr_t>(c->k_pages) | reinterpret_cast<uintptr_t>(c->v_pages)) % 16) { dkv_set_error("pages must be 16-byte aligned"); return DKV_E_INVALID_ARG; }
     view = PagedCache{static_cast<unsigned char *>(c->k_pages), static_cast<unsigned char *>(c->v_pages), c->k_scale, c->v_scale,
                       c->page_table, c->seq_len, c->batch, c->n_pages, c->max_pages, __builtin_ctz((unsigned)c->page_size), c->n_kv_heads};

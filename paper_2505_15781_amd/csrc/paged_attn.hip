@@ -26,7 +26,7 @@ struct Plan {
     int nq, q_groups;       // query tiles of 16 rows per workgroup, groups of them
     int cap;                // slices of the whole batch at most
     bool split;             // whether a sequence can have several
-    int wide;               // paged_wide.h: workgroups of an XCD, or 0
+    int wide, wide_groups;  // paged_wide.h: blocks of 128 query rows at most, or 0; groups of wavefronts in a workgroup
     SlicePlan slices;
 };
 
@@ -38,15 +38,21 @@ constexpr int kWorkgroups = 256, kLeast = 32;
 Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int dtype, int head_dim) {
     Plan p;
     max_rows = max_rows < rows ? max_rows : rows;
-    const int G = n_q_heads / c.n_kv_heads, pairs = ceil_div(c.batch * c.n_kv_heads, 8);      // of the fullest XCD
-    const int64_t blocks = (int64_t)pairs + (int64_t)ceil_div(c.n_kv_heads, 8) * ceil_div(rows * G, 128);
-    const int64_t bound = (int64_t)pairs * ceil_div(max_rows * G, 128);
-    p.wide = (int)(blocks < bound ? blocks : bound);
-    if (dtype != DKV_BF16 || head_dim != 128 || max_rows * G <= 64 || p.wide < 24) p.wide = 0;
-    const int tiles = ceil_div(max_rows > 0 ? max_rows * (n_q_heads / c.n_kv_heads) : 1, 16), key_tiles = ceil_div(c.max_pages << c.page_shift, PKT);
+    const int G = n_q_heads / c.n_kv_heads;
+    const int tiles = ceil_div(max_rows > 0 ? max_rows * G : 1, 16), key_tiles = ceil_div(c.max_pages << c.page_shift, PKT);
     p.nq = dtype == DKV_BF16 && tiles > 1 ? 2 : 1;
     p.q_groups = ceil_div(tiles, p.nq);
     const int64_t whole = (int64_t)c.n_kv_heads * p.q_groups;       // workgroups of one slice for each sequence: batch times this
+    // Blocks of 128 query rows (paged_wide.h) where tiles of 32 would make more than one round of workgroups: 28/4 heads, 1024 keys, 1
+    // sequence of 300 rows (264 workgroups) 42 -> 22 us, 4 of 128 rows (448) 30 -> 23, but 4 of 64 rows (224) 19 -> 22 and 16 of 16
+    // rows (256) 18 -> 25; 4096 keys the same way round. Two groups of wavefronts to a workgroup where the blocks are few and the
+    // keys many enough to share: 96 blocks of 1024 keys 24.8 -> 22.5 us, 384 blocks 41 -> 47, 128 blocks of 256 keys 11.8 -> 12.6.
+    p.wide = p.wide_groups = 0;
+    if (dtype == DKV_BF16 && head_dim == 128 && max_rows * G > 64 && c.batch * whole > kWorkgroups) {
+        const int64_t blocks = c.batch + (int64_t)ceil_div(rows * G, 128), bound = (int64_t)c.batch * ceil_div(max_rows * G, 128);
+        p.wide = (int)((blocks < bound ? blocks : bound) * c.n_kv_heads);
+        p.wide_groups = p.wide <= 320 && key_tiles > 16 ? 2 : 1;
+    }
     p.split = key_tiles > kLeast && c.batch * whole < kWorkgroups;
     p.slices.split = p.split;
     p.slices.want = Divisor(p.split ? (int)(kWorkgroups / whole) : 1);
@@ -94,16 +100,17 @@ int launch_split(const PagedCache &c, const Plan &p, const void *q, int64_t q_st
     return DKV_OK;
 }
 
-template <typename C>
+template <typename C, int KS>
 int launch_wide(const PagedCache &c, const Plan &p, const void *q, int64_t q_stride, const int *row_off, void *out, int rows, int max_rows,
                 int Hq, hipStream_t s) {
     static std::atomic<bool> lds_ok{false};
     if (!lds_ok.load(std::memory_order_acquire)) {
-        DKV_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(&paged_attn_wide<C>), hipFuncAttributeMaxDynamicSharedMemorySize, WIDE_LDS_BYTES));
+        DKV_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(&paged_attn_wide<C, KS>), hipFuncAttributeMaxDynamicSharedMemorySize, KS * WIDE_LDS_BYTES));
         lds_ok.store(true, std::memory_order_release);
     }
-    hipLaunchKernelGGL(paged_attn_wide<C>, dim3((unsigned)p.wide * 8), dim3(256), WIDE_LDS_BYTES, s, c, (const bf16_t *)q, q_stride, row_off,
-                       (bf16_t *)out, rows, max_rows, Hq, 1.4426950408889634f / sqrtf(128.f));
+    hipLaunchKernelGGL((paged_attn_wide<C, KS>), dim3((unsigned)p.wide), dim3(256 * KS), KS * WIDE_LDS_BYTES, s, c, (const bf16_t *)q, q_stride, row_off,
+                       (bf16_t *)out, rows, max_rows, Divisor(c.n_kv_heads), Divisor(Hq / c.n_kv_heads), kWorkgroups / c.n_kv_heads,
+                       1.4426950408889634f / sqrtf(128.f));
     DKV_LAUNCH_CHECK();
     return DKV_OK;
 }
@@ -112,7 +119,8 @@ template <typename T, typename C, int DH>
 int launch_heads(const PagedCache &c, const Plan &p, const void *q, int64_t q_stride, const int *row_off, void *out, void *part, int rows,
                  int max_rows, int Hq, hipStream_t s) {
     if constexpr (sizeof(T) == 4) return launch_split<T, C, DH, 1, 4>(c, p, q, q_stride, row_off, out, part, rows, max_rows, Hq, s);
-    else if (DH == 128 && p.wide) return launch_wide<C>(c, p, q, q_stride, row_off, out, rows, max_rows, Hq, s);
+    else if (DH == 128 && p.wide_groups == 1) return launch_wide<C, 1>(c, p, q, q_stride, row_off, out, rows, max_rows, Hq, s);
+    else if (DH == 128 && p.wide) return launch_wide<C, 2>(c, p, q, q_stride, row_off, out, rows, max_rows, Hq, s);
     else if (p.nq == 1) return launch_split<T, C, DH, 1, 8>(c, p, q, q_stride, row_off, out, part, rows, max_rows, Hq, s);
     else return launch_split<T, C, DH, 2, 8>(c, p, q, q_stride, row_off, out, part, rows, max_rows, Hq, s);
 }
@@ -135,7 +143,7 @@ int attn_call(const dkv_paged_cache *cache, PagedCache &view, Plan &plan, int32_
     if ((int64_t)rows * n_q_heads < 1 << 24 && (int64_t)cache->batch * cache->n_kv_heads < 1 << 22 &&
         (int64_t)cache->batch * cache->max_pages * cache->page_size <= 1ll << 35) {
         plan = make_plan(view, n_q_heads, rows, max_rows_per_seq, dtype, cache->head_dim);
-        if (plan.wide ? plan.wide < 1 << 20 : (int64_t)plan.cap * cache->n_kv_heads * plan.q_groups < 1 << 22) return DKV_OK;
+        if (plan.wide ? plan.wide < 1 << 23 : (int64_t)plan.cap * cache->n_kv_heads * plan.q_groups < 1 << 22) return DKV_OK;
     }
     dkv_set_error("%d rows of %d heads in %d sequences are too many for one call", rows, n_q_heads, cache->batch);
     return DKV_E_UNSUPPORTED;

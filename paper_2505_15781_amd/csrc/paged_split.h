@@ -196,9 +196,9 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
         const int key = t * PKT, slot = key & (c.page_size() - 1), slot1 = (key + 16) & (c.page_size() - 1);
         seen0 = id0 < 0 ? 0 : min(16, len - key);
         seen1 = id1 < 0 ? 0 : min(16, len - key - 16);
-        const size_t row0 = c.row(max(id0, 0), kvh, slot), row1 = c.row(max(id1, 0), kvh, slot1);
+        const uint32_t row0 = c.row(max(id0, 0), kvh, slot), row1 = c.row(max(id1, 0), kvh, slot1);
         auto fetch = [&](u32x4 (&reg)[N], const unsigned char *base) {
-            const unsigned char *p0 = base + row0 * ROW, *p1 = base + row1 * ROW;
+            const unsigned char *p0 = base + (size_t)row0 * ROW, *p1 = base + (size_t)row1 * ROW;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const unsigned char *p;

@@ -12,6 +12,7 @@
 
 typedef __attribute__((address_space(3))) void *lds_ptr_t;
 template <int V> struct StageC { static constexpr int value = V; };
+constexpr float kLag = 8.f;                          // log2 of the largest probability
 constexpr int WIDE_LDS_BYTES = 4 * 64 * 256;         // K0 K1 V0 V1, rows of 256 bytes
 
 // Place of the 16-byte chunk c of row r: c ^ wide_swizzle(r) (see attn_wide.h).
@@ -19,22 +20,51 @@ __device__ __forceinline__ int wide_swizzle(int row) { return ((row & 3) << 2) |
 
 __device__ __align__(256) const u32x4 zero_row[16] = {};
 
-// Work item of this workgroup. The blocks of a (sequence, K/V head) pair read the same keys and live on one XCD, pair % 8; workgroups
-// are handed out to the blocks that hold rows, pair by pair, so that none without rows stands between others.
-__device__ __forceinline__ bool wide_item(const PagedCache &c, const int *row_off, int max_rows, int G, int &pair, int &qb) {
-    const int lane = threadIdx.x & 63, slot = blockIdx.x >> 3, pairs = c.batch * c.n_kv_heads;
+// Work item of this workgroup: the sequences in the order of their key tiles, the longest first (64 of them at a time), so that
+// compute units that get two workgroups get short ones, and none without rows stands between others. Within a sequence the K/V
+// heads go fastest: the blocks of a head, which read the same keys, are on one XCD (id % 8) with 8 heads, on two with 4.
+// With two groups of wavefronts a workgroup takes one block of a long sequence, a group each half of its key tiles (parts = 2), or two
+// blocks of a short one, a group each: as many sequences are long as `units` workgroups (one per compute unit) have room for.
+struct WideItem {
+    Slices seq;
+    int kvh, qb, parts;                // qb: the first block
+};
+template <int KS>
+__device__ __forceinline__ bool wide_item(const PagedCache &c, const int *row_off, int max_rows, Divisor heads, int G, int units, WideItem &w) {
+    const int lane = threadIdx.x & 63, at = heads.div(blockIdx.x);
+    w.kvh = heads.mod(blockIdx.x);
     int before = 0;
-    for (int p0 = blockIdx.x & 7; p0 < pairs; p0 += 512) {
-        const int p = p0 + 8 * lane, b = min(p, pairs - 1) / c.n_kv_heads;
-        int r0, n;
-        rows_of_sequence(row_off, b, r0, n);
-        n = p < pairs ? (max(0, min(n, max_rows)) * G + 127) / 128 : 0;
+    for (int i = 0; i < c.batch; i += 64) {
+        const int b = min(i + lane, c.batch - 1), keys = c.keys(b);
+        int r0, rows;
+        rows_of_sequence(row_off, b, r0, rows);
+        const int blocks = i + lane < c.batch ? (max(0, min(rows, max_rows)) * G + 127) / 128 : 0, cost = (keys + 63) / 64;
+        int rank = 0;                                      // sequences before this one
+        for (int k = 0; k < min(64, c.batch - i); ++k) {
+            const int other = __builtin_amdgcn_readlane(cost, k);
+            rank += other > cost || (other == cost && k < lane);
+        }
+        if (i + lane >= c.batch) rank = lane;
+        int n = __builtin_amdgcn_ds_permute(rank << 2, blocks);
+        const int from = __builtin_amdgcn_ds_permute(rank << 2, lane);
+        int parts = 1;
+        if constexpr (KS == 2) {
+            const int pairs = (n + 1) / 2, one = __builtin_amdgcn_ds_permute(rank << 2, (int)(cost <= 1)) ? pairs : n;
+            // workgroups if this sequence and all before it are long
+            const int all = __builtin_amdgcn_readlane(wave_prefix(pairs), 63) + wave_prefix(one - pairs);
+            parts = c.batch <= 64 && one == n && all <= units ? 2 : 1;
+            n = parts == 2 ? n : pairs;
+        }
         const int upto = before + wave_prefix(n);
-        const unsigned long long behind = __builtin_amdgcn_ballot_w64(upto > slot);
+        const unsigned long long behind = __builtin_amdgcn_ballot_w64(upto > at);
         if (behind) {
-            const int at = __builtin_ctzll(behind);
-            pair = p0 + 8 * at;
-            qb = slot - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(n, at));
+            const int k = __builtin_ctzll(behind), l = __builtin_amdgcn_readlane(from, k);
+            w.parts = __builtin_amdgcn_readlane(parts, k);
+            w.qb = (at - (__builtin_amdgcn_readlane(upto, k) - __builtin_amdgcn_readlane(n, k))) * (KS == 2 && w.parts == 1 ? 2 : 1);
+            w.seq.b = i + l;
+            w.seq.r0 = __builtin_amdgcn_readlane(r0, l);
+            w.seq.rows = __builtin_amdgcn_readlane(rows, l);
+            w.seq.keys = __builtin_amdgcn_readlane(keys, l);
             return true;
         }
         before = __builtin_amdgcn_readlane(upto, 63);
@@ -44,65 +74,77 @@ __device__ __forceinline__ bool wide_item(const PagedCache &c, const int *row_of
 
 // Where a tile of 64 keys is: the rows (see PagedCache::row) of its four groups of 16 keys, and which of them have a page.
 struct WideTile {
-    size_t row[4];
+    uint32_t row[4];
     int pages;
 };
 
-template <typename C>
-__global__ __launch_bounds__(256, 2) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_attn_wide(
+template <typename C, int KS>
+__global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_attn_wide(
     PagedCache c, const bf16_t *__restrict__ Q, int64_t q_stride, const int *__restrict__ row_off, bf16_t *__restrict__ out, int rows,
-    int max_rows, int Hq, float scale_log2e) {
+    int max_rows, Divisor heads, Divisor G, int units, float scale_log2e) {
     constexpr int NW = 4, DH = 128, ROW = DH * 2, KT2 = 64, TILE = KT2 * ROW;     // bytes of an LDS row, of a K or V tile
     constexpr bool E4M3 = sizeof(C) == 1;
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem_all[];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int G = Hq / c.n_kv_heads;
+    // KS groups of four wavefronts, in LDS stages of their own
+    const int tid = threadIdx.x & 255, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int group_id = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 8);
+    unsigned char *smem_raw = smem_all + group_id * WIDE_LDS_BYTES;
     const int qi = lane & 31, g = lane >> 5, l16 = lane & 15, l4 = lane >> 4;
     const uint32_t lds_base = (uint32_t)(size_t)(lds_ptr_t)smem_raw;
-    int pair, qb;
-    if (!wide_item(c, row_off, max_rows, G, pair, qb)) return;
-    const int kvh = pair % c.n_kv_heads, b = pair / c.n_kv_heads;
-    int r0, nrows;
-    rows_of_sequence(row_off, b, r0, nrows);
-    const int nq = min(nrows, max_rows) * G, mb0 = qb * NW * 32;
-    const int L = c.keys(b), n_tiles = max(1, (L + KT2 - 1) / KT2);
+    WideItem item;
+    if (!wide_item<KS>(c, row_off, max_rows, heads, G.d, units, item)) return;
+    const int b = item.seq.b, r0 = item.seq.r0, L = item.seq.keys, kvh = item.kvh;
+    // a group works on the tiles part, part + parts, ... of the sequence
+    const int parts = KS == 1 ? 1 : item.parts, part = parts == 1 ? 0 : group_id;
+    const int n_tiles = (max(1, (L + KT2 - 1) / KT2) + parts - 1) / parts;
+    const int nq = min(item.seq.rows, max_rows) * G.d, mb0 = (item.qb + (parts == 1 ? group_id : 0)) * NW * 32;
 
-    // pages of the 64 groups of 16 keys of a window, a lane each; -1: none, or behind the end
-    auto load_pages = [&](int window) {
-        const int key = (window * 64 + lane) * 16;
-        return key < L ? c.page(b, key) : -1;
-    };
-    int pages = load_pages(0), pages_ahead = load_pages(1);
-    auto find = [&](int t) {                        // tiles in order
-        WideTile x;
-        x.pages = 0;
+    // this lane's query row; rows beyond the host's bound have no slot in Q and out
+    const int mq = mb0 + wave * 32 + qi, r = r0 + G.div(mq), h = kvh * G.d + G.mod(mq);
+    const bool q_ok = mq < nq && (unsigned)r < (unsigned)rows;
+    bf16x8 qf[DH / 16];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int id = __builtin_amdgcn_readlane(pages, (t & 15) * 4 + i);
-            x.pages |= (id >= 0) << i;
-            x.row[i] = c.row(max(id, 0), kvh, (t * KT2 + 16 * i) & (c.page_size() - 1));
-        }
-        if ((t & 15) == 15) {
+    for (int i = 0; i < DH / 16; ++i)
+        qf[i] = __builtin_bit_cast(bf16x8, (u32x4)*reinterpret_cast<const bf16x8_el *>(Q + (q_ok ? r * q_stride + h * DH : 0) + 8 * g + 16 * i));
+    // The 64 groups of 16 keys of a window, a lane each: the row of the first key, and (a bit each) whether there is a page.
+    auto look_up = [&](int window, uint32_t &row, unsigned long long &pages) {
+        const int key = (window * 64 + lane) * 16, id = key < L ? c.page(b, key) : -1;
+        row = c.row(max(id, 0), kvh, key & (c.page_size() - 1));
+        pages = __builtin_amdgcn_ballot_w64(id >= 0);
+    };
+    uint32_t group, group_ahead;
+    unsigned long long pages, pages_ahead;
+    look_up(0, group, pages);
+    look_up(1, group_ahead, pages_ahead);
+    auto find = [&](int step) {                     // steps in order
+        const int t = step * parts + part;
+        WideTile x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x.row[i] = __builtin_amdgcn_readlane(group, (t & 15) * 4 + i);
+        x.pages = (int)(pages >> ((t & 15) * 4)) & 15;
+        if ((t & 15) >= 16 - parts) {
+            group = group_ahead;
             pages = pages_ahead;
-            pages_ahead = load_pages((t >> 4) + 2);
+            look_up((t >> 4) + 2, group_ahead, pages_ahead);
         }
         return x;
     };
     // keys that are there of a tile's group
-    auto there = [&](int t, int tile_pages, int i) { return tile_pages >> i & 1 ? L - (t * KT2 + 16 * i) : 0; };
+    auto there = [&](int step, int tile_pages, int i) { return tile_pages >> i & 1 ? L - ((step * parts + part) * KT2 + 16 * i) : 0; };
+    auto whole = [&](int step, int tile_pages) { return tile_pages == 15 && (step * parts + part + 1) * KT2 <= L; };
 
     // bf16. Load i of a wavefront fills rows 16 i + 4 wave + [0, 4) of a tile; lane -> row lane / 16, place lane % 16.
     const uint32_t chunk = (l16 ^ wide_swizzle(4 * wave + l4)) << 4;
     auto fill = [&](const unsigned char *base, const WideTile &x, int t, uint32_t dst) {
-        if (x.pages == 15 && (t + 1) * KT2 <= L) {
+        if (whole(t, x.pages)) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                dma16_at(l4 * ROW + chunk, base + (x.row[i] + 4 * wave) * ROW, lds_base + dst + (16 * i + 4 * wave) * ROW);
+                dma16_at(l4 * ROW + chunk, base + (size_t)(x.row[i] + 4 * wave) * ROW, lds_base + dst + (16 * i + 4 * wave) * ROW);
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const unsigned char *p = base + (x.row[i] + 4 * wave + l4) * ROW;
+                const unsigned char *p = base + (size_t)(x.row[i] + 4 * wave + l4) * ROW;
                 dma16((4 * wave + l4 < there(t, x.pages, i) ? p : reinterpret_cast<const unsigned char *>(zero_row)) + chunk,
                       lds_base + dst + (16 * i + 4 * wave) * ROW);
             }
@@ -115,13 +157,13 @@ __global__ __launch_bounds__(256, 2) __attribute__((amdgpu_waves_per_eu(2, 2))) 
     auto fetch = [&](u32x4 (&reg)[2], uint32_t (&scale)[2], const unsigned char *base, const uint8_t *scales, const WideTile &x) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const size_t row = wave >> 1 ? x.row[2 * i + 1] : x.row[2 * i];
-            reg[i] = *reinterpret_cast<const u32x4 *>(base + row * DH + r16 * DH + 16 * (lane & 7));
-            scale[i] = scales[row + r16];
+            const size_t row = wave >> 1 ? x.row[2 * i + 1] : x.row[2 * i];      // uniform
+            reg[i] = *reinterpret_cast<const u32x4 *>(base + row * DH + (uint32_t)(r16 * DH + 16 * (lane & 7)));
+            scale[i] = (scales + row)[(uint32_t)r16];
         }
     };
     auto convert = [&](const u32x4 (&reg)[2], const uint32_t (&scale)[2], int tile_pages, int t, uint32_t dst) {
-        const bool whole = tile_pages == 15 && (t + 1) * KT2 <= L;    // uniform
+        const bool all = whole(t, tile_pages);                        // uniform
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int row = 32 * i + 8 * wave + (lane >> 3), sw = wide_swizzle(row);
@@ -132,40 +174,31 @@ __global__ __launch_bounds__(256, 2) __attribute__((amdgpu_waves_per_eu(2, 2))) 
                 y[e >> 1][2 * (e & 1)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(reg[i][e], s, false));
                 y[e >> 1][2 * (e & 1) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(reg[i][e], s, true));
             }
-            if (!whole && r16 >= there(t, tile_pages, 2 * i + (wave >> 1))) y[0] = y[1] = u32x4{0, 0, 0, 0};
+            if (!all && r16 >= there(t, tile_pages, 2 * i + (wave >> 1))) y[0] = y[1] = u32x4{0, 0, 0, 0};
 #pragma unroll
             for (int e = 0; e < 2; ++e)
                 *reinterpret_cast<u32x4 *>(smem_raw + dst + row * ROW + (((2 * (lane & 7) + e) ^ sw) << 4)) = y[e];
         }
     };
-    // this lane's query row; rows beyond the host's bound have no slot in Q and out
-    const int mq = mb0 + wave * 32 + qi, r = r0 + mq / G, h = kvh * G + mq % G;
-    const bool q_ok = mq < nq && (unsigned)r < (unsigned)rows;
-    bf16x8 qf[DH / 16];
-#pragma unroll
-    for (int ks = 0; ks < DH / 16; ++ks)
-        qf[ks] = __builtin_bit_cast(bf16x8, (u32x4)*reinterpret_cast<const bf16x8_el *>(Q + (q_ok ? r * q_stride + h * DH : 0) + 8 * g + 16 * ks));
     // pages of the tiles t, t + 1, t + 2 (of the last ones: of some tile), and where tile t + 1 (bf16) or t + 2 (e4m3) is
     int pages_0, pages_1, pages_2;
     WideTile x = find(0), ahead = x;
     pages_0 = pages_1 = pages_2 = x.pages;
-    if constexpr (E4M3) {
-        fetch(kreg, k_scale, c.k, c.ks, x);
+    if constexpr (E4M3) {                        // all loads at once: K0 V0 K1, and V1 K2 for the loop
+        u32x4 k0[2], v0[2], k1[2];
+        uint32_t k0_scale[2], v0_scale[2], k1_scale[2];
+        fetch(k0, k0_scale, c.k, c.ks, x);
+        fetch(v0, v0_scale, c.v, c.vs, x);
+        if (n_tiles > 1) x = find(1);
+        pages_1 = x.pages;
+        fetch(k1, k1_scale, c.k, c.ks, x);
         fetch(vreg, v_scale, c.v, c.vs, x);
-        convert(kreg, k_scale, pages_0, 0, 0);
-        convert(vreg, v_scale, pages_0, 0, 2 * TILE);
-        if (n_tiles > 1) {
-            x = find(1);
-            pages_1 = x.pages;
-            fetch(kreg, k_scale, c.k, c.ks, x);
-            fetch(vreg, v_scale, c.v, c.vs, x);
-            convert(kreg, k_scale, pages_1, 1, TILE);
-        }
-        if (n_tiles > 2) {
-            x = find(2);
-            pages_2 = x.pages;
-            fetch(kreg, k_scale, c.k, c.ks, x);
-        }
+        if (n_tiles > 2) x = find(2);
+        pages_2 = x.pages;
+        fetch(kreg, k_scale, c.k, c.ks, x);
+        convert(k0, k0_scale, pages_0, 0, 0);
+        convert(v0, v0_scale, pages_0, 0, 2 * TILE);
+        convert(k1, k1_scale, pages_1, 1, TILE);
     } else {
         fill(c.k, x, 0, 0);
         fill(c.v, x, 0, 2 * TILE);
@@ -186,14 +219,7 @@ __global__ __launch_bounds__(256, 2) __attribute__((amdgpu_waves_per_eu(2, 2))) 
     // lowest finite start: scores of -inf then give probabilities of zero, also where a whole half tile is masked
     float m_run = -3.0e38f, alpha = 1.f;
     bool behind = false;
-    // sum of exactly the rounded probabilities of the second product: a product with a tile whose row 0 is ones; element 0
-    // of the lanes below 32 is the sum of query qi, everything else stays zero
-    f32x16 l_acc;
-    bf16x8 ones;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) l_acc[v] = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) ones[e] = qi == 0 ? (__bf16)1.0f : (__bf16)0.0f;
+    float l[2] = {0.f, 0.f};                     // sums of this lane's probabilities
     f32x16 acc[DH / 32], stA, stB;               // stA, stB: scores of the first and the second 32 keys of a tile
     bf16x8 pA[2], pB[2];                         // their probabilities
 #pragma unroll
@@ -221,29 +247,28 @@ __global__ __launch_bounds__(256, 2) __attribute__((amdgpu_waves_per_eu(2, 2))) 
         for (int v = 0; v < 16; ++v) sn[v] = 0.f;
         f32x8 p[2];
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) l_acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ones, pv[ks], l_acc, 0, 0, 0);
-#pragma unroll
         for (int i = 0; i < 8; ++i) {
             sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(i, kstage, khalf), qf[i], sn, 0, 0, 0);
             acc[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(i & 3, i >> 2, vstage, vhalf), pv[i >> 2], acc[i & 3], 0, 0, 0);
 #pragma unroll
             for (int e = 2 * i; e < 2 * i + 2; ++e)
                 p[e >> 3][e & 7] = __builtin_amdgcn_exp2f(fmaf(so[e], scale_log2e, -m_run));
+            l[0] += p[i >> 2][2 * (i & 3)];
+            l[1] += p[i >> 2][2 * (i & 3) + 1];
         }
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) pn[ks] = __builtin_convertvector(p[ks], bf16x8);
         asm volatile("" : "+v"(pn[0]), "+v"(pn[1]));        // here, not behind the branches of maximum()
         __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
             __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-            __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
             __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
         }
     };
@@ -252,29 +277,34 @@ __global__ __launch_bounds__(256, 2) __attribute__((amdgpu_waves_per_eu(2, 2))) 
         if (!behind) return;
 #pragma unroll
         for (int mt = 0; mt < DH / 32; ++mt) acc[mt] *= alpha;
-        l_acc[0] *= alpha;
     };
-    // Maximum of half `half` of tile t. The running maximum is the reference of the exponentials, so that the largest
-    // probability is exactly 1. The probabilities of the half tile before still wait for their product: the output is
-    // rescaled to the new reference only behind that product, at the next call.
+    // Maximum of half `half` of tile t. The reference of the exponentials follows it only where it gets more than 2^8 ahead: probabilities
+    // go up to 2^8 then, which costs fp32 sums and the rounding to bf16 (half a step of the value, whatever its size) nothing but that
+    // the largest one is no longer exact, and of a wavefront's vector instructions a third, the rescaling of the output at
+    // nearly every half tile (32 queries, each with a new maximum now and then): 4 sequences x 32 heads, 1536 rows and keys 205 -> 193 us.
+    // The probabilities of the half tile before still wait for their product: the output is rescaled to the new reference
+    // only behind that product, at the next call.
     auto maximum = [&](f32x16 &st, int t, int half, int tile_pages) {
         rescale();
-        if ((tile_pages >> (2 * half) & 3) != 3 || t * KT2 + 32 * half + 32 > L) {           // uniform
+        if (!whole(t, tile_pages)) {                                   // uniform
             const int left[2] = {there(t, tile_pages, 2 * half), there(t, tile_pages, 2 * half + 1)};
 #pragma unroll
             for (int v = 0; v < 16; ++v)
                 if (8 * (v >> 2 & 1) + 4 * g + (v & 3) >= left[v >> 3]) st[v] = -INFINITY;
         }
-        float mx = st[0];
+        float mx = st[0];                // a NaN goes on: v_maximum3_f32 needs no canonical operands, v_max3_f32 does
 #pragma unroll
-        for (int v = 1; v < 16; ++v) mx = fmaxf(mx, st[v]);
+        for (int v = 1; v < 16; ++v) mx = __builtin_elementwise_maximum(mx, st[v]);
         float u, w;
         swap_rows32(mx, u, w);
         mx = fmaxf(u, w) * scale_log2e;
+        behind = __builtin_amdgcn_ballot_w64(mx > m_run + kLag) != 0;
+        if (!behind) return;
         const float m_new = fmaxf(m_run, mx);
-        behind = __builtin_amdgcn_ballot_w64(m_new > m_run) != 0;       // else the factor is exactly 1 for every query
         alpha = __builtin_amdgcn_exp2f(m_run - m_new);
         m_run = m_new;
+        l[0] *= alpha;
+        l[1] *= alpha;
     };
     auto tile_barrier = [&]() {
         asm volatile("" ::: "memory");
@@ -331,16 +361,36 @@ __global__ __launch_bounds__(256, 2) __attribute__((amdgpu_waves_per_eu(2, 2))) 
     const int last = (n_tiles - 1) & 1;
     rescale();
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) l_acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ones, pB[ks], l_acc, 0, 0, 0);
-#pragma unroll
     for (int i = 0; i < 8; ++i)
         acc[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(i & 3, i >> 2, last, 1), pB[i >> 2], acc[i & 3], 0, 0, 0);
 
     float u, w;
-    swap_rows32(l_acc[0], u, w);
-    const float inv = u + w == 0.f ? 0.f : 1.f / (u + w);
+    swap_rows32(l[0] + l[1], u, w);
+    float sum = u + w;
+    if (KS == 2 && parts == 2) {                 // the second group's state goes through LDS to the same lanes of the first
+        f32x4 *parked = reinterpret_cast<f32x4 *>(smem_all + WIDE_LDS_BYTES);
+        float2 *stats = reinterpret_cast<float2 *>(smem_all);
+        __syncthreads();
+        if (part == 1) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) parked[i * 256 + tid] = f32x4{acc[i >> 2][4 * (i & 3)], acc[i >> 2][4 * (i & 3) + 1], acc[i >> 2][4 * (i & 3) + 2], acc[i >> 2][4 * (i & 3) + 3]};
+            stats[tid] = make_float2(m_run, sum);
+        }
+        __syncthreads();
+        if (part == 1) return;
+        const float2 other = stats[tid];
+        const float m = fmaxf(m_run, other.x), mine = __builtin_amdgcn_exp2f(m_run - m), theirs = __builtin_amdgcn_exp2f(other.x - m);
+        sum = mine * sum + theirs * other.y;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const f32x4 x = parked[i * 256 + tid];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i >> 2][4 * (i & 3) + e] = mine * acc[i >> 2][4 * (i & 3) + e] + theirs * x[e];
+        }
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
     if (!q_ok) return;
-    bf16_t *op = out + ((size_t)r * Hq + h) * DH + 8 * g;
+    bf16_t *op = out + ((size_t)r * (c.n_kv_heads * G.d) + h) * DH + 8 * g;
 #pragma unroll
     for (int mt = 0; mt < DH / 32; ++mt)
 #pragma unroll

@@ -52,7 +52,7 @@ def attn(q=16, stride=256, off=16, out=16, rows=3, most=2, heads=4, dtype=0, ws=
 CACHE_FAULTS = [(dict(k_pages=None), -1), (dict(v_pages=None), -1), (dict(page_table=None), -1), (dict(k_scale=None), -1),
                 (dict(v_scale=None), -1), (dict(cache_dtype=3), -1), (dict(cache_dtype=-1), -1), (dict(batch=0), -1), (dict(n_pages=0), -1),
                 (dict(max_pages=0), -1), (dict(n_kv_heads=0), -1), (dict(head_dim=48), -3), (dict(head_dim=256), -3), (dict(page_size=8), -3),
-                (dict(page_size=48), -3), (dict(page_size=131072), -3), (dict(page_size=0), -3), (dict(page_size=65536, max_pages=16385), -3),
+                (dict(page_size=48), -3), (dict(page_size=131072), -3), (dict(page_size=0), -3), (dict(page_size=65536, max_pages=16385), -3), (dict(n_pages=2 ** 27 + 1), -3),
                 (dict(k_pages=24), -1), (dict(v_pages=17), -1)]
 
 
