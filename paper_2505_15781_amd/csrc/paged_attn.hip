@@ -92,7 +92,7 @@ int launch_split(const PagedCache &c, const Plan &p, const void *q, int64_t q_st
 #undef SPLIT
     DKV_LAUNCH_CHECK();
     if (p.split) {
-        hipLaunchKernelGGL((paged_merge<T, DH>), dim3((unsigned)ceil_div(rows * Hq, 4)), dim3(256), 0, s, row_off, c.batch,
+        hipLaunchKernelGGL((paged_merge<T, DH>), dim3((unsigned)(rows * Hq)), dim3(256), 0, s, row_off, c.batch,
                            (const int2 *)meta, (const float *)records, (T *)out, rows, max_rows, Divisor(Hq), Divisor(Hq / c.n_kv_heads),
                            p.q_groups * NQ * 16);
         DKV_LAUNCH_CHECK();

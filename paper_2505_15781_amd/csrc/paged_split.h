@@ -383,16 +383,17 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
     }
 }
 
-// Joins the slices of one (row, query head): one wavefront each. Rows of sequences with one slice have their result already.
+// Joins the slices of one (row, query head): a workgroup each, so that up to GROUPS records are on their way at once (with a wavefront
+// each, 32 slices were 16 memory latencies). Rows of sequences with one slice have their result already.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void paged_merge(const int *__restrict__ row_off, int batch, const int2 *__restrict__ meta,
                                                    const float *__restrict__ part, T *__restrict__ out, int rows, int max_rows, Divisor Hq,
                                                    Divisor G, int q_rows) {
-    constexpr int REC = DH + 4, CH = DH / 4, LANES = 64 / CH;      // CH lanes hold a record's output, LANES records at a time
-    const int lane = threadIdx.x & 63, pair = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int r = Hq.div(pair), h = Hq.mod(pair);
-    if (r >= rows) return;
-    const int b = sequence_of_row(row_off, batch, r);
+    constexpr int REC = DH + 4, CH = DH / 4, GROUPS = 256 / CH;    // CH lanes hold a record's output
+    __shared__ f32x4 os[GROUPS][CH];
+    __shared__ float2 stats[GROUPS];
+    const int tid = threadIdx.x, lane = tid % CH, group = tid / CH, pair = (int)blockIdx.x, r = Hq.div(pair), h = Hq.mod(pair);
+    const int b = sequence_of_row(row_off, batch, r);              // uniform
     if (b >= batch) return;
     const int in = row_off ? r - row_off[b] : 0;
     const int2 sl = meta[b];                                       // first slice, slices
@@ -400,21 +401,38 @@ __global__ __launch_bounds__(256) void paged_merge(const int *__restrict__ row_o
     const int kvh = G.div(h), mq = in * G.d + G.mod(h), heads = G.div(Hq.d);
     const size_t step = (size_t)heads * q_rows * REC;
     const float *rec = part + (((size_t)sl.x * heads + kvh) * q_rows + mq) * REC;
-    float M = -3.0e38f;
-    for (int s = lane; s < sl.y; s += 64) M = fmaxf(M, rec[s * step]);
-    M = wave_max(M);
-    float l = 0.f;
+    float m = -3.0e38f, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = lane / CH; s < sl.y; s += LANES) {
-        const float *x = rec + s * step, w = __builtin_amdgcn_exp2f(x[0] - M);
-        l += w * x[1];
-        o += w * *reinterpret_cast<const f32x4 *>(x + 4 + 4 * (lane % CH));
+    for (int s = group; s < sl.y; s += 2 * GROUPS) {
+        const bool two = s + GROUPS < sl.y;
+        const float *x = rec + s * step, *y = two ? x + GROUPS * step : x;
+        const float2 xs = *reinterpret_cast<const float2 *>(x), ys = *reinterpret_cast<const float2 *>(y);
+        const f32x4 xo = *reinterpret_cast<const f32x4 *>(x + 4 + 4 * lane), yo = *reinterpret_cast<const f32x4 *>(y + 4 + 4 * lane);
+        const float top = fmaxf(m, fmaxf(xs.x, ys.x)), w = __builtin_amdgcn_exp2f(m - top), wx = __builtin_amdgcn_exp2f(xs.x - top),
+                    wy = two ? __builtin_amdgcn_exp2f(ys.x - top) : 0.f;
+        l = w * l + wx * xs.y;
+        o = w * o + wx * xo;
+        if (two) {
+            l += wy * ys.y;
+            o += wy * yo;
+        }
+        m = top;
     }
+    os[group][lane] = o;
+    if (lane == 0) stats[group] = make_float2(m, l);
+    __syncthreads();
+    if (group) return;
+    float top = m;
+    for (int i = 1; i < GROUPS; ++i) top = fmaxf(top, stats[i].x);
+    const float w = __builtin_amdgcn_exp2f(m - top);
+    l *= w;
+    o *= w;
 #pragma unroll
-    for (int d = CH; d < 64; d <<= 1) {
-        l += __shfl_xor(l, d, 64);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], d, 64);
+    for (int i = 1; i < GROUPS; ++i) {
+        const float2 x = stats[i];
+        const float wi = __builtin_amdgcn_exp2f(x.x - top);
+        l += wi * x.y;
+        o += wi * os[i][lane];
     }
-    if (lane < CH) store_result(out + (size_t)pair * DH + 4 * lane, o, l);
+    store_result(out + (size_t)pair * DH + 4 * lane, o, l);
 }
