@@ -362,9 +362,15 @@ class PagedCache(NamedTuple):
     v_scale: Optional[torch.Tensor] = None
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _place(cache):
     """(current device, its stream) for a cache on a GPU; the marshalling refuses a cache that is elsewhere."""
-    return (-1, 0) if cache[0].get_device() < 0 else (torch.cuda.current_device(), _stream())
+    if cache[0].get_device() < 0:
+        return -1, 0
+    dev = _current_device()
+    return dev, torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(dev)
 
 
 def paged_store(cache, k_new, v_new, positions, row_off=None):

@@ -172,6 +172,12 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
     // the query groups of a (slice, K/V head) read the same keys: consecutive workgroups of one XCD (id mod 8)
     const int slot = (int)(blockIdx.x >> 3), unit = groups.div(slot) * 8 + (int)(blockIdx.x & 7), qg = groups.mod(slot);
     const int at = heads.div(unit), kvh = heads.mod(unit);
+    // Pages of this wavefront's tiles t_begin + wave + NW j: lane i has half i & 1 of tile j0 + i / 2. The entry is read whatever the
+    // length is, so that a plan without slices asks for it before it knows the length.
+    int entry = -1, entry_ahead = -1;
+    auto first_key = [&](int t_begin, int j0) { return (t_begin + wave + NW * (j0 + (lane >> 1))) * PKT + 16 * (lane & 1); };
+    auto load_entry = [&](int b, int key) { return key < c.capacity() ? c.table[(size_t)b * c.max_pages + (key >> c.page_shift)] : -1; };
+    if (!plan.split && at < c.batch) entry = load_entry(at, first_key(0, 0));
     Slices sl;
     if (!find_slice(c, row_off, plan, at, sl)) return;
     const int b = sl.b, r0 = sl.r0, len = sl.keys;
@@ -182,15 +188,12 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
     if (plan.split && tid == 0 && at == sl.first && kvh == 0 && qg == 0) meta[b] = make_int2(sl.first, sl.n);
     const int64_t q_rows = groups.d * (NQ * 16);
 
-    // Pages of this wavefront's tiles t_begin + wave + NW j: lane i has half i & 1 of tile j0 + i / 2. -1: none, or behind the end.
-    auto load_pages = [&](int j0) {
-        const int key = (t_begin + wave + NW * (j0 + (lane >> 1))) * PKT + 16 * (lane & 1);
-        return key < len ? c.page(b, key) : -1;
-    };
+    // the page of such an entry; -1: none, or behind the end
+    auto page_of = [&](int entry, int j0) { return first_key(t_begin, j0) < len && (unsigned)entry < (unsigned)c.n_pages ? entry : -1; };
     constexpr int ROW = DH * (int)sizeof(C), LPR = ROW / 16, RPI = 64 / LPR, N = PKT / RPI;    // lanes per row, rows per load, loads
     u32x4 kreg[N], vreg[N];
     uint32_t scales = 0;                      // e4m3: lane i has the scale of K row i, or of V row i - 32, as a float
-    int pages, pages_ahead, seen0 = 0, seen1 = 0;     // seen: keys of each half that are attended to
+    int pages = -1, seen0 = 0, seen1 = 0;     // seen: keys of each half that are attended to
     auto load_tile = [&](int t, int j) {
         const int id0 = __builtin_amdgcn_readlane(pages, 2 * (j & 31)), id1 = __builtin_amdgcn_readlane(pages, 2 * (j & 31) + 1);
         const int key = t * PKT, slot = key & (c.page_size() - 1), slot1 = (key + 16) & (c.page_size() - 1);
@@ -241,8 +244,8 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
         for (int i = 0; i < DH / 16; ++i) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     int t = t_begin + wave, j = 0;
-    pages = load_pages(0);
-    pages_ahead = load_pages(32);
+    if (plan.split) entry = load_entry(b, first_key(t_begin, 0));
+    entry_ahead = load_entry(b, first_key(t_begin, 32));
     // Query operands. bf16: dims 32 ks + 8 g + [0, 8); fp32: dims 16 ks + 4 g + [0, 4), one of the four for each product
     constexpr int QS = BF ? DH / 32 : DH / 16;
     u32x4 qf[NQ][QS];
@@ -258,6 +261,7 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
             qf[n][ks] = ok ? x : u32x4{0, 0, 0, 0};
         }
     }
+    pages = page_of(entry, 0);
     if (t < t_end) load_tile(t, 0);
     const bf16x8 ones = row_sum_operand(lane);
     const unsigned char *vrow0 = vsm + (4 * g + (qi >> 2)) * SM::V_STRIDE + (qi & 3) * 8;      // bf16: see vt_operand
@@ -270,8 +274,8 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
         if ((j & 31) == 31) {
-            pages = pages_ahead;
-            pages_ahead = load_pages(j + 33);
+            pages = page_of(entry_ahead, j + 1);
+            entry_ahead = load_entry(b, first_key(t_begin, j + 33));
         }
         if (t + NW < t_end) load_tile(t + NW, j + 1);
 

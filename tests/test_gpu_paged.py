@@ -129,6 +129,19 @@ def test_rows_are_held_to_the_bit_and_read_back(act, dtype, dh, heads, page):
         assert np.array_equal(ko.double().cpu().numpy(), wk, equal_nan=True) and np.array_equal(vo.double().cpu().numpy(), wv, equal_nan=True)
 
 
+@pytest.mark.parametrize("out,heads,dh", [("bf16", 33, 128), ("fp32", 20, 64), ("bf16", 65, 32)])
+def test_many_rows_are_read_back(out, heads, dh):
+    """Calls large enough that a lane reads several pieces, the last ones of a row not all there; rows without a page, rows of no sequence."""
+    c = Cache([700, 0, 850], 32, heads, dh, "e4m3", seed=heads, holes=0.1).fill()
+    off = np.array([0, 700, 700, 1550])
+    pos = np.concatenate([np.random.default_rng(1).permutation(700), np.random.default_rng(2).permutation(850), [3, 4, 5]])
+    ko, vo = (torch.full((1553, heads, dh), 7.0, dtype=TORCH[out], device="cuda") for _ in "kv")
+    P.paged_load(c.t, ko, vo, dev(pos), dev(off))
+    wk, wv = (np.full((1553, heads, dh), 7.0) for _ in "kv")
+    O.load(c.o, pos, off, wk, wv)
+    assert np.array_equal(ko.double().cpu().numpy(), wk) and np.array_equal(vo.double().cpu().numpy(), wv)
+
+
 def test_every_bf16_value_is_quantised_as_the_oracle_does():
     """All 65536 bit patterns, 32 to a row: rows of one magnitude (all exponents, zeros, infinities, NaN) and shuffled ones."""
     bits = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
