@@ -30,10 +30,15 @@ struct Plan {
     SlicePlan slices;
 };
 
-// One workgroup of 8 wavefronts holds a compute unit (its LDS): slices make up to that many, a second round costs what the first does
-// (two sequences of 131072 keys: 56 us with 256 workgroups, 67 with 512). A slice has 32 tiles of keys at least, four for each wavefront:
-// 512 keys in one slice take 8.6 us, in two with the launch that joins them 10.8.
-constexpr int kWorkgroups = 256, kLeast = 32;
+// One workgroup of paged_attn_split holds a compute unit (its LDS): slices make up to that many, a second round costs what the first does
+// (two sequences of 131072 keys: 56 us with 256 workgroups, 67 with 512). A slice has 4 tiles of keys at least: what a compute unit
+// reads is bound to some 50 GB/s, so idle units cost more than wavefronts without a tile (28/4 heads, 4 sequences of 2000 keys in
+// bf16: 10.5 us with 4 tiles, 11.4 with 8, 17.2 with 32, 22.3 without slices).
+constexpr int kWorkgroups = 256, kLeast = 4;
+// Key tiles up to which a sequence stays whole: the launch that joins slices costs some 2 us. bf16, 128 dims: 16 tiles 8.6 us whole and 9.0
+// in slices, 24 tiles 11.5 and 9.3; 64 dims: 24 tiles 7.3 and 8.1, 47 tiles 10.8 and 9.0. fp32 (four wavefronts, matrix instructions of an
+// eighth of the rate): 128 dims, 8 tiles 13.3 and 11.8; 64 dims, 8 tiles 7.4 and 8.4, 16 tiles 12.1 and 8.5; 32 dims, 16 tiles 7.5 and 8.2, 24 9.7 and 8.5.
+int whole_tiles(int dtype, int head_dim) { return (dtype == DKV_BF16 ? 2304 : 640) / head_dim; }
 
 Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int dtype, int head_dim) {
     Plan p;
@@ -53,7 +58,7 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
         p.wide = (int)((blocks < bound ? blocks : bound) * c.n_kv_heads);
         p.wide_groups = p.wide <= 320 && key_tiles > 16 ? 2 : 1;
     }
-    p.split = key_tiles > kLeast && c.batch * whole < kWorkgroups;
+    p.split = key_tiles > whole_tiles(dtype, head_dim) && c.batch * whole < kWorkgroups;
     p.slices.split = p.split;
     p.slices.want = Divisor(p.split ? (int)(kWorkgroups / whole) : 1);
     p.slices.least = kLeast;
