@@ -34,13 +34,9 @@ def quantise(x):
     """Rows [..., n] -> (values held, exponents of their scales)."""
     x = np.asarray(x, dtype=np.float64)
     fine = np.isfinite(x)
-    a = np.where(fine, np.abs(x), 0.0).max(-1)
-    e = np.full(a.shape, -110)
-    while True:                                     # the smallest exponent that brings the row to at most 448
-        more = (a > 448.0 * 2.0 ** e) & (e < 120)
-        if not more.any():
-            break
-        e = e + more
+    a = np.where(fine, np.abs(x), 0.0).max(-1, initial=0.0)
+    # the smallest exponent that brings the row to at most 448
+    e = -110 + np.searchsorted(448.0 * 2.0 ** np.arange(-110, 120, dtype=np.float64), a)
     scale = (2.0 ** e)[..., None]
     y = np.where(fine, x, 0.0) / scale
     y = np.where((e == 120)[..., None], np.clip(y, -240.0, 240.0), y)
@@ -75,11 +71,11 @@ def rows_of(cache, off, rows):
 
 
 def store(cache, k_new, v_new, positions, off, dtype):
+    k, v = hold(k_new, dtype), hold(v_new, dtype)
     for r, b in rows_of(cache, off, len(positions)):
         at = place(cache, b, int(positions[r]))
         if at:
-            cache["k"][at[0], :, at[1]] = hold(k_new[r], dtype)
-            cache["v"][at[0], :, at[1]] = hold(v_new[r], dtype)
+            cache["k"][at[0], :, at[1]], cache["v"][at[0], :, at[1]] = k[r], v[r]
 
 
 def load(cache, positions, off, k_out, v_out):

@@ -22,6 +22,18 @@ __device__ __forceinline__ void store_result(bf16_t *p, f32x4 o, float l) {
 #include "paged_split.h"
 #include "paged_wide.h"
 
+// Lets a kernel have its LDS on the current device, once (racing threads only repeat it).
+int allow_lds(const void *kernel, int bytes, std::atomic<uint64_t> &devices) {
+    int dev = -1;
+    DKV_HIP_TRY(hipGetDevice(&dev));
+    const uint64_t bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+    if (!(devices.load(std::memory_order_acquire) & bit)) {
+        DKV_HIP_TRY(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+        devices.fetch_or(bit, std::memory_order_release);
+    }
+    return DKV_OK;
+}
+
 struct Plan {
     int nq, q_groups;       // query tiles of 16 rows per workgroup, groups of them
     int cap;                // slices of the whole batch at most
@@ -53,7 +65,7 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     // rows (256) 18 -> 25; 4096 keys the same way round. Two groups of wavefronts to a workgroup where the blocks are few and the
     // keys many enough to share: 96 blocks of 1024 keys 24.8 -> 22.5 us, 384 blocks 41 -> 47, 128 blocks of 256 keys 11.8 -> 12.6.
     p.wide = p.wide_groups = 0;
-    if (dtype == DKV_BF16 && head_dim == 128 && max_rows * G > 64 && c.batch * whole > kWorkgroups) {
+    if (dtype == DKV_BF16 && head_dim >= 64 && max_rows * G > 64 && c.batch * whole > kWorkgroups) {
         const int64_t blocks = c.batch + (int64_t)ceil_div(rows * G, 128), bound = (int64_t)c.batch * ceil_div(max_rows * G, 128);
         p.wide = (int)((blocks < bound ? blocks : bound) * c.n_kv_heads);
         p.wide_groups = p.wide <= 320 && key_tiles > 16 ? 2 : 1;
@@ -82,12 +94,9 @@ int launch_split(const PagedCache &c, const Plan &p, const void *q, int64_t q_st
     const unsigned grid = (unsigned)(ceil_div(p.cap * c.n_kv_heads, 8) * 8 * p.q_groups);
 #define SPLIT(ONCE)                                                                                                              \
     do {                                                                                                                         \
-        static std::atomic<bool> lds_ok{false};       /* idempotent call: racing threads only repeat it */                      \
-        if (!lds_ok.load(std::memory_order_acquire)) {                                                                           \
-            DKV_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(&paged_attn_split<T, C, DH, NQ, NW, ONCE>),           \
-                                            hipFuncAttributeMaxDynamicSharedMemorySize, smem));                                  \
-            lds_ok.store(true, std::memory_order_release);                                                                       \
-        }                                                                                                                        \
+        static std::atomic<uint64_t> devices{0};                                                                                 \
+        const int rc = allow_lds(reinterpret_cast<const void *>(&paged_attn_split<T, C, DH, NQ, NW, ONCE>), smem, devices);      \
+        if (rc) return rc;                                                                                                       \
         hipLaunchKernelGGL((paged_attn_split<T, C, DH, NQ, NW, ONCE>), dim3(grid), dim3(64 * NW), smem, s, c, p.slices, (const T *)q, \
                            q_stride, row_off, (T *)out, meta, records, rows, max_rows, Divisor(p.q_groups), Divisor(c.n_kv_heads), \
                            Divisor(Hq / c.n_kv_heads), scale_log2e);                                                             \
@@ -105,17 +114,15 @@ int launch_split(const PagedCache &c, const Plan &p, const void *q, int64_t q_st
     return DKV_OK;
 }
 
-template <typename C, int KS>
+template <typename C, int DH, int KS>
 int launch_wide(const PagedCache &c, const Plan &p, const void *q, int64_t q_stride, const int *row_off, void *out, int rows, int max_rows,
                 int Hq, hipStream_t s) {
-    static std::atomic<bool> lds_ok{false};
-    if (!lds_ok.load(std::memory_order_acquire)) {
-        DKV_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(&paged_attn_wide<C, KS>), hipFuncAttributeMaxDynamicSharedMemorySize, KS * WIDE_LDS_BYTES));
-        lds_ok.store(true, std::memory_order_release);
-    }
-    hipLaunchKernelGGL((paged_attn_wide<C, KS>), dim3((unsigned)p.wide), dim3(256 * KS), KS * WIDE_LDS_BYTES, s, c, (const bf16_t *)q, q_stride, row_off,
+    static std::atomic<uint64_t> devices{0};
+    const int rc = allow_lds(reinterpret_cast<const void *>(&paged_attn_wide<C, DH, KS>), KS * kWideLds<DH>, devices);
+    if (rc) return rc;
+    hipLaunchKernelGGL((paged_attn_wide<C, DH, KS>), dim3((unsigned)p.wide), dim3(256 * KS), KS * kWideLds<DH>, s, c, (const bf16_t *)q, q_stride, row_off,
                        (bf16_t *)out, rows, max_rows, Divisor(c.n_kv_heads), Divisor(Hq / c.n_kv_heads), kWorkgroups / c.n_kv_heads,
-                       1.4426950408889634f / sqrtf(128.f));
+                       1.4426950408889634f / sqrtf((float)DH));
     DKV_LAUNCH_CHECK();
     return DKV_OK;
 }
@@ -123,11 +130,16 @@ int launch_wide(const PagedCache &c, const Plan &p, const void *q, int64_t q_str
 template <typename T, typename C, int DH>
 int launch_heads(const PagedCache &c, const Plan &p, const void *q, int64_t q_stride, const int *row_off, void *out, void *part, int rows,
                  int max_rows, int Hq, hipStream_t s) {
-    if constexpr (sizeof(T) == 4) return launch_split<T, C, DH, 1, 4>(c, p, q, q_stride, row_off, out, part, rows, max_rows, Hq, s);
-    else if (DH == 128 && p.wide_groups == 1) return launch_wide<C, 1>(c, p, q, q_stride, row_off, out, rows, max_rows, Hq, s);
-    else if (DH == 128 && p.wide) return launch_wide<C, 2>(c, p, q, q_stride, row_off, out, rows, max_rows, Hq, s);
-    else if (p.nq == 1) return launch_split<T, C, DH, 1, 8>(c, p, q, q_stride, row_off, out, part, rows, max_rows, Hq, s);
-    else return launch_split<T, C, DH, 2, 8>(c, p, q, q_stride, row_off, out, part, rows, max_rows, Hq, s);
+    if constexpr (sizeof(T) == 4) {
+        return launch_split<T, C, DH, 1, 4>(c, p, q, q_stride, row_off, out, part, rows, max_rows, Hq, s);
+    } else {
+        if constexpr (DH >= 64) {
+            if (p.wide_groups == 1) return launch_wide<C, DH, 1>(c, p, q, q_stride, row_off, out, rows, max_rows, Hq, s);
+            if (p.wide_groups == 2) return launch_wide<C, DH, 2>(c, p, q, q_stride, row_off, out, rows, max_rows, Hq, s);
+        }
+        return p.nq == 1 ? launch_split<T, C, DH, 1, 8>(c, p, q, q_stride, row_off, out, part, rows, max_rows, Hq, s)
+                         : launch_split<T, C, DH, 2, 8>(c, p, q, q_stride, row_off, out, part, rows, max_rows, Hq, s);
+    }
 }
 
 template <typename T, typename C, typename... A> int launch_attn(int head_dim, A... a) {
@@ -182,7 +194,8 @@ extern "C" int dkv_paged_attn(const dkv_paged_cache *cache, const void *q, int64
     }
     if (need && reinterpret_cast<uintptr_t>(workspace) % 16) { dkv_set_error("workspace must be 16-byte aligned"); return DKV_E_INVALID_ARG; }
     hipStream_t s = static_cast<hipStream_t>(stream);
-    auto launch = [&](auto f) { return f(dh, c, p, q, q_stride, row_off, out, workspace, rows, max_rows_per_seq, n_q_heads, s); };
+    const int max_rows = max_rows_per_seq < rows ? max_rows_per_seq : rows;
+    auto launch = [&](auto f) { return f(dh, c, p, q, q_stride, row_off, out, workspace, rows, max_rows, n_q_heads, s); };
     if (dtype == DKV_BF16)
         return cache->dtype == DKV_BF16 ? launch([](auto... a) { return launch_attn<bf16_t, bf16_t>(a...); })
                                         : launch([](auto... a) { return launch_attn<bf16_t, e4m3_t>(a...); });

@@ -401,7 +401,7 @@ __global__ __launch_bounds__(256) void paged_merge(const int *__restrict__ row_o
     if (b >= batch) return;
     const int in = row_off ? r - row_off[b] : 0;
     const int2 sl = meta[b];                                       // first slice, slices
-    if (in >= max_rows || sl.y <= 1) return;
+    if ((unsigned)in >= (unsigned)max_rows || sl.y <= 1) return;
     const int kvh = G.div(h), mq = in * G.d + G.mod(h), heads = G.div(Hq.d);
     const size_t step = (size_t)heads * q_rows * REC;
     const float *rec = part + (((size_t)sl.x * heads + kvh) * q_rows + mq) * REC;

@@ -1,4 +1,4 @@
-// Attention over a paged cache for blocks of 128 query rows: 32 query rows per wavefront, 32x32x16 MFMA, head_dim 128.
+// Attention over a paged cache for blocks of 128 query rows: 32 query rows per wavefront, 32x32x16 MFMA, head_dim 64 or 128.
 // Included by paged_attn.hip.
 //
 // Work item = (sequence, K/V head, block of 128 query rows). The loop is that of attn_wide.h: keys in tiles of 64 through two LDS
@@ -13,10 +13,15 @@
 typedef __attribute__((address_space(3))) void *lds_ptr_t;
 template <int V> struct StageC { static constexpr int value = V; };
 constexpr float kLag = 8.f;                          // log2 of the largest probability
-constexpr int WIDE_LDS_BYTES = 4 * 64 * 256;         // K0 K1 V0 V1, rows of 256 bytes
+template <int DH> constexpr int kWideLds = 4 * 64 * DH * 2;       // K0 K1 V0 V1
 
-// Place of the 16-byte chunk c of row r: c ^ wide_swizzle(r) (see attn_wide.h).
-__device__ __forceinline__ int wide_swizzle(int row) { return ((row & 3) << 2) | ((row >> 2) & 3); }
+// Place of the 16-byte chunk c of row r: c ^ wide_swizzle(r). 16 consecutive rows put a chunk (score operands) into 16 different places of
+// 256 bytes, and the 4 chunks of 8 rows that a transposing read takes are spread evenly over them. Rows of 128 bytes lie two to
+// 256 bytes; with either length the value of row r + 8 is that of row r with bit 1 turned, of row r + 16 the same.
+template <int DH> __device__ __forceinline__ int wide_swizzle(int row) {
+    if (DH == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+    return ((row >> 1 & 1) << 2) | ((row >> 2) & 3);
+}
 
 __device__ __align__(256) const u32x4 zero_row[16] = {};
 
@@ -78,18 +83,18 @@ struct WideTile {
     int pages;
 };
 
-template <typename C, int KS>
-__global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_attn_wide(
+template <typename C, int DH, int KS>
+__global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, DH == 128 ? 2 : 4))) void paged_attn_wide(
     PagedCache c, const bf16_t *__restrict__ Q, int64_t q_stride, const int *__restrict__ row_off, bf16_t *__restrict__ out, int rows,
     int max_rows, Divisor heads, Divisor G, int units, float scale_log2e) {
-    constexpr int NW = 4, DH = 128, ROW = DH * 2, KT2 = 64, TILE = KT2 * ROW;     // bytes of an LDS row, of a K or V tile
+    constexpr int NW = 4, ROW = DH * 2, KT2 = 64, TILE = KT2 * ROW;     // bytes of an LDS row, of a K or V tile
     constexpr bool E4M3 = sizeof(C) == 1;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_all[];
 
     // KS groups of four wavefronts, in LDS stages of their own
     const int tid = threadIdx.x & 255, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int group_id = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 8);
-    unsigned char *smem_raw = smem_all + group_id * WIDE_LDS_BYTES;
+    unsigned char *smem_raw = smem_all + group_id * kWideLds<DH>;
     const int qi = lane & 31, g = lane >> 5, l16 = lane & 15, l4 = lane >> 4;
     const uint32_t lds_base = (uint32_t)(size_t)(lds_ptr_t)smem_raw;
     WideItem item;
@@ -134,39 +139,45 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
     auto there = [&](int step, int tile_pages, int i) { return tile_pages >> i & 1 ? L - ((step * parts + part) * KT2 + 16 * i) : 0; };
     auto whole = [&](int step, int tile_pages) { return tile_pages == 15 && (step * parts + part + 1) * KT2 <= L; };
 
-    // bf16. Load i of a wavefront fills rows 16 i + 4 wave + [0, 4) of a tile; lane -> row lane / 16, place lane % 16.
-    const uint32_t chunk = (l16 ^ wide_swizzle(4 * wave + l4)) << 4;
+    // bf16. Load i of a wavefront fills rows RPL (4 i + wave) + [0, RPL) of a tile; lane -> row lane / LPR, place lane % LPR.
+    constexpr int LPR = ROW / 16, RPL = 64 / LPR, LOADS = KT2 / (RPL * NW);
+    const int d_row = (RPL * wave + lane / LPR) % 16;                  // row within its group of 16, the same for all loads
+    const uint32_t chunk = (lane % LPR ^ wide_swizzle<DH>(d_row)) << 4;
     auto fill = [&](const unsigned char *base, const WideTile &x, int t, uint32_t dst) {
-        if (whole(t, x.pages)) {
+        const bool all = whole(t, x.pages);                           // uniform
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                dma16_at(l4 * ROW + chunk, base + (size_t)(x.row[i] + 4 * wave) * ROW, lds_base + dst + (16 * i + 4 * wave) * ROW);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const unsigned char *p = base + (size_t)(x.row[i] + 4 * wave + l4) * ROW;
-                dma16((4 * wave + l4 < there(t, x.pages, i) ? p : reinterpret_cast<const unsigned char *>(zero_row)) + chunk,
-                      lds_base + dst + (16 * i + 4 * wave) * ROW);
+        for (int i = 0; i < LOADS; ++i) {
+            const int first = RPL * (NW * i + wave), gr = RPL * NW * i / 16 + RPL * wave / 16;      // first row, its group: uniform
+            const uint32_t row = (RPL * NW >= 32 ? (wave >> 1 ? x.row[RPL * NW * i / 16 + 1] : x.row[RPL * NW * i / 16]) : x.row[i]) + first % 16;
+            const uint32_t lds = lds_base + dst + first * ROW;
+            if (all) {
+                dma16_at(lane / LPR * ROW + chunk, base + (size_t)row * ROW, lds);
+            } else {
+                const unsigned char *p = base + (size_t)(row + lane / LPR) * ROW;
+                dma16((d_row < there(t, x.pages, gr) ? p : reinterpret_cast<const unsigned char *>(zero_row)) + chunk, lds);
             }
         }
     };
-    // e4m3. Load i of a wavefront has rows 32 i + 8 wave + [0, 8); lane -> row lane / 8, elements 16 (lane % 8) + [0, 16).
-    const int r16 = 8 * (wave & 1) + (lane >> 3);                     // row within the group 2 i + wave / 2
-    u32x4 kreg[2], vreg[2];
-    uint32_t k_scale[2], v_scale[2];
-    auto fetch = [&](u32x4 (&reg)[2], uint32_t (&scale)[2], const unsigned char *base, const uint8_t *scales, const WideTile &x) {
+    // e4m3. Load i of a wavefront has rows RPF (4 i + wave) + [0, RPF); lane -> row lane / LPF, elements 16 (lane % LPF) + [0, 16).
+    constexpr int LPF = DH / 16, RPF = 64 / LPF, FETCHES = KT2 / (RPF * NW);
+    const int f_row = (RPF * wave + lane / LPF) % 16;
+    auto f_group = [&](const WideTile &x, int i) { return RPF == 16 ? (wave & 2 ? (wave & 1 ? x.row[3] : x.row[2]) : (wave & 1 ? x.row[1] : x.row[0]))
+                                                                    : (wave >> 1 ? x.row[2 * i + 1] : x.row[2 * i]); };
+    u32x4 kreg[FETCHES], vreg[FETCHES];
+    uint32_t k_scale[FETCHES], v_scale[FETCHES];
+    auto fetch = [&](u32x4 (&reg)[FETCHES], uint32_t (&scale)[FETCHES], const unsigned char *base, const uint8_t *scales, const WideTile &x) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const size_t row = wave >> 1 ? x.row[2 * i + 1] : x.row[2 * i];      // uniform
-            reg[i] = *reinterpret_cast<const u32x4 *>(base + row * DH + (uint32_t)(r16 * DH + 16 * (lane & 7)));
-            scale[i] = (scales + row)[(uint32_t)r16];
+        for (int i = 0; i < FETCHES; ++i) {
+            const size_t row = f_group(x, i);                         // uniform
+            reg[i] = *reinterpret_cast<const u32x4 *>(base + row * DH + (uint32_t)(f_row * DH + 16 * (lane % LPF)));
+            scale[i] = (scales + row)[(uint32_t)f_row];
         }
     };
-    auto convert = [&](const u32x4 (&reg)[2], const uint32_t (&scale)[2], int tile_pages, int t, uint32_t dst) {
+    auto convert = [&](const u32x4 (&reg)[FETCHES], const uint32_t (&scale)[FETCHES], int tile_pages, int t, uint32_t dst) {
         const bool all = whole(t, tile_pages);                        // uniform
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int row = 32 * i + 8 * wave + (lane >> 3), sw = wide_swizzle(row);
+        for (int i = 0; i < FETCHES; ++i) {
+            const int row = RPF * (NW * i + wave) + lane / LPF, sw = wide_swizzle<DH>(row);
             const float s = __uint_as_float(scale[i] << 23);
             u32x4 y[2];
 #pragma unroll
@@ -174,10 +185,10 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
                 y[e >> 1][2 * (e & 1)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(reg[i][e], s, false));
                 y[e >> 1][2 * (e & 1) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(reg[i][e], s, true));
             }
-            if (!all && r16 >= there(t, tile_pages, 2 * i + (wave >> 1))) y[0] = y[1] = u32x4{0, 0, 0, 0};
+            if (!all && f_row >= there(t, tile_pages, RPF == 16 ? wave : 2 * i + (wave >> 1))) y[0] = y[1] = u32x4{0, 0, 0, 0};
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-                *reinterpret_cast<u32x4 *>(smem_raw + dst + row * ROW + (((2 * (lane & 7) + e) ^ sw) << 4)) = y[e];
+                *reinterpret_cast<u32x4 *>(smem_raw + dst + row * ROW + (((2 * (lane % LPF) + e) ^ sw) << 4)) = y[e];
         }
     };
     // pages of the tiles t, t + 1, t + 2 (of the last ones: of some tile), and where tile t + 1 (bf16) or t + 2 (e4m3) is
@@ -185,8 +196,8 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
     WideTile x = find(0), ahead = x;
     pages_0 = pages_1 = pages_2 = x.pages;
     if constexpr (E4M3) {                        // all loads at once: K0 V0 K1, and V1 K2 for the loop
-        u32x4 k0[2], v0[2], k1[2];
-        uint32_t k0_scale[2], v0_scale[2], k1_scale[2];
+        u32x4 k0[FETCHES], v0[FETCHES], k1[FETCHES];
+        uint32_t k0_scale[FETCHES], v0_scale[FETCHES], k1_scale[FETCHES];
         fetch(k0, k0_scale, c.k, c.ks, x);
         fetch(v0, v0_scale, c.v, c.vs, x);
         if (n_tiles > 1) x = find(1);
@@ -211,10 +222,10 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
 
     // score operands: row lane & 31, chunk 2 ks + g
     const unsigned char *krow = smem_raw + qi * ROW;
-    const int kx = (g ^ wide_swizzle(qi)) << 4;
+    const int kx = (g ^ wide_swizzle<DH>(qi)) << 4;
     // output operand: see vt_operand; block lane / 16 = (g, dims + 16 half), key 4 g + j / 4 (+ 8), dims 4 (j % 4)
     const unsigned char *vrow = smem_raw + 2 * TILE + (4 * g + (l16 >> 2)) * ROW + ((l16 & 1) << 3);
-    const int vx = ((2 * (l4 & 1) + ((l16 & 3) >> 1)) ^ (((l16 >> 2) << 2) | g)) << 4;       // keys + 8: swizzle ^ 2
+    const int vx = ((2 * (l4 & 1) + ((l16 & 3) >> 1)) ^ wide_swizzle<DH>(4 * g + (l16 >> 2))) << 4;
 
     // lowest finite start: scores of -inf then give probabilities of zero, also where a whole half tile is masked
     float m_run = -3.0e38f, alpha = 1.f;
@@ -246,30 +257,31 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
         for (int v = 0; v < 16; ++v) sn[v] = 0.f;
         f32x8 p[2];
+        constexpr int MT = DH / 32, N = DH / 16, PER = 16 / N;        // products of the scores, and of the output; exponentials next to each two
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < N; ++i) {
             sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(i, kstage, khalf), qf[i], sn, 0, 0, 0);
-            acc[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(i & 3, i >> 2, vstage, vhalf), pv[i >> 2], acc[i & 3], 0, 0, 0);
+            acc[i % MT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(i % MT, i / MT, vstage, vhalf), pv[i / MT], acc[i % MT], 0, 0, 0);
 #pragma unroll
-            for (int e = 2 * i; e < 2 * i + 2; ++e)
+            for (int e = PER * i; e < PER * (i + 1); ++e) {
                 p[e >> 3][e & 7] = __builtin_amdgcn_exp2f(fmaf(so[e], scale_log2e, -m_run));
-            l[0] += p[i >> 2][2 * (i & 3)];
-            l[1] += p[i >> 2][2 * (i & 3) + 1];
+                l[e & 1] += p[e >> 3][e & 7];
+            }
         }
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) pn[ks] = __builtin_convertvector(p[ks], bf16x8);
         asm volatile("" : "+v"(pn[0]), "+v"(pn[1]));        // here, not behind the branches of maximum()
         __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < N; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
-            __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 3 * PER / 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x400, PER / 2, 0);
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-            __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
-            __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 3 * PER / 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x400, PER / 2, 0);
         }
     };
     // Brings the output up to the reference m_run of the exponentials.
@@ -320,7 +332,7 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
     for (int v = 0; v < 16; ++v) stA[v] = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) stA = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(i, 0, 0), qf[i], stA, 0, 0, 0);
+    for (int i = 0; i < DH / 16; ++i) stA = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(i, 0, 0), qf[i], stA, 0, 0, 0);
     maximum(stA, 0, 0, pages_0);
     // Tile t, in stage S; the scores of its first half are formed.
     auto step = [&](int t, auto stage) {
@@ -361,19 +373,19 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
     const int last = (n_tiles - 1) & 1;
     rescale();
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        acc[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(i & 3, i >> 2, last, 1), pB[i >> 2], acc[i & 3], 0, 0, 0);
+    for (int i = 0; i < DH / 16; ++i)
+        acc[i % (DH / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(i % (DH / 32), i / (DH / 32), last, 1), pB[i / (DH / 32)], acc[i % (DH / 32)], 0, 0, 0);
 
     float u, w;
     swap_rows32(l[0] + l[1], u, w);
     float sum = u + w;
     if (KS == 2 && parts == 2) {                 // the second group's state goes through LDS to the same lanes of the first
-        f32x4 *parked = reinterpret_cast<f32x4 *>(smem_all + WIDE_LDS_BYTES);
+        f32x4 *parked = reinterpret_cast<f32x4 *>(smem_all + kWideLds<DH>);
         float2 *stats = reinterpret_cast<float2 *>(smem_all);
         __syncthreads();
         if (part == 1) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) parked[i * 256 + tid] = f32x4{acc[i >> 2][4 * (i & 3)], acc[i >> 2][4 * (i & 3) + 1], acc[i >> 2][4 * (i & 3) + 2], acc[i >> 2][4 * (i & 3) + 3]};
+            for (int i = 0; i < DH / 8; ++i) parked[i * 256 + tid] = f32x4{acc[i >> 2][4 * (i & 3)], acc[i >> 2][4 * (i & 3) + 1], acc[i >> 2][4 * (i & 3) + 2], acc[i >> 2][4 * (i & 3) + 3]};
             stats[tid] = make_float2(m_run, sum);
         }
         __syncthreads();
@@ -382,7 +394,7 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
         const float m = fmaxf(m_run, other.x), mine = __builtin_amdgcn_exp2f(m_run - m), theirs = __builtin_amdgcn_exp2f(other.x - m);
         sum = mine * sum + theirs * other.y;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < DH / 8; ++i) {
             const f32x4 x = parked[i * 256 + tid];
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[i >> 2][4 * (i & 3) + e] = mine * acc[i >> 2][4 * (i & 3) + e] + theirs * x[e];

@@ -182,7 +182,8 @@ ATTN = [  # lens, rows, page, kv heads, group, dh
     ([63, 64, 65, 127, 129], [3, 0, 17, 1, 16], 32, 2, 1, 64), ([1300, 7], [1, 5], 64, 2, 7, 128), ([5000], [2], 128, 1, 7, 128),
     ([333, 1000, 16], [40, 70, 16], 16, 3, 1, 128), ([769, 100, 257], [65, 129, 33], 32, 2, 7, 128), ([300, 513], [130, 257], 256, 2, 1, 64),
     ([200, 40], [17, 23], 16, 4, 1, 32), ([2100], [1], 16, 1, 16, 32), ([640, 448], [300, 64], 64, 8, 4, 128), ([1, 2, 3], [130, 1, 140], 16, 26, 1, 128),
-    ([1333, 64, 333, 0], [200, 100, 400, 70], 16, 8, 4, 128), ([63, 129, 1024], [300, 5, 900], 128, 32, 1, 128)]
+    ([1333, 64, 333, 0], [200, 100, 400, 70], 16, 8, 4, 128), ([63, 129, 1024], [300, 5, 900], 128, 32, 1, 128),
+    ([300, 1050, 40], [130, 257, 1], 256, 16, 2, 64), ([100, 190, 80, 70], [300, 300, 200, 100], 16, 32, 1, 64)]
 
 
 @pytest.mark.parametrize("types", ["bf16 bf16", "bf16 e4m3", "fp32 fp32", "fp32 e4m3"])
@@ -228,6 +229,98 @@ def test_attention_to_large_scores_infinities_and_nan(types, n, most):
     O.store(c.o, low.double().cpu().numpy(), one.double().cpu().numpy(), np.arange(40), np.array([0, 0, 0, 40]), dtype)
     out = check_attn(c, q, [n, 1, 1])
     assert (out[n + 1] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("heads,group,dh,most,longest", [(1, 2, 64, 1, 1500), (1, 4, 128, 3, 2100), (4, 4, 128, 40, 300), (2, 2, 64, 40, 700), (2, 2, 128, 45, 900)])
+def test_attention_of_more_sequences_than_a_wavefront_has_lanes(heads, group, dh, most, longest, dtype):
+    """70 sequences, some without keys and some without rows, whose keys are cut into slices, or whose rows make blocks of 128."""
+    g = np.random.default_rng(heads * dh + most)
+    lens = (longest ** g.random(70)).astype(int) - 1
+    lens[5], lens[69] = longest, longest - 1
+    counts = g.integers(0, most + 1, 70)
+    counts[5] = counts[68] = most
+    c = Cache([int(n) for n in lens], 32, heads, dh, dtype, seed=most, holes=0.05).fill()
+    check_attn(c, rows(g, (int(counts.sum()) + 1, heads * group, dh), "bf16"), counts, most=most + 1)
+
+
+@pytest.mark.parametrize("act", ["bf16", "fp32"])
+@pytest.mark.parametrize("dh,n", [(32, 1), (64, 1), (128, 1), (64, 300), (128, 300)])
+def test_every_code_and_scale_comes_out_of_the_attention_as_it_is_held(act, dh, n):
+    """One key in each sequence, whose probability is 1: the result is its V row, bit for bit. All 256 codes with the scales of -110
+    to 120, with one row a sequence and (bf16, 64 and 128 dims) with enough for the kernel of 128-row blocks."""
+    if act == "fp32" and n > 1:
+        pytest.skip("one kernel")
+    heads, lens = 256 // dh, [1] * (231 if n == 1 else 6)
+    c = Cache(lens, 16, heads, dh, "e4m3", wider=0)
+    codes = torch.arange(256, dtype=torch.uint8, device="cuda").view(heads, dh)
+    first = torch.from_numpy(c.o["table"][:, 0]).cuda()
+    scale = (torch.arange(len(lens), device="cuda") * (230 // (len(lens) - 1)) + 17).to(torch.uint8)
+    c.t.v_pages.view(torch.uint8)[first, :, 0] = codes
+    c.t.v_scale.view(torch.uint8)[first, :, 0] = scale[:, None].expand(-1, heads)
+    c.t.k_pages.view(torch.uint8)[first, :, 0] = 0
+    c.t.k_scale.view(torch.uint8)[first, :, 0] = 127
+    q = rows(np.random.default_rng(1), (n * len(lens), 8 * heads if n > 1 else heads, dh), act)
+    out = torch.zeros_like(q)
+    P.paged_attn(c.t, q, dev(np.arange(len(lens) + 1) * n), out, n, workspace(c, q, n))
+    held = O.e4m3_values().reshape(1, heads, 1, dh) * 2.0 ** (scale.double().cpu().numpy() - 127.0)[:, None, None, None]
+    want = np.broadcast_to(np.repeat(held, n, axis=0), (len(q), heads, q.shape[1] // heads, dh)).reshape(q.shape)
+    got = out.double().cpu().numpy()
+    finite = np.abs(want) <= 3.4e38                       # 256 * 2^120 and more is not held by a store
+    assert np.array_equal(got[finite | np.isnan(want)], want[finite | np.isnan(want)], equal_nan=True)
+
+
+def test_fp32_rows_of_all_magnitudes_are_quantised_as_the_oracle_does():
+    """Random bit patterns: denormals, infinities, NaN among them; rows of one exponent, where ties and the border between two scales lie."""
+    g = np.random.default_rng(12)
+    bits = g.integers(0, 2 ** 32, (200, 64), dtype=np.uint64).astype(np.uint32)
+    near = ((g.integers(1, 255, (200, 1)).astype(np.uint32) << 23) | (g.integers(0, 16, (200, 64)).astype(np.uint32) << 19)) + g.integers(0, 2, (200, 64)).astype(np.uint32)
+    x = torch.from_numpy(np.concatenate([bits, near]).view(np.float32)).cuda().view(2, 200, 64)
+    c = Cache([2], 16, 200, 64, "e4m3")
+    P.paged_store(c.t, x, x, dev([0, 1]), dev([0, 2]))
+    y = x.double().cpu().numpy()
+    O.store(c.o, y, y, np.array([0, 1]), np.array([0, 2]), "e4m3")
+    assert c.same()
+
+
+@pytest.mark.parametrize("act", ["bf16", "fp32"])
+def test_rows_that_start_at_any_element(act):
+    """Rows and results in the middle of other tensors, at odd elements: every call, few rows and many."""
+    for n, dh in ((2, 32), (3, 128), (300, 128)):
+        c = Cache([n + 40, 30], 16, 2, dh, "e4m3", seed=n).fill(act)
+        g = np.random.default_rng(n)
+        inside = lambda *shape: rows(g, (int(np.prod(shape)) + 8,), act)[3:3 + int(np.prod(shape))].view(shape)
+        k, v, q, out = inside(n, 2, dh), inside(n, 2, dh), inside(n + 1, 16, dh), inside(n + 1, 16, dh).fill_(7.0)
+        P.paged_store(c.t, k, v, dev(np.arange(n)), dev([0, n, n]))
+        O.store(c.o, k.double().cpu().numpy(), v.double().cpu().numpy(), np.arange(n), np.array([0, n, n]), "e4m3")
+        assert c.same()
+        ko, vo = inside(n, 2, dh), inside(n, 2, dh)
+        P.paged_load(c.t, ko, vo, dev(np.arange(n)), dev([0, n, n]))
+        wk, wv = np.zeros(k.shape), np.zeros(k.shape)
+        O.load(c.o, np.arange(n), np.array([0, n, n]), wk, wv)
+        assert np.array_equal(ko.double().cpu().numpy(), wk) and np.array_equal(vo.double().cpu().numpy(), wv)
+        check_attn(c, q, [n, 1], out=out)
+
+
+def test_two_calls_at_once_on_two_streams():
+    """Long enough to overlap, each with a workspace of its own: the same bits as one after the other."""
+    c = Cache([9000, 7000], 64, 4, 128, "bf16", seed=21).fill()
+    qs = [rows(np.random.default_rng(i), (2, 28, 128), "bf16") for i in range(2)]
+    ws, want, got = [], [], []
+    for q in qs:
+        ws.append(workspace(c, q, 1))
+        want.append(torch.zeros_like(q))
+        got.append(torch.zeros_like(q))
+        P.paged_attn(c.t, q, None, want[-1], 1, ws[-1])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in qs]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                P.paged_attn(c.t, qs[i], None, got[i], 1, ws[i])
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16))
 
 
 def test_lengths_out_of_range_are_those_of_the_table():

@@ -74,6 +74,11 @@ def test_refused_arguments():
     assert attn(q=None) == attn(out=None) == attn(seq_len=None) == attn(rows=-1) == attn(dtype=2) == -1
     assert attn(heads=3) == attn(heads=0) == attn(most=-1) == attn(rows=5) == attn(off=None) == attn(stride=255) == -1
     assert attn(rows=0, q=None, out=None, ws=None, nbytes=0) == 0
+    for ws, nbytes, code in ((None, 1 << 40, -4), (16, 16, -4), (24, 1 << 40, -1)):       # 2048 keys: joined from slices, in the workspace
+        assert attn(max_pages=128, ws=ws, nbytes=nbytes) == code
+    assert attn(max_pages=1 << 20, page_size=1024, batch=64) == -3                        # 2^36 positions
+    assert B.lib.dkv_paged_attn_workspace_bytes(C.byref(desc(max_pages=128)), 4, 3, 2, 0) > 256
+    assert B.lib.dkv_paged_attn_workspace_bytes(C.byref(desc(max_pages=128)), 4, 0, 0, 0) > 0
     assert B.lib.dkv_paged_store(None, 16, 16, 128, 16, 16, 3, 0, None) == -1
     assert attn(dtype=B.BF16, cache_dtype=B.FP32) == attn(dtype=B.FP32, cache_dtype=B.BF16) == -3
 
