@@ -95,9 +95,6 @@ lib.dkv_paged_load.argtypes = [C.POINTER(PagedCacheDesc), c_vp, c_vp, c_vp, c_vp
 lib.dkv_paged_attn_workspace_bytes.restype = c_sz
 lib.dkv_paged_attn_workspace_bytes.argtypes = [C.POINTER(PagedCacheDesc), c_i32, c_i32, c_i32, c_i32]
 lib.dkv_paged_attn.argtypes = [C.POINTER(PagedCacheDesc), c_vp, C.c_int64, c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_vp, c_sz, c_vp]
-_marshal.bind_paged(*(C.cast(f, c_vp).value for f in (lib.dkv_paged_store, lib.dkv_paged_load, lib.dkv_paged_attn_workspace_bytes,
-                                                      lib.dkv_paged_attn)),
-                    torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.int32)
 lib.dkv_peak_copy.argtypes = [c_vp, c_vp, c_sz, c_vp]
 lib.dkv_peak_read.argtypes = [c_vp, c_vp, c_sz, c_vp]
 lib.dkv_peak_mfma.argtypes = [c_vp, c_i32, C.POINTER(C.c_double), c_vp]
@@ -346,6 +343,18 @@ def concat_reorder(k_cached, v_cached, k_new, v_new, take, dtype):
     return k_out, v_out
 
 
+class _Streams:
+    """Current device and stream, for builds of torch without the two functions of these names."""
+    _cuda_getDevice = staticmethod(lambda: torch.cuda.current_device())
+    _cuda_getCurrentRawStream = staticmethod(lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+_marshal.bind_paged(*(C.cast(f, c_vp).value for f in (lib.dkv_paged_store, lib.dkv_paged_load, lib.dkv_paged_attn_workspace_bytes,
+                                                      lib.dkv_paged_attn)),
+                    torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.int32,
+                    torch._C if _raw_stream is not None and hasattr(torch._C, "_cuda_getDevice") else _Streams)
+
+
 class PagedCache(NamedTuple):
     """The tensors of a paged K/V cache, all of the caller's (see dkv_paged_cache in dkv.h).
 
@@ -362,27 +371,16 @@ class PagedCache(NamedTuple):
     v_scale: Optional[torch.Tensor] = None
 
 
-_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-
-
-def _place(cache):
-    """(current device, its stream) for a cache on a GPU; the marshalling refuses a cache that is elsewhere."""
-    if cache[0].get_device() < 0:
-        return -1, 0
-    dev = _current_device()
-    return dev, torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(dev)
-
-
 def paged_store(cache, k_new, v_new, positions, row_off=None):
     """Write rows of new K and V to their positions, quantised where the cache holds e4m3: row r of sequence b, i.e.
     row_off[b] <= r < row_off[b + 1], goes to position positions[r]; without row_off, row r belongs to sequence r.
     k_new, v_new [rows, n_kv_heads, head_dim], bfloat16 or float32; the rows may be parts of longer ones."""
-    _check(_marshal.paged_store(cache, k_new, v_new, positions, row_off, *_place(cache)))
+    _check(_marshal.paged_store(cache, k_new, v_new, positions, row_off))
 
 
 def paged_load(cache, k_out, v_out, positions, row_off=None):
     """The rows at these positions, as paged_store takes them; zeros where there is no page."""
-    _check(_marshal.paged_load(cache, k_out, v_out, positions, row_off, *_place(cache)))
+    _check(_marshal.paged_load(cache, k_out, v_out, positions, row_off))
 
 
 def paged_attn_workspace_bytes(cache, n_q_heads, rows, max_rows_per_seq, dtype=BF16):
@@ -393,7 +391,7 @@ def paged_attn_workspace_bytes(cache, n_q_heads, rows, max_rows_per_seq, dtype=B
 def paged_attn(cache, q, row_off, out, max_rows_per_seq, workspace):
     """Attention of the rows of q [rows, n_q_heads, head_dim] over all positions of their sequences (below seq_len, on a
     page) into `out`; row_off as in paged_store (None: one row per sequence)."""
-    _check(_marshal.paged_attn(cache, q, row_off, out, max_rows_per_seq, workspace, *_place(cache)))
+    _check(_marshal.paged_attn(cache, q, row_off, out, max_rows_per_seq, workspace))
 
 
 GEMM_OPT_STAGGER, GEMM_OPT_XCD_GROUP, GEMM_OPT_SWIGLU, GEMM_OPT_STREAM_W = 1, 2, 4, 8

@@ -167,7 +167,8 @@ static paged_bytes_fn f_paged_bytes;
 static paged_attn_fn f_paged_attn;
 enum { T_BF16 = DKV_BF16, T_FP32 = DKV_FP32, T_E4M3 = DKV_E4M3, T_E8M0, T_I32, T_COUNT };
 static PyObject *dtypes[T_COUNT];
-static PyObject *s_dtype, *s_is_contiguous, *s_get_device, *s_stride;
+static PyObject *s_dtype, *s_is_contiguous, *s_get_device, *s_stride, *s_current, *s_stream;
+static PyObject *place_of;        /* has _cuda_getDevice() and _cuda_getCurrentRawStream(device) */
 
 typedef struct {
     void *ptr;
@@ -274,11 +275,20 @@ static int look_offsets(PyObject *t, int32_t batch, int32_t rows, int device, co
     return 0;
 }
 
-static int look_place(PyObject *current, PyObject *stream, int device, void **s) {
+/* the current stream of the cache's device, which has to be the current one: asked of torch only where there is a GPU */
+static int look_place(int device, void **s) {
     if (device < 0) return refuse("k_pages", "the cache is not on a GPU");
-    if (PyLong_AsLong(current) != device) return PyErr_Occurred() ? -1 : refuse("k_pages", "the cache is not on the current device");
-    *s = PyLong_AsVoidPtr(stream);
-    return PyErr_Occurred() ? -1 : 0;
+    PyObject *at = PyObject_CallMethodObjArgs(place_of, s_current, NULL);
+    if (!at) return -1;
+    const long current = PyLong_AsLong(at);
+    if (current == device) {
+        PyObject *stream = PyObject_CallMethodObjArgs(place_of, s_stream, at, NULL);
+        if (stream) *s = PyLong_AsVoidPtr(stream);
+        Py_XDECREF(stream);
+    }
+    Py_DECREF(at);
+    if (PyErr_Occurred()) return -1;
+    return current == device ? 0 : refuse("k_pages", "the cache is not on the current device");
 }
 
 static int ready(Py_ssize_t n, Py_ssize_t want) {
@@ -288,9 +298,9 @@ static int ready(Py_ssize_t n, Py_ssize_t want) {
     return 0;
 }
 
-/* (cache, k, v, positions, row_off, current device, stream): the status code of the library call */
+/* (cache, k, v, positions, row_off): the status code of the library call */
 static PyObject *rows_call(PyObject *const *a, Py_ssize_t n, int storing) {
-    if (!ready(n, 7)) return NULL;
+    if (!ready(n, 5)) return NULL;
     dkv_paged_cache c;
     tensor_info k, v, pos;
     int64_t stride, v_stride;
@@ -310,7 +320,7 @@ static PyObject *rows_call(PyObject *const *a, Py_ssize_t n, int storing) {
         return NULL;
     }
     if (look_whole(a[3], "positions", T_I32, 1, &k.dims[0], device, &pos) || look_offsets(a[4], c.batch, k.dims[0], device, &off) ||
-        look_place(a[5], a[6], device, &stream))
+        look_place(device, &stream))
         return NULL;
     int rc;
     Py_BEGIN_ALLOW_THREADS
@@ -335,9 +345,9 @@ static PyObject *py_paged_attn_workspace_bytes(PyObject *self, PyObject *const *
     return PyLong_FromLong((long)f_paged_bytes(&c, x[0], x[1], x[2], x[3]));
 }
 
-/* (cache, q, row_off, out, max_rows_per_seq, workspace, current device, stream): the status code of the library call */
+/* (cache, q, row_off, out, max_rows_per_seq, workspace): the status code of the library call */
 static PyObject *py_paged_attn(PyObject *self, PyObject *const *a, Py_ssize_t n) {
-    if (!ready(n, 8)) return NULL;
+    if (!ready(n, 6)) return NULL;
     dkv_paged_cache c;
     tensor_info q, out, ws = {0};
     int64_t stride;
@@ -366,7 +376,7 @@ static PyObject *py_paged_attn(PyObject *self, PyObject *const *a, Py_ssize_t n)
         Py_DECREF(b);
         if (PyErr_Occurred()) return NULL;
     }
-    if (look_place(a[6], a[7], device, &stream)) return NULL;
+    if (look_place(device, &stream)) return NULL;
     int rc;
     Py_BEGIN_ALLOW_THREADS
     rc = f_paged_attn(&c, q.ptr, stride, off, out.ptr, q.dims[0], most, q.dims[1], q.dtype, ws.ptr, bytes, stream);
@@ -375,10 +385,10 @@ static PyObject *py_paged_attn(PyObject *self, PyObject *const *a, Py_ssize_t n)
 }
 
 /* bind_paged(addresses of dkv_paged_store, _load, _attn_workspace_bytes, _attn, then the types bfloat16, float32, float8_e4m3fn,
- * float8_e8m0fnu, int32) */
+ * float8_e8m0fnu, int32, and what tells the current device and stream) */
 static PyObject *py_bind_paged(PyObject *self, PyObject *const *a, Py_ssize_t n) {
-    if (n != 4 + T_COUNT) {
-        PyErr_SetString(PyExc_TypeError, "four addresses and five types are expected");
+    if (n != 5 + T_COUNT) {
+        PyErr_SetString(PyExc_TypeError, "four addresses, five types and a source of streams are expected");
         return NULL;
     }
     void *f[4];
@@ -390,6 +400,10 @@ static PyObject *py_bind_paged(PyObject *self, PyObject *const *a, Py_ssize_t n)
         dtypes[i] = a[4 + i];
         Py_XDECREF(old);
     }
+    PyObject *before = place_of;
+    Py_INCREF(a[4 + T_COUNT]);
+    place_of = a[4 + T_COUNT];
+    Py_XDECREF(before);
     f_paged_store = (paged_store_fn)f[0];
     f_paged_load = (paged_load_fn)f[1];
     f_paged_bytes = (paged_bytes_fn)f[2];
@@ -419,5 +433,7 @@ PyMODINIT_FUNC PyInit__marshal(void) {
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     s_get_device = PyUnicode_InternFromString("get_device");
     s_stride = PyUnicode_InternFromString("stride");
-    return s_data_ptr && s_shape && s_nbytes && s_value && s_dtype && s_is_contiguous && s_get_device && s_stride ? PyModule_Create(&module) : NULL;
+    s_current = PyUnicode_InternFromString("_cuda_getDevice");
+    s_stream = PyUnicode_InternFromString("_cuda_getCurrentRawStream");
+    return s_data_ptr && s_shape && s_nbytes && s_value && s_dtype && s_is_contiguous && s_get_device && s_stride && s_current && s_stream ? PyModule_Create(&module) : NULL;
 }
