@@ -397,18 +397,30 @@ __global__ __launch_bounds__(256) void paged_merge(const int *__restrict__ row_o
     __shared__ f32x4 os[GROUPS][CH];
     __shared__ float2 stats[GROUPS];
     const int tid = threadIdx.x, lane = tid % CH, group = tid / CH, pair = (int)blockIdx.x, r = Hq.div(pair), h = Hq.mod(pair);
-    const int b = sequence_of_row(row_off, batch, r);              // uniform
-    if (b >= batch) return;
-    const int in = row_off ? r - row_off[b] : 0;
-    const int2 sl = meta[b];                                       // first slice, slices
-    if ((unsigned)in >= (unsigned)max_rows || sl.y <= 1) return;
+    // the row's sequence, its first row and slices: a lane per sequence asks for all three at once
+    int in = 0, first = 0, n = 0;
+    for (int i = 0; i < batch; i += 64) {
+        const int b = min(i + (tid & 63), batch - 1);
+        int r0, rows_here;
+        rows_of_sequence(row_off, b, r0, rows_here);
+        const int2 slices = meta[b];
+        const unsigned long long hit = __builtin_amdgcn_ballot_w64(r >= r0 && r < r0 + rows_here && b == i + (tid & 63));
+        if (hit) {
+            const int l = __builtin_ctzll(hit);
+            in = r - __builtin_amdgcn_readlane(r0, l);
+            first = __builtin_amdgcn_readlane(slices.x, l);
+            n = __builtin_amdgcn_readlane(slices.y, l);
+            break;
+        }
+    }
+    if ((unsigned)in >= (unsigned)max_rows || n <= 1) return;      // no sequence, left out, or done
     const int kvh = G.div(h), mq = in * G.d + G.mod(h), heads = G.div(Hq.d);
     const size_t step = (size_t)heads * q_rows * REC;
-    const float *rec = part + (((size_t)sl.x * heads + kvh) * q_rows + mq) * REC;
+    const float *rec = part + (((size_t)first * heads + kvh) * q_rows + mq) * REC;
     float m = -3.0e38f, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = group; s < sl.y; s += 2 * GROUPS) {
-        const bool two = s + GROUPS < sl.y;
+    for (int s = group; s < n; s += 2 * GROUPS) {
+        const bool two = s + GROUPS < n;
         const float *x = rec + s * step, *y = two ? x + GROUPS * step : x;
         const float2 xs = *reinterpret_cast<const float2 *>(x), ys = *reinterpret_cast<const float2 *>(y);
         const f32x4 xo = *reinterpret_cast<const f32x4 *>(x + 4 + 4 * lane), yo = *reinterpret_cast<const f32x4 *>(y + 4 + 4 * lane);
