@@ -36,9 +36,10 @@ int allow_lds(const void *kernel, int bytes, std::atomic<uint64_t> &devices) {
 
 struct Plan {
     int nq, q_groups;       // query tiles of 16 rows per workgroup, groups of them
+    int wide;               // 0: paged_attn_split; paged_attn_wide: groups of wavefronts in a workgroup
+    int blocks;             // blocks of 128 query rows over all K/V heads at most: the workgroups of paged_attn_wide without slices
+    bool split;             // whether a sequence can have several slices
     int cap;                // slices of the whole batch at most
-    bool split;             // whether a sequence can have several
-    int wide, wide_groups;  // paged_wide.h: blocks of 128 query rows at most, or 0; groups of wavefronts in a workgroup
     SlicePlan slices;
 };
 
@@ -46,7 +47,7 @@ struct Plan {
 // (two sequences of 131072 keys: 56 us with 256 workgroups, 67 with 512). A slice has 4 tiles of keys at least: what a compute unit
 // reads is bound to some 50 GB/s, so idle units cost more than wavefronts without a tile (28/4 heads, 4 sequences of 2000 keys in
 // bf16: 10.5 us with 4 tiles, 11.4 with 8, 17.2 with 32, 22.3 without slices).
-constexpr int kWorkgroups = 256, kLeast = 4;
+constexpr int kWorkgroups = 256, kLeast = 4, kLeastWide = 16;
 // Key tiles up to which a sequence stays whole: the launch that joins slices costs some 2 us. bf16, 128 dims: 16 tiles 8.6 us whole and 9.0
 // in slices, 24 tiles 11.5 and 9.3; 64 dims: 24 tiles 7.3 and 8.1, 47 tiles 10.8 and 9.0. fp32 (four wavefronts, matrix instructions of an
 // eighth of the rate): 128 dims, 8 tiles 13.3 and 11.8; 64 dims, 8 tiles 7.4 and 8.4, 16 tiles 12.1 and 8.5; 32 dims, 16 tiles 7.5 and 8.2, 24 9.7 and 8.5.
@@ -59,29 +60,59 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     const int tiles = ceil_div(max_rows > 0 ? max_rows * G : 1, 16), key_tiles = ceil_div(c.max_pages << c.page_shift, PKT);
     p.nq = dtype == DKV_BF16 && tiles > 1 ? 2 : 1;
     p.q_groups = ceil_div(tiles, p.nq);
-    const int64_t whole = (int64_t)c.n_kv_heads * p.q_groups;       // workgroups of one slice for each sequence: batch times this
+    int64_t whole = (int64_t)c.n_kv_heads * p.q_groups;             // workgroups of one slice for each sequence: batch times this
     // Blocks of 128 query rows (paged_wide.h) where tiles of 32 would make more than one round of workgroups: 28/4 heads, 1024 keys, 1
-    // sequence of 300 rows (264 workgroups) 42 -> 22 us, 4 of 128 rows (448) 30 -> 23, but 4 of 64 rows (224) 19 -> 22 and 16 of 16
-    // rows (256) 18 -> 25; 4096 keys the same way round. Two groups of wavefronts to a workgroup where the blocks are few and the
+    // sequence of 300 rows (264 workgroups) 42 -> 22 us, 4 of 128 rows (448) 30 -> 23, but 4 of 64 rows (224) 16 -> 22 and 16 of 16
+    // rows (256) 18 -> 25. Also where the keys are so many that slices of them keep the compute units busy without those
+    // workgroups: 1536 keys each for tiles of 32 (28/4 heads, 1 sequence of 128 rows, 4096 keys 30.5 -> 27.2 us, 32768 keys 128 -> 82, but
+    // 32 rows, 4096 keys 16.5 -> 19.7, 8192 keys 20.8 -> 21.6), of more than 4096 keys of 128 dims (64 dims, 2 sequences of 128 rows: 4096 keys
+    // 25.1 -> 28.7, 8192 keys 43.6 -> 40.6). Two groups of wavefronts to a workgroup where the blocks are few and the
     // keys many enough to share: 96 blocks of 1024 keys 24.8 -> 22.5 us, 384 blocks 41 -> 47, 128 blocks of 256 keys 11.8 -> 12.6.
-    p.wide = p.wide_groups = 0;
-    if (dtype == DKV_BF16 && head_dim >= 64 && max_rows * G > 64 && c.batch * whole > kWorkgroups) {
+    // Their keys are cut from 4096 on, where every sequence can have two slices: 8 heads, 300 rows (80 blocks of 64 dims), 2048 keys
+    // 27.2 us whole and 27.9 in slices, 4096 keys 47.6 and 34.3; at 128 dims, 2048 keys 36.2 and 34.4, 4096 keys 62.3 and 43.8.
+    p.wide = p.blocks = 0;
+    int least = kLeast, share = 1;
+    p.split = key_tiles > whole_tiles(dtype, head_dim);
+    const int64_t keys = (int64_t)key_tiles * PKT;
+    if (dtype == DKV_BF16 && head_dim >= 64 && max_rows * G > 64 &&
+        (c.batch * whole > kWorkgroups || (keys * head_dim >= 4096 * 128 && c.batch * whole * keys >= kWorkgroups * 1536))) {
         const int64_t blocks = c.batch + (int64_t)ceil_div(rows * G, 128), bound = (int64_t)c.batch * ceil_div(max_rows * G, 128);
-        p.wide = (int)((blocks < bound ? blocks : bound) * c.n_kv_heads);
-        p.wide_groups = p.wide <= 320 && key_tiles > 16 ? 2 : 1;
+        p.blocks = (int)((blocks < bound ? blocks : bound) * c.n_kv_heads);
+        p.wide = p.blocks <= 320 && key_tiles > 16 ? 2 : 1;
+        p.nq = 8;
+        p.q_groups = ceil_div(tiles, p.nq);
+        whole = (int64_t)c.n_kv_heads * p.q_groups;
+        least = kLeastWide;
+        share = 2;
+        p.split = p.wide == 2 && keys >= 4096;
     }
-    p.split = key_tiles > whole_tiles(dtype, head_dim) && c.batch * whole < kWorkgroups;
+    // Slices of a K/V head, all sequences together. The workgroups of one slice are on one XCD, and so many to an XCD that all run at once
+    // (28/4 heads, 32 rows, 8192 keys: 7 workgroups to a slice; 9 slices are 35 workgroups to some XCDs and 29.6 us, 8 are 28 and 20.8).
+    const int on_xcd = kWorkgroups / 8 / p.q_groups;
+    const int want = on_xcd ? on_xcd * 8 / c.n_kv_heads : (int)(kWorkgroups / whole);
+    p.split = p.split && (share == 1 ? want > c.batch : want >= 2 * c.batch);
     p.slices.split = p.split;
-    p.slices.want = Divisor(p.split ? (int)(kWorkgroups / whole) : 1);
-    p.slices.least = kLeast;
-    // at most `want` slices where that is twice the sequences or more (see slice_length), else `want` and one for each sequence
-    const int64_t most = (int64_t)c.batch * ceil_div(key_tiles, kLeast), cap = (int64_t)c.batch + p.slices.want.d + 1;
-    p.cap = !p.split ? c.batch : (int)(most < cap ? most : cap);
+    p.slices.want = Divisor(p.split ? want : 1);
+    p.slices.least = least;
+    const int64_t most = (int64_t)c.batch * ceil_div(key_tiles, least);
+    p.cap = !p.split ? c.batch : (int)(most < want ? most : want);      // see slice_length
     return p;
 }
 
+// Workspace: (first slice, slices) of each sequence, then the records.
+size_t meta_bytes(const PagedCache &c) { return align_up(c.batch * sizeof(int2), 16); }
 size_t partial_bytes(const Plan &p, const PagedCache &c, int head_dim) {
-    return p.split && !p.wide ? align_up(c.batch * sizeof(int2), 16) + (size_t)p.cap * c.n_kv_heads * (p.q_groups * p.nq * 16) * (head_dim + 4) * sizeof(float) : 0;
+    return p.split ? meta_bytes(c) + (size_t)p.cap * c.n_kv_heads * (p.q_groups * p.nq * 16) * (head_dim + 4) * sizeof(float) : 0;
+}
+unsigned split_grid(const Plan &p, const PagedCache &c) { return (unsigned)(ceil_div(p.cap * c.n_kv_heads, 8) * 8 * p.q_groups); }
+
+template <typename T, int DH>
+int launch_merge(const PagedCache &c, const Plan &p, const int *row_off, void *out, void *part, int rows, int max_rows, int Hq, hipStream_t s) {
+    hipLaunchKernelGGL((paged_merge<T, DH>), dim3((unsigned)(rows * Hq)), dim3(256), 0, s, row_off, c.batch, (const int2 *)part,
+                       (const float *)((char *)part + meta_bytes(c)), (T *)out, rows, max_rows, Divisor(Hq), Divisor(Hq / c.n_kv_heads),
+                       p.q_groups * p.nq * 16);
+    DKV_LAUNCH_CHECK();
+    return DKV_OK;
 }
 
 template <typename T, typename C, int DH, int NQ, int NW>
@@ -89,42 +120,34 @@ int launch_split(const PagedCache &c, const Plan &p, const void *q, int64_t q_st
                  int max_rows, int Hq, hipStream_t s) {
     constexpr int smem = NW * SplitSmem<T, DH>::WAVE_BYTES;
     const float scale_log2e = 1.4426950408889634f / sqrtf((float)DH);
-    int2 *meta = static_cast<int2 *>(part);
-    float *records = reinterpret_cast<float *>(static_cast<char *>(part) + align_up(c.batch * sizeof(int2), 16));
-    const unsigned grid = (unsigned)(ceil_div(p.cap * c.n_kv_heads, 8) * 8 * p.q_groups);
 #define SPLIT(ONCE)                                                                                                              \
     do {                                                                                                                         \
         static std::atomic<uint64_t> devices{0};                                                                                 \
         const int rc = allow_lds(reinterpret_cast<const void *>(&paged_attn_split<T, C, DH, NQ, NW, ONCE>), smem, devices);      \
         if (rc) return rc;                                                                                                       \
-        hipLaunchKernelGGL((paged_attn_split<T, C, DH, NQ, NW, ONCE>), dim3(grid), dim3(64 * NW), smem, s, c, p.slices, (const T *)q, \
-                           q_stride, row_off, (T *)out, meta, records, rows, max_rows, Divisor(p.q_groups), Divisor(c.n_kv_heads), \
-                           Divisor(Hq / c.n_kv_heads), scale_log2e);                                                             \
+        hipLaunchKernelGGL((paged_attn_split<T, C, DH, NQ, NW, ONCE>), dim3(split_grid(p, c)), dim3(64 * NW), smem, s, c, p.slices, \
+                           (const T *)q, q_stride, row_off, (T *)out, (int2 *)part, (float *)((char *)part + meta_bytes(c)), rows, max_rows, \
+                           Divisor(p.q_groups), Divisor(c.n_kv_heads), Divisor(Hq / c.n_kv_heads), scale_log2e);                \
     } while (0)
     if (p.q_groups == 1) SPLIT(true);
     else SPLIT(false);
 #undef SPLIT
     DKV_LAUNCH_CHECK();
-    if (p.split) {
-        hipLaunchKernelGGL((paged_merge<T, DH>), dim3((unsigned)(rows * Hq)), dim3(256), 0, s, row_off, c.batch,
-                           (const int2 *)meta, (const float *)records, (T *)out, rows, max_rows, Divisor(Hq), Divisor(Hq / c.n_kv_heads),
-                           p.q_groups * NQ * 16);
-        DKV_LAUNCH_CHECK();
-    }
-    return DKV_OK;
+    return p.split ? launch_merge<T, DH>(c, p, row_off, out, part, rows, max_rows, Hq, s) : DKV_OK;
 }
 
 template <typename C, int DH, int KS>
-int launch_wide(const PagedCache &c, const Plan &p, const void *q, int64_t q_stride, const int *row_off, void *out, int rows, int max_rows,
-                int Hq, hipStream_t s) {
+int launch_wide(const PagedCache &c, const Plan &p, const void *q, int64_t q_stride, const int *row_off, void *out, void *part, int rows,
+                int max_rows, int Hq, hipStream_t s) {
     static std::atomic<uint64_t> devices{0};
     const int rc = allow_lds(reinterpret_cast<const void *>(&paged_attn_wide<C, DH, KS>), KS * kWideLds<DH>, devices);
     if (rc) return rc;
-    hipLaunchKernelGGL((paged_attn_wide<C, DH, KS>), dim3((unsigned)p.wide), dim3(256 * KS), KS * kWideLds<DH>, s, c, (const bf16_t *)q, q_stride, row_off,
-                       (bf16_t *)out, rows, max_rows, Divisor(c.n_kv_heads), Divisor(Hq / c.n_kv_heads), kWorkgroups / c.n_kv_heads,
+    hipLaunchKernelGGL((paged_attn_wide<C, DH, KS>), dim3(p.split ? split_grid(p, c) : (unsigned)p.blocks), dim3(256 * KS), KS * kWideLds<DH>, s, c,
+                       (const bf16_t *)q, q_stride, row_off, (bf16_t *)out, rows, (int2 *)part, (float *)((char *)part + meta_bytes(c)), p.slices,
+                       max_rows, Divisor(p.q_groups), Divisor(c.n_kv_heads), Divisor(Hq / c.n_kv_heads), kWorkgroups / c.n_kv_heads,
                        1.4426950408889634f / sqrtf((float)DH));
     DKV_LAUNCH_CHECK();
-    return DKV_OK;
+    return p.split ? launch_merge<bf16_t, DH>(c, p, row_off, out, part, rows, max_rows, Hq, s) : DKV_OK;
 }
 
 template <typename T, typename C, int DH>
@@ -134,8 +157,8 @@ int launch_heads(const PagedCache &c, const Plan &p, const void *q, int64_t q_st
         return launch_split<T, C, DH, 1, 4>(c, p, q, q_stride, row_off, out, part, rows, max_rows, Hq, s);
     } else {
         if constexpr (DH >= 64) {
-            if (p.wide_groups == 1) return launch_wide<C, DH, 1>(c, p, q, q_stride, row_off, out, rows, max_rows, Hq, s);
-            if (p.wide_groups == 2) return launch_wide<C, DH, 2>(c, p, q, q_stride, row_off, out, rows, max_rows, Hq, s);
+            if (p.wide == 1) return launch_wide<C, DH, 1>(c, p, q, q_stride, row_off, out, part, rows, max_rows, Hq, s);
+            if (p.wide == 2) return launch_wide<C, DH, 2>(c, p, q, q_stride, row_off, out, part, rows, max_rows, Hq, s);
         }
         return p.nq == 1 ? launch_split<T, C, DH, 1, 8>(c, p, q, q_stride, row_off, out, part, rows, max_rows, Hq, s)
                          : launch_split<T, C, DH, 2, 8>(c, p, q, q_stride, row_off, out, part, rows, max_rows, Hq, s);
@@ -160,7 +183,7 @@ int attn_call(const dkv_paged_cache *cache, PagedCache &view, Plan &plan, int32_
     if ((int64_t)rows * n_q_heads < 1 << 24 && (int64_t)cache->batch * cache->n_kv_heads < 1 << 22 &&
         (int64_t)cache->batch * cache->max_pages * cache->page_size <= 1ll << 35) {
         plan = make_plan(view, n_q_heads, rows, max_rows_per_seq, dtype, cache->head_dim);
-        if (plan.wide ? plan.wide < 1 << 23 : (int64_t)plan.cap * cache->n_kv_heads * plan.q_groups < 1 << 22) return DKV_OK;
+        if (plan.wide && !plan.split ? plan.blocks < 1 << 23 : (int64_t)plan.cap * cache->n_kv_heads * plan.q_groups < 1 << 22) return DKV_OK;
     }
     dkv_set_error("%d rows of %d heads in %d sequences are too many for one call", rows, n_q_heads, cache->batch);
     return DKV_E_UNSUPPORTED;

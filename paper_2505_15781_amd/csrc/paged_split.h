@@ -18,9 +18,9 @@
 
 constexpr int PKT = 32;                // keys per tile
 
-// How the keys of a batch are cut: into at most `want` slices for one K/V head and query group over the whole batch where that
-// is possible (each sequence with rows has one at least), none shorter than `least` tiles before they are evened
-// out within their sequence. want = 0: one slice for each sequence.
+// How the keys of a batch are cut: into at most `want` slices for one K/V head and query group over the whole batch (each sequence
+// with rows has one at least, and there are fewer sequences than `want`), none shorter than `least` tiles before they are evened
+// out within their sequence.
 struct SlicePlan {
     int least;
     Divisor want;
@@ -40,9 +40,13 @@ __device__ __forceinline__ int wave_prefix(int x) {        // inclusive: within 
     x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
     return x;
 }
-// x / d rounded up for 0 <= x < 2^25, from an approximate quotient that is off by one at most
+// x / d rounded up for 0 <= x <= 2^25 and d > 0: a quotient that is off by a few at most, that of what it leaves, and one more or less
 __device__ __forceinline__ int ceil_div_fast(int x, int d) {
-    int q = (int)((float)x * __builtin_amdgcn_rcpf((float)d)), r = x - q * d;
+    const float inv = __builtin_amdgcn_rcpf((float)d);
+    int q = (int)((float)x * inv), r = x - q * d;
+    const int more = (int)((float)r * inv);
+    q += more;
+    r -= more * d;
     if (r < 0) --q, r += d;
     return q + (r > 0) + (r > d);
 }
@@ -51,8 +55,8 @@ __device__ __forceinline__ int key_tiles(int keys, int rows) { return rows > 0 ?
 __device__ __forceinline__ int key_tiles(const PagedCache &c, const int *row_off, int b) {
     return key_tiles(c.keys(b), row_off ? row_off[b + 1] - row_off[b] : 1);
 }
-// Key tiles of a slice: the least that makes at most `want` slices of the whole batch, or (where rounding up within the sequences
-// makes more than that) a length that surely does. Whole wavefronts; `tiles`: of sequence `lane`.
+// Key tiles of a slice: a want-th of all, or, where rounding up within the sequences makes more than `want` slices of that, a
+// (want - batch)th: no more than want - batch whole slices, and one for each sequence's rest. Whole wavefronts; `tiles`: of sequence `lane`.
 __device__ __forceinline__ int slice_length(const PagedCache &c, const int *row_off, const SlicePlan &plan, int tiles) {
     const int lane = threadIdx.x & 63;
     auto sum = [&](auto f) {
@@ -62,7 +66,7 @@ __device__ __forceinline__ int slice_length(const PagedCache &c, const int *row_
     };
     const int total = sum([](int x) { return x; });
     int slice = max(plan.least, plan.want.div(total + plan.want.d - 1));
-    if (sum([&](int x) { return ceil_div_fast(x, slice); }) > plan.want.d) slice = max(plan.least, ceil_div(total, max(plan.want.d - c.batch, 1)));
+    if (sum([&](int x) { return ceil_div_fast(x, slice); }) > plan.want.d) slice = max(plan.least, ceil_div(total, plan.want.d - c.batch));
     return slice;
 }
 // Whole wavefronts. Finds slice `at` of the batch; false if there are fewer.
@@ -180,12 +184,14 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
     if (!plan.split && at < c.batch) entry = load_entry(at, first_key(0, 0));
     Slices sl;
     if (!find_slice(c, row_off, plan, at, sl)) return;
-    const int b = sl.b, r0 = sl.r0, len = sl.keys;
-    const int nq = min(sl.rows, max_rows) * G.d, m0 = qg * NQ * 16;   // query rows of this (sequence, K/V head), first one here
+    // the same in every lane, which the compiler does not see behind the two ways to a slice
+    auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+    const int b = uniform(sl.b), r0 = uniform(sl.r0), len = uniform(sl.keys), first = uniform(sl.first), n_slices = uniform(sl.n);
+    const int nq = uniform(min(sl.rows, max_rows)) * G.d, m0 = qg * NQ * 16;      // query rows of this (sequence, K/V head), first one here
     if (m0 >= nq) return;                                             // uniform for the workgroup
-    const int tiles = key_tiles(len, 1), per = plan.split ? ceil_div_fast(tiles, sl.n) : tiles;
-    const int t_begin = (at - sl.first) * per, t_end = min(tiles, t_begin + per);
-    if (plan.split && tid == 0 && at == sl.first && kvh == 0 && qg == 0) meta[b] = make_int2(sl.first, sl.n);
+    const int tiles = key_tiles(len, 1), per = plan.split ? uniform(ceil_div_fast(tiles, n_slices)) : tiles;
+    const int t_begin = (at - first) * per, t_end = min(tiles, t_begin + per);
+    if (plan.split && tid == 0 && at == first && kvh == 0 && qg == 0) meta[b] = make_int2(first, n_slices);
     const int64_t q_rows = groups.d * (NQ * 16);
 
     // the page of such an entry; -1: none, or behind the end
@@ -374,7 +380,7 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
             lsum += wgt * rec[1];
             o += wgt * *reinterpret_cast<const f32x4 *>(rec + 4 + 4 * ch);
         }
-        if (sl.n == 1) {
+        if (n_slices == 1) {
             store_result(out + (((size_t)r * c.n_kv_heads + kvh) * G.d + G.mod(mq)) * DH + 4 * ch, o, lsum);
         } else {
             float *rec = part + (unit * q_rows + mq) * REC;

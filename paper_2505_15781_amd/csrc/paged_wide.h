@@ -7,7 +7,7 @@
 // their places are found once per tile from page numbers that a lane each holds for the next 1024 keys.
 //   bf16: global memory to LDS without registers; keys that are not there (behind the end, no page) come from a row of zeros.
 //   e4m3: through registers, a tile ahead, converted with their row's scale (exact) on the way into LDS. K and V are converted
-//         once per 128 query rows: 32 of a wavefront's vector instructions per tile, next to some 280 of softmax and rescaling.
+//         once per 128 query rows: 32 of a wavefront's vector instructions per tile, next to some 230 of the softmax.
 #pragma once
 
 typedef __attribute__((address_space(3))) void *lds_ptr_t;
@@ -30,6 +30,7 @@ __device__ __align__(256) const u32x4 zero_row[16] = {};
 // heads go fastest: the blocks of a head, which read the same keys, are on one XCD (id % 8) with 8 heads, on two with 4.
 // With two groups of wavefronts a workgroup takes one block of a long sequence, a group each half of its key tiles (parts = 2), or two
 // blocks of a short one, a group each: as many sequences are long as `units` workgroups (one per compute unit) have room for.
+// (Where blocks are so few that compute units would be idle, the keys are cut into slices as for paged_attn_split instead.)
 struct WideItem {
     Slices seq;
     int kvh, qb, parts;                // qb: the first block
@@ -86,7 +87,8 @@ struct WideTile {
 template <typename C, int DH, int KS>
 __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, DH == 128 ? 2 : 4))) void paged_attn_wide(
     PagedCache c, const bf16_t *__restrict__ Q, int64_t q_stride, const int *__restrict__ row_off, bf16_t *__restrict__ out, int rows,
-    int max_rows, Divisor heads, Divisor G, int units, float scale_log2e) {
+    int2 *__restrict__ meta, float *__restrict__ partial, SlicePlan plan, int max_rows, Divisor blocks, Divisor heads, Divisor G, int units,
+    float scale_log2e) {
     constexpr int NW = 4, ROW = DH * 2, KT2 = 64, TILE = KT2 * ROW;     // bytes of an LDS row, of a K or V tile
     constexpr bool E4M3 = sizeof(C) == 1;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_all[];
@@ -97,13 +99,36 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
     unsigned char *smem_raw = smem_all + group_id * kWideLds<DH>;
     const int qi = lane & 31, g = lane >> 5, l16 = lane & 15, l4 = lane >> 4;
     const uint32_t lds_base = (uint32_t)(size_t)(lds_ptr_t)smem_raw;
+    // a group works on the tiles t0 + part, t0 + part + parts, ... below t1
     WideItem item;
-    if (!wide_item<KS>(c, row_off, max_rows, heads, G.d, units, item)) return;
-    const int b = item.seq.b, r0 = item.seq.r0, L = item.seq.keys, kvh = item.kvh;
-    // a group works on the tiles part, part + parts, ... of the sequence
-    const int parts = KS == 1 ? 1 : item.parts, part = parts == 1 ? 0 : group_id;
-    const int n_tiles = (max(1, (L + KT2 - 1) / KT2) + parts - 1) / parts;
-    const int nq = min(item.seq.rows, max_rows) * G.d, mb0 = (item.qb + (parts == 1 ? group_id : 0)) * NW * 32;
+    int parts = 1, t0 = 0, t1 = INT_MAX, slices = 1;
+    int64_t record = 0;                              // first record of this (slice, K/V head)
+    if (KS == 2 && plan.split) {                     // slices as in paged_attn_split, two groups to a block
+        const int slot = (int)(blockIdx.x >> 3), unit = blocks.div(slot) * 8 + (int)(blockIdx.x & 7), at = heads.div(unit);
+        item.qb = blocks.mod(slot);
+        item.kvh = heads.mod(unit);
+        if (!find_slice(c, row_off, plan, at, item.seq)) return;
+        slices = item.seq.n;
+        parts = 2;
+        const int tiles = (key_tiles(item.seq.keys, 1) + 1) / 2, per = __builtin_amdgcn_readfirstlane(ceil_div_fast(tiles, slices));
+        t0 = (at - item.seq.first) * per;
+        t1 = t0 + per;
+        record = (int64_t)unit * (blocks.d * 128);
+        if (threadIdx.x == 0 && at == item.seq.first && item.kvh == 0 && item.qb == 0) meta[item.seq.b] = make_int2(item.seq.first, slices);
+    } else {
+        if (!wide_item<KS>(c, row_off, max_rows, heads, G.d, units, item)) return;
+        if (KS == 2) parts = item.parts;
+    }
+    // all of it the same in every lane, which the compiler does not see behind the two ways to an item
+    auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+    parts = KS == 1 ? 1 : uniform(parts);
+    t0 = KS == 1 ? 0 : uniform(t0);
+    const int part = parts == 1 ? 0 : group_id, b = uniform(item.seq.b), r0 = uniform(item.seq.r0), kvh = uniform(item.kvh);
+    const int keys = uniform(item.seq.keys), tiles = (keys + KT2 - 1) / KT2, end = KS == 1 ? tiles : uniform(min(tiles, t1));
+    const int L = end < tiles ? end * KT2 : keys;                     // keys from here on are another slice's, or none
+    const int n_tiles = (max(1, end - t0) + parts - 1) / parts;
+    const int nq = uniform(min(item.seq.rows, max_rows)) * G.d, mb0 = (uniform(item.qb) + (parts == 1 ? group_id : 0)) * NW * 32;
+    if (KS == 2 && mb0 >= nq && parts == 2) return;                   // uniform for the workgroup
 
     // this lane's query row; rows beyond the host's bound have no slot in Q and out
     const int mq = mb0 + wave * 32 + qi, r = r0 + G.div(mq), h = kvh * G.d + G.mod(mq);
@@ -120,10 +145,10 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
     };
     uint32_t group, group_ahead;
     unsigned long long pages, pages_ahead;
-    look_up(0, group, pages);
-    look_up(1, group_ahead, pages_ahead);
+    look_up((t0 + part) >> 4, group, pages);
+    look_up(((t0 + part) >> 4) + 1, group_ahead, pages_ahead);
     auto find = [&](int step) {                     // steps in order
-        const int t = step * parts + part;
+        const int t = t0 + step * parts + part;
         WideTile x;
 #pragma unroll
         for (int i = 0; i < 4; ++i) x.row[i] = __builtin_amdgcn_readlane(group, (t & 15) * 4 + i);
@@ -136,8 +161,8 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
         return x;
     };
     // keys that are there of a tile's group
-    auto there = [&](int step, int tile_pages, int i) { return tile_pages >> i & 1 ? L - ((step * parts + part) * KT2 + 16 * i) : 0; };
-    auto whole = [&](int step, int tile_pages) { return tile_pages == 15 && (step * parts + part + 1) * KT2 <= L; };
+    auto there = [&](int step, int tile_pages, int i) { return tile_pages >> i & 1 ? L - ((t0 + step * parts + part) * KT2 + 16 * i) : 0; };
+    auto whole = [&](int step, int tile_pages) { return tile_pages == 15 && (t0 + step * parts + part + 1) * KT2 <= L; };
 
     // bf16. Load i of a wavefront fills rows RPL (4 i + wave) + [0, RPL) of a tile; lane -> row lane / LPR, place lane % LPR.
     constexpr int LPR = ROW / 16, RPL = 64 / LPR, LOADS = KT2 / (RPL * NW);
@@ -393,6 +418,7 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
         const float2 other = stats[tid];
         const float m = fmaxf(m_run, other.x), mine = __builtin_amdgcn_exp2f(m_run - m), theirs = __builtin_amdgcn_exp2f(other.x - m);
         sum = mine * sum + theirs * other.y;
+        m_run = m;
 #pragma unroll
         for (int i = 0; i < DH / 8; ++i) {
             const f32x4 x = parked[i * 256 + tid];
@@ -400,8 +426,20 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
             for (int e = 0; e < 4; ++e) acc[i >> 2][4 * (i & 3) + e] = mine * acc[i >> 2][4 * (i & 3) + e] + theirs * x[e];
         }
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
     if (!q_ok) return;
+    if (KS == 2 && slices > 1) {                     // a record for paged_merge: m, l, -, -, o[DH]
+        float *rec = partial + (record + mq) * (DH + 4);
+        if (g == 0) {
+            rec[0] = m_run;
+            rec[1] = sum;
+        }
+#pragma unroll
+        for (int i = 0; i < DH / 8; ++i)
+            *reinterpret_cast<f32x4 *>(rec + 4 + 32 * (i >> 2) + 8 * (i & 3) + 4 * g) =
+                f32x4{acc[i >> 2][4 * (i & 3)], acc[i >> 2][4 * (i & 3) + 1], acc[i >> 2][4 * (i & 3) + 2], acc[i >> 2][4 * (i & 3) + 3]};
+        return;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
     bf16_t *op = out + ((size_t)r * (c.n_kv_heads * G.d) + h) * DH + 8 * g;
 #pragma unroll
     for (int mt = 0; mt < DH / 32; ++mt)

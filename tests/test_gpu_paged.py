@@ -183,7 +183,8 @@ ATTN = [  # lens, rows, page, kv heads, group, dh
     ([333, 1000, 16], [40, 70, 16], 16, 3, 1, 128), ([769, 100, 257], [65, 129, 33], 32, 2, 7, 128), ([300, 513], [130, 257], 256, 2, 1, 64),
     ([200, 40], [17, 23], 16, 4, 1, 32), ([2100], [1], 16, 1, 16, 32), ([640, 448], [300, 64], 64, 8, 4, 128), ([1, 2, 3], [130, 1, 140], 16, 26, 1, 128),
     ([1333, 64, 333, 0], [200, 100, 400, 70], 16, 8, 4, 128), ([63, 129, 1024], [300, 5, 900], 128, 32, 1, 128),
-    ([300, 1050, 40], [130, 257, 1], 256, 16, 2, 64), ([100, 190, 80, 70], [300, 300, 200, 100], 16, 32, 1, 64)]
+    ([300, 1050, 40], [130, 257, 1], 256, 16, 2, 64), ([100, 190, 80, 70], [300, 300, 200, 100], 16, 32, 1, 64),
+    ([4500, 40, 2100], [100, 70, 129], 32, 2, 4, 128), ([9000, 0, 2081], [50, 257, 130], 64, 1, 4, 64), ([5000, 2081], [150, 257], 64, 8, 4, 64)]
 
 
 @pytest.mark.parametrize("types", ["bf16 bf16", "bf16 e4m3", "fp32 fp32", "fp32 e4m3"])
@@ -232,7 +233,7 @@ def test_attention_to_large_scores_infinities_and_nan(types, n, most):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
-@pytest.mark.parametrize("heads,group,dh,most,longest", [(1, 2, 64, 1, 1500), (1, 4, 128, 3, 2100), (4, 4, 128, 40, 300), (2, 2, 64, 40, 700), (2, 2, 128, 45, 900)])
+@pytest.mark.parametrize("heads,group,dh,most,longest", [(1, 2, 64, 1, 1500), (1, 4, 128, 3, 2100), (4, 4, 128, 40, 300), (2, 2, 64, 40, 700), (2, 2, 128, 45, 900), (1, 4, 128, 30, 4200)])
 def test_attention_of_more_sequences_than_a_wavefront_has_lanes(heads, group, dh, most, longest, dtype):
     """70 sequences, some without keys and some without rows, whose keys are cut into slices, or whose rows make blocks of 128."""
     g = np.random.default_rng(heads * dh + most)
