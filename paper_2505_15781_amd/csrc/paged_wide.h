@@ -32,7 +32,8 @@ template <int DH> __device__ __forceinline__ int wide_swizzle(int row) {
 __device__ __align__(256) const u32x4 zero_row[16] = {};
 
 // Work item of this workgroup: the sequences in the order of their key tiles, the longest first (64 of them at a time), so that
-// compute units that get two workgroups get short ones, and none without rows stands between others. Within a sequence the K/V
+// compute units that get two workgroups get short ones, and none without rows stands between others (rows behind those of the call
+// count for nothing: the host has no workgroups for them). Within a sequence the K/V
 // heads go fastest: the blocks of a head, which read the same keys, are on one XCD (id % 8) with 8 heads, on two with 4.
 // With two groups of wavefronts a workgroup takes one block of a long sequence, a group each half of its key tiles (parts = 2), or two
 // blocks of a short one, a group each: as many sequences are long as `units` workgroups (one per compute unit) have room for.
@@ -42,7 +43,7 @@ struct WideItem {
     int kvh, qb, parts;                // qb: the first block
 };
 template <int KS>
-__device__ __forceinline__ bool wide_item(const PagedCache &c, const int *row_off, int max_rows, Divisor heads, int G, int units, WideItem &w) {
+__device__ __forceinline__ bool wide_item(const PagedCache &c, const int *row_off, int total_rows, int max_rows, Divisor heads, int G, int units, WideItem &w) {
     const int lane = threadIdx.x & 63, at = heads.div(blockIdx.x);
     w.kvh = heads.mod(blockIdx.x);
     int before = 0;
@@ -50,7 +51,7 @@ __device__ __forceinline__ bool wide_item(const PagedCache &c, const int *row_of
         const int b = min(i + lane, c.batch - 1), keys = c.keys(b);
         int r0, rows;
         rows_of_sequence(row_off, b, r0, rows);
-        const int blocks = i + lane < c.batch ? (max(0, min(rows, max_rows)) * G + 127) / 128 : 0, cost = (keys + 63) / 64;
+        const int blocks = i + lane < c.batch ? (max(0, min(min(rows, max_rows), total_rows - r0)) * G + 127) / 128 : 0, cost = (keys + 63) / 64;
         int rank = 0;                                      // sequences before this one
         for (int k = 0; k < min(64, c.batch - i); ++k) {
             const int other = __builtin_amdgcn_readlane(cost, k);
@@ -122,7 +123,7 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
         record = (int64_t)unit * (blocks.d * 128);
         if (threadIdx.x == 0 && at == item.seq.first && item.kvh == 0 && item.qb == 0) meta[item.seq.b] = make_int2(item.seq.first, slices);
     } else {
-        if (!wide_item<KS>(c, row_off, max_rows, heads, G.d, units, item)) return;
+        if (!wide_item<KS>(c, row_off, rows, max_rows, heads, G.d, units, item)) return;
         if (KS == 2) parts = item.parts;
     }
     // all of it the same in every lane, which the compiler does not see behind the two ways to an item

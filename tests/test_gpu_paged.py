@@ -414,6 +414,18 @@ def test_rows_beyond_the_bound_of_a_sequence_are_left_out():
     assert (np.abs(out.double().cpu().numpy() - ref) <= bars(q, c, ref, spread, size))[ok].all()
 
 
+@pytest.mark.parametrize("group,n", [(4, 300), (2, 3)])
+def test_offsets_that_go_on_behind_the_rows_of_a_call(group, n):
+    """Sequences whose rows lie behind those of the call, with more keys than the one that has them: what is there is complete."""
+    c = Cache([200, 700, 600, 650], 16, 8, 128, "bf16", seed=2).fill()
+    q = rows(np.random.default_rng(2), (n, 8 * group, 128), "bf16")
+    out = torch.full_like(q, 7.0)
+    P.paged_attn(c.t, q, dev([0, n, 2 * n, 3 * n, 4 * n]), out, n, workspace(c, q, n))
+    ref, spread, size = O.attn(c.o, q.double().cpu().numpy(), np.array([0, n, n, n, n]))
+    fits = np.abs(out.double().cpu().numpy() - ref) <= bars(q, c, ref, spread, size)
+    assert fits.all()
+
+
 def test_positions_behind_four_gigabytes():
     """Pages whose offsets pass 32 bits: 2^18 slots of 4 heads of 128 dims behind the first ones, in bf16 2.1 GB a million rows."""
     page, heads, dh, n_pages = 4096, 4, 128, 1100
