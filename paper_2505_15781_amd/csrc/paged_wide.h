@@ -13,7 +13,9 @@
 // for data the same launch takes 160 us. Softmax, products and LDS reads hide behind each other: without its exponentials it takes
 // 5 % less, without the maximum 2 %, without the reads of V 4 %. Measured and not kept there: the maximum inside the stretch (193 us), 64 query rows
 // per wavefront (227), row sums by products with ones (182 against 179), e4m3 conversion spread over the stretch (no gain;
-// 64 dims 125 -> 150), two groups of wavefronts (187-209), LDS reads 9 and 12 ahead instead of 6 (no change).
+// 64 dims 125 -> 150), two groups of wavefronts (187-209), blocks of 256 query rows with eight
+// wavefronts behind one barrier, which halves the fills (201 against 183: two workgroups to a compute unit drift apart and fill each other's
+// gaps), LDS reads 9 and 12 ahead instead of 6 (no change).
 #pragma once
 
 typedef __attribute__((address_space(3))) void *lds_ptr_t;
