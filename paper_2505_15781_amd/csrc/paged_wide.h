@@ -368,11 +368,13 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
     for (int i = 0; i < DH / 16; ++i) stA = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(i, 0, 0), qf[i], stA, 0, 0, 0);
     maximum(stA, 0, 0, pages_0);
-    // Tile t, in stage S; the scores of its first half are formed.
-    auto step = [&](int t, auto stage) {
-        constexpr int S = decltype(stage)::value;
-        stretch(stB, S, 1, pB, S ^ 1, 1, stA, pA);
-        maximum(stB, t, 1, pages_0);
+    // Tile t, in stage S; the scores of its first half are formed. LIVE: a wavefront with query rows; the others bring their share of the tiles.
+    auto step = [&](int t, auto stage, auto alive) {
+        constexpr int S = decltype(stage)::value, LIVE = decltype(alive)::value;
+        if constexpr (LIVE) {
+            stretch(stB, S, 1, pB, S ^ 1, 1, stA, pA);
+            maximum(stB, t, 1, pages_0);
+        }
         // behind the barrier K(t + 1) and V(t) have landed for everybody, and everybody is done with K(t) and V(t - 1)
         tile_barrier();
         if constexpr (E4M3) {
@@ -397,13 +399,19 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
             pages_0 = pages_1;
             pages_1 = pages_2;
         }
-        stretch(stA, S ^ 1, 0, pA, S, 0, stB, pB);            // behind the last tile: scores of an old tile, never used
-        if (t + 1 < n_tiles) maximum(stA, t + 1, 0, pages_0);
+        if constexpr (LIVE) {
+            stretch(stA, S ^ 1, 0, pA, S, 0, stB, pB);        // behind the last tile: scores of an old tile, never used
+            if (t + 1 < n_tiles) maximum(stA, t + 1, 0, pages_0);
+        }
     };
-    for (int t = 0; t < n_tiles; t += 2) {
-        step(t, StageC<0>{});
-        if (t + 1 < n_tiles) step(t + 1, StageC<1>{});
-    }
+    auto all_steps = [&](auto alive) {
+        for (int t = 0; t < n_tiles; t += 2) {
+            step(t, StageC<0>{}, alive);
+            if (t + 1 < n_tiles) step(t + 1, StageC<1>{}, alive);
+        }
+    };
+    if (mb0 + wave * 32 < nq) all_steps(StageC<1>{});
+    else all_steps(StageC<0>{});
     const int last = (n_tiles - 1) & 1;
     rescale();
 #pragma unroll
