@@ -40,6 +40,7 @@ struct Plan {
     int blocks;             // blocks of 128 query rows over all K/V heads at most: the workgroups of paged_attn_wide without slices
     bool split;             // whether a sequence can have several slices
     int cap;                // slices of the whole batch at most
+    int spread;             // log2 of the XCDs that the query groups of one (slice, K/V head) are on
     SlicePlan slices;
 };
 
@@ -60,7 +61,7 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     const int tiles = ceil_div(max_rows > 0 ? max_rows * G : 1, 16), key_tiles = ceil_div(c.max_pages << c.page_shift, PKT);
     p.nq = dtype == DKV_BF16 && tiles > 1 ? 2 : 1;
     p.q_groups = ceil_div(tiles, p.nq);
-    int64_t whole = (int64_t)c.n_kv_heads * p.q_groups;             // workgroups of one slice for each sequence: batch times this
+    const int64_t whole = (int64_t)c.n_kv_heads * p.q_groups;             // workgroups of one slice for each sequence: batch times this
     // Blocks of 128 query rows (paged_wide.h) where tiles of 32 would make more than one round of workgroups: 28/4 heads, 1024 keys, 1
     // sequence of 300 rows (264 workgroups) 42 -> 22 us, 4 of 128 rows (448) 30 -> 23, but 4 of 64 rows (224) 16 -> 22 and 16 of 16
     // rows (256) 18 -> 25. Also where the keys are so many that slices of them keep the compute units busy without those
@@ -81,16 +82,26 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
         p.wide = p.blocks <= 320 && key_tiles > 16 ? 2 : 1;
         p.nq = 8;
         p.q_groups = ceil_div(tiles, p.nq);
-        whole = (int64_t)c.n_kv_heads * p.q_groups;
         least = kLeastWide;
         share = 2;
         p.split = p.wide == 2 && keys >= 4096;
     }
-    // Slices of a K/V head, all sequences together. The workgroups of one slice are on one XCD, and so many to an XCD that all run at once
-    // (28/4 heads, 32 rows, 8192 keys: 7 workgroups to a slice; 9 slices are 35 workgroups to some XCDs and 29.6 us, 8 are 28 and 20.8).
-    const int on_xcd = kWorkgroups / 8 / p.q_groups;
-    const int want = on_xcd ? on_xcd * 8 / c.n_kv_heads : (int)(kWorkgroups / whole);
+    // Query groups on one XCD or several (see GroupMap): whatever allows most slices of a K/V head (all sequences together), with all workgroups
+    // running at once, 32 to an XCD (28/4 heads, 32 rows, 8192 keys: 7 groups; 9 slices with 35 workgroups on some XCDs 29.6 us, 8 slices
+    // with 28 on each 20.5; 300 rows, 16384 keys: 17 blocks, 2 slices on one XCD each 140 us, 3 on two each 105), and without slices
+    // the fewest rounds (one K/V head, 33 groups of 6 sequences of 1006 keys: 6 XCDs 29 us, 8 XCDs 15.6; 150 groups of one of 1000 keys 67 and 15.7).
+    const int on_xcd = kWorkgroups / 8;
+    auto groups_of_part = [&](int shift) { return ceil_div(p.q_groups, 1 << shift); };
+    int want = 0, rounds = INT_MAX, spread_whole = 0;
+    p.spread = 0;
+    for (int shift = 0; shift <= 3; ++shift) {
+        const int slices = on_xcd / groups_of_part(shift) * 8 / (c.n_kv_heads << shift);
+        const int64_t fullest = (((int64_t)c.batch * c.n_kv_heads << shift) + 7) / 8 * groups_of_part(shift), r = (fullest + on_xcd - 1) / on_xcd;
+        if (slices > want) want = slices, p.spread = shift;
+        if (r < rounds) rounds = (int)r, spread_whole = shift;
+    }
     p.split = p.split && (share == 1 ? want > c.batch : want >= 2 * c.batch);
+    if (!p.split) p.spread = spread_whole;
     p.slices.split = p.split;
     p.slices.want = Divisor(p.split ? want : 1);
     p.slices.least = least;
@@ -104,7 +115,10 @@ size_t meta_bytes(const PagedCache &c) { return align_up(c.batch * sizeof(int2),
 size_t partial_bytes(const Plan &p, const PagedCache &c, int head_dim) {
     return p.split ? meta_bytes(c) + (size_t)p.cap * c.n_kv_heads * (p.q_groups * p.nq * 16) * (head_dim + 4) * sizeof(float) : 0;
 }
-unsigned split_grid(const Plan &p, const PagedCache &c) { return (unsigned)(ceil_div(p.cap * c.n_kv_heads, 8) * 8 * p.q_groups); }
+GroupMap group_map(const Plan &p) { return GroupMap{Divisor(ceil_div(p.q_groups, 1 << p.spread)), p.spread, p.q_groups * p.nq * 16}; }
+int64_t split_grid(const Plan &p, const PagedCache &c) {
+    return (((int64_t)p.cap * c.n_kv_heads << p.spread) + 7) / 8 * 8 * ceil_div(p.q_groups, 1 << p.spread);
+}
 
 template <typename T, int DH>
 int launch_merge(const PagedCache &c, const Plan &p, const int *row_off, void *out, void *part, int rows, int max_rows, int Hq, hipStream_t s) {
@@ -125,9 +139,9 @@ int launch_split(const PagedCache &c, const Plan &p, const void *q, int64_t q_st
         static std::atomic<uint64_t> devices{0};                                                                                 \
         const int rc = allow_lds(reinterpret_cast<const void *>(&paged_attn_split<T, C, DH, NQ, NW, ONCE>), smem, devices);      \
         if (rc) return rc;                                                                                                       \
-        hipLaunchKernelGGL((paged_attn_split<T, C, DH, NQ, NW, ONCE>), dim3(split_grid(p, c)), dim3(64 * NW), smem, s, c, p.slices, \
+        hipLaunchKernelGGL((paged_attn_split<T, C, DH, NQ, NW, ONCE>), dim3((unsigned)split_grid(p, c)), dim3(64 * NW), smem, s, c, p.slices, \
                            (const T *)q, q_stride, row_off, (T *)out, (int2 *)part, (float *)((char *)part + meta_bytes(c)), rows, max_rows, \
-                           Divisor(p.q_groups), Divisor(c.n_kv_heads), Divisor(Hq / c.n_kv_heads), scale_log2e);                \
+                           group_map(p), Divisor(c.n_kv_heads), Divisor(Hq / c.n_kv_heads), scale_log2e);                \
     } while (0)
     if (p.q_groups == 1) SPLIT(true);
     else SPLIT(false);
@@ -142,9 +156,9 @@ int launch_wide(const PagedCache &c, const Plan &p, const void *q, int64_t q_str
     static std::atomic<uint64_t> devices{0};
     const int rc = allow_lds(reinterpret_cast<const void *>(&paged_attn_wide<C, DH, KS>), KS * kWideLds<DH>, devices);
     if (rc) return rc;
-    hipLaunchKernelGGL((paged_attn_wide<C, DH, KS>), dim3(p.split ? split_grid(p, c) : (unsigned)p.blocks), dim3(256 * KS), KS * kWideLds<DH>, s, c,
+    hipLaunchKernelGGL((paged_attn_wide<C, DH, KS>), dim3((unsigned)(p.split ? split_grid(p, c) : p.blocks)), dim3(256 * KS), KS * kWideLds<DH>, s, c,
                        (const bf16_t *)q, q_stride, row_off, (bf16_t *)out, rows, (int2 *)part, (float *)((char *)part + meta_bytes(c)), p.slices,
-                       max_rows, Divisor(p.q_groups), Divisor(c.n_kv_heads), Divisor(Hq / c.n_kv_heads), kWorkgroups / c.n_kv_heads,
+                       max_rows, group_map(p), Divisor(c.n_kv_heads), Divisor(Hq / c.n_kv_heads), kWorkgroups / c.n_kv_heads,
                        1.4426950408889634f / sqrtf((float)DH));
     DKV_LAUNCH_CHECK();
     return p.split ? launch_merge<bf16_t, DH>(c, p, row_off, out, part, rows, max_rows, Hq, s) : DKV_OK;
@@ -183,7 +197,7 @@ int attn_call(const dkv_paged_cache *cache, PagedCache &view, Plan &plan, int32_
     if ((int64_t)rows * n_q_heads < 1 << 24 && (int64_t)cache->batch * cache->n_kv_heads < 1 << 22 &&
         (int64_t)cache->batch * cache->max_pages * cache->page_size <= 1ll << 35) {
         plan = make_plan(view, n_q_heads, rows, max_rows_per_seq, dtype, cache->head_dim);
-        if (plan.wide && !plan.split ? plan.blocks < 1 << 23 : (int64_t)plan.cap * cache->n_kv_heads * plan.q_groups < 1 << 22) return DKV_OK;
+        if (plan.wide && !plan.split ? plan.blocks < 1 << 23 : split_grid(plan, view) < 1 << 22) return DKV_OK;
     }
     dkv_set_error("%d rows of %d heads in %d sequences are too many for one call", rows, n_q_heads, cache->batch);
     return DKV_E_UNSUPPORTED;

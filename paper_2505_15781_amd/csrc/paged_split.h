@@ -31,6 +31,17 @@ struct SlicePlan {
     Divisor want;
     bool split;
 };
+// Workgroup id -> (slice, K/V head) and query group. The groups of one (slice, K/V head) read the same keys and are on one XCD (id mod 8),
+// or in 2^shift parts on as many, where one XCD would get more of them than run at once.
+struct GroupMap {
+    Divisor groups;                    // of a part
+    int shift, q_rows;                 // q_rows: rows of records for each (slice, K/V head)
+    __device__ __forceinline__ void find(int id, int &unit, int &group) const {
+        const int slot = id >> 3, at = groups.div(slot) * 8 + (id & 7);
+        unit = at >> shift;
+        group = (at & ((1 << shift) - 1)) * groups.d + groups.mod(slot);
+    }
+};
 struct Slices {
     int first, n;                      // slices of the sequences before, and of this one
     int b, r0, rows, keys;             // the sequence
@@ -168,7 +179,7 @@ __device__ __forceinline__ void softmax_step_f32(f32x4 (&st)[NT], float &m_run, 
 template <typename T, typename C, int DH, int NQ, int NW, bool ONCE>
 __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c, SlicePlan plan, const T *__restrict__ Q, int64_t q_stride,
                                                                     const int *__restrict__ row_off, T *__restrict__ out, int2 *__restrict__ meta,
-                                                                    float *__restrict__ part, int rows, int max_rows, Divisor groups, Divisor heads,
+                                                                    float *__restrict__ part, int rows, int max_rows, GroupMap map, Divisor heads,
                                                                     Divisor G, float scale_log2e) {
     using SM = SplitSmem<T, DH>;
     constexpr bool BF = sizeof(T) == 2;
@@ -178,8 +189,8 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     unsigned char *ksm = smem_raw + wave * SM::WAVE_BYTES, *vsm = ksm + SM::K_BYTES;
 
-    // the query groups of a (slice, K/V head) read the same keys: consecutive workgroups of one XCD (id mod 8)
-    const int slot = (int)(blockIdx.x >> 3), unit = groups.div(slot) * 8 + (int)(blockIdx.x & 7), qg = groups.mod(slot);
+    int unit, qg;
+    map.find((int)blockIdx.x, unit, qg);
     const int at = heads.div(unit), kvh = heads.mod(unit);
     // Pages of this wavefront's tiles t_begin + wave + NW j: lane i has half i & 1 of tile j0 + i / 2. The entry is read whatever the
     // length is, so that a plan without slices asks for it before it knows the length.
@@ -197,7 +208,6 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
     const int tiles = key_tiles(len, 1), per = plan.split ? uniform(ceil_div_fast(tiles, n_slices)) : tiles;
     const int t_begin = (at - first) * per, t_end = min(tiles, t_begin + per);
     if (plan.split && tid == 0 && at == first && kvh == 0 && qg == 0) meta[b] = make_int2(first, n_slices);
-    const int64_t q_rows = groups.d * (NQ * 16);
 
     // the page of such an entry; -1: none, or behind the end
     auto page_of = [&](int entry, int j0) { return first_key(t_begin, j0) < len && (unsigned)entry < (unsigned)c.n_pages ? entry : -1; };
@@ -388,7 +398,7 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
         if (n_slices == 1) {
             store_result(out + (((size_t)r * c.n_kv_heads + kvh) * G.d + G.mod(mq)) * DH + 4 * ch, o, lsum);
         } else {
-            float *rec = part + (unit * q_rows + mq) * REC;
+            float *rec = part + ((int64_t)unit * map.q_rows + mq) * REC;
             if (ch == 0) {
                 rec[0] = M;
                 rec[1] = lsum;

@@ -96,7 +96,7 @@ struct WideTile {
 template <typename C, int DH, int KS>
 __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, DH == 128 ? 2 : 4))) void paged_attn_wide(
     PagedCache c, const bf16_t *__restrict__ Q, int64_t q_stride, const int *__restrict__ row_off, bf16_t *__restrict__ out, int rows,
-    int2 *__restrict__ meta, float *__restrict__ partial, SlicePlan plan, int max_rows, Divisor blocks, Divisor heads, Divisor G, int units,
+    int2 *__restrict__ meta, float *__restrict__ partial, SlicePlan plan, int max_rows, GroupMap map, Divisor heads, Divisor G, int units,
     float scale_log2e) {
     constexpr int NW = 4, ROW = DH * 2, KT2 = 64, TILE = KT2 * ROW;     // bytes of an LDS row, of a K or V tile
     constexpr bool E4M3 = sizeof(C) == 1;
@@ -113,8 +113,9 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
     int parts = 1, t0 = 0, t1 = INT_MAX, slices = 1;
     int64_t record = 0;                              // first record of this (slice, K/V head)
     if (KS == 2 && plan.split) {                     // slices as in paged_attn_split, two groups to a block
-        const int slot = (int)(blockIdx.x >> 3), unit = blocks.div(slot) * 8 + (int)(blockIdx.x & 7), at = heads.div(unit);
-        item.qb = blocks.mod(slot);
+        int unit;
+        map.find((int)blockIdx.x, unit, item.qb);
+        const int at = heads.div(unit);
         item.kvh = heads.mod(unit);
         if (!find_slice(c, row_off, plan, at, item.seq)) return;
         slices = item.seq.n;
@@ -122,7 +123,7 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
         const int tiles = (key_tiles(item.seq.keys, 1) + 1) / 2, per = __builtin_amdgcn_readfirstlane(ceil_div_fast(tiles, slices));
         t0 = (at - item.seq.first) * per;
         t1 = t0 + per;
-        record = (int64_t)unit * (blocks.d * 128);
+        record = (int64_t)unit * map.q_rows;
         if (threadIdx.x == 0 && at == item.seq.first && item.kvh == 0 && item.qb == 0) meta[item.seq.b] = make_int2(item.seq.first, slices);
     } else {
         if (!wide_item<KS>(c, row_off, rows, max_rows, heads, G.d, units, item)) return;
