@@ -63,23 +63,28 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     p.q_groups = ceil_div(tiles, p.nq);
     const int64_t whole = (int64_t)c.n_kv_heads * p.q_groups;             // workgroups of one slice for each sequence: batch times this
     // Blocks of 128 query rows (paged_wide.h) where tiles of 32 would make more than one round of workgroups: 28/4 heads, 1024 keys, 1
-    // sequence of 300 rows (264 workgroups) 42 -> 22 us, 4 of 128 rows (448) 30 -> 23, but 4 of 64 rows (224) 16 -> 22 and 16 of 16
-    // rows (256) 18 -> 25. Also where the keys are so many that slices of them keep the compute units busy without those
-    // workgroups: 1536 keys each for tiles of 32 (28/4 heads, 1 sequence of 128 rows, 4096 keys 30.5 -> 27.2 us, 32768 keys 128 -> 82, but
-    // 32 rows, 4096 keys 16.5 -> 19.7, 8192 keys 20.8 -> 21.6), of more than 4096 keys of 128 dims (64 dims, 2 sequences of 128 rows: 4096 keys
-    // 25.1 -> 28.7, 8192 keys 43.6 -> 40.6). Two groups of wavefronts to a workgroup where the blocks are few and the
-    // keys many enough to share: 96 blocks of 1024 keys 24.8 -> 22.5 us, 384 blocks 41 -> 47, 128 blocks of 256 keys 11.8 -> 12.6.
+    // sequence of 300 rows (264 workgroups) 42 -> 22 us, 4 of 128 rows (448) 30 -> 23, but 4 of 64 rows (224) 16 -> 22. Also where the
+    // keys are so many that slices of them keep the compute units busy without those workgroups: 1536 keys each for tiles of 32 (28/4
+    // heads, 1 sequence of 128 rows, 4096 keys 30.5 -> 27.2 us, 32768 keys 128 -> 82, but 32 rows, 4096 keys 16.5 -> 19.7, 8192 keys 20.8 -> 21.6),
+    // of more than 4096 keys of 128 dims (64 dims, 2 sequences of 128 rows: 4096 keys 25.1 -> 28.7, 8192 keys 43.6 -> 40.6).
+    // More than 32 query rows to a sequence, which two of the four wavefronts work on (19 sequences of 700 keys, 32/32 heads, 40 rows 72 -> 57 us,
+    // 32/8 heads, 10 rows 27.6 -> 22.9); with 64 dims more than 64 (32/32 heads, 64 rows, 12 sequences of 8192 keys 160 -> 198, e4m3 156 -> 245).
+    // Two groups of wavefronts to a workgroup where the blocks are few and the keys many enough to share (96 blocks of 1024 keys 24.8 ->
+    // 22.5 us, 384 blocks 41 -> 47, 128 blocks of 256 keys 11.8 -> 12.6), and one round of workgroups holds them two by two (36 sequences
+    // of 700 keys, 32/8 heads, 32 rows: 288 blocks, each of a sequence of its own, 37.7 -> 54).
     // Their keys are cut from 4096 on, where every sequence can have two slices: 8 heads, 300 rows (80 blocks of 64 dims), 2048 keys
     // 27.2 us whole and 27.9 in slices, 4096 keys 47.6 and 34.3; at 128 dims, 2048 keys 36.2 and 34.4, 4096 keys 62.3 and 43.8.
     p.wide = p.blocks = 0;
     int least = kLeast, share = 1;
     p.split = key_tiles > whole_tiles(dtype, head_dim);
     const int64_t keys = (int64_t)key_tiles * PKT;
-    if (dtype == DKV_BF16 && head_dim >= 64 && max_rows * G > 64 &&
+    if (dtype == DKV_BF16 && head_dim >= 64 && max_rows * G > (head_dim == 128 ? 32 : 64) &&
         (c.batch * whole > kWorkgroups || (keys * head_dim >= 4096 * 128 && c.batch * whole * keys >= kWorkgroups * 1536))) {
         const int64_t blocks = c.batch + (int64_t)ceil_div(rows * G, 128), bound = (int64_t)c.batch * ceil_div(max_rows * G, 128);
         p.blocks = (int)((blocks < bound ? blocks : bound) * c.n_kv_heads);
-        p.wide = p.blocks <= 320 && key_tiles > 16 ? 2 : 1;
+        // workgroups if each takes two blocks of a sequence, by either bound
+        const int64_t pairs = (int64_t)c.batch * c.n_kv_heads * ceil_div(max_rows * G, 256), fewer = (p.blocks + (int64_t)c.batch * c.n_kv_heads) / 2;
+        p.wide = p.blocks <= 320 && (pairs < fewer ? pairs : fewer) <= kWorkgroups && key_tiles > 16 ? 2 : 1;
         p.nq = 8;
         p.q_groups = ceil_div(tiles, p.nq);
         least = kLeastWide;
@@ -94,7 +99,7 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     auto groups_of_part = [&](int shift) { return ceil_div(p.q_groups, 1 << shift); };
     int want = 0, rounds = INT_MAX, spread_whole = 0;
     p.spread = 0;
-    for (int shift = 0; shift <= 3; ++shift) {
+    for (int shift = 0; shift <= 3 && p.q_groups >> shift; ++shift) {
         const int slices = on_xcd / groups_of_part(shift) * 8 / (c.n_kv_heads << shift);
         const int64_t fullest = (((int64_t)c.batch * c.n_kv_heads << shift) + 7) / 8 * groups_of_part(shift), r = (fullest + on_xcd - 1) / on_xcd;
         if (slices > want) want = slices, p.spread = shift;
