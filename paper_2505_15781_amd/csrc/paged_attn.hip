@@ -54,16 +54,37 @@ constexpr int kWorkgroups = 256, kLeast = 4, kLeastWide = 16;
 // eighth of the rate): 128 dims, 8 tiles 13.3 and 11.8; 64 dims, 8 tiles 7.4 and 8.4, 16 tiles 12.1 and 8.5; 32 dims, 16 tiles 7.5 and 8.2, 24 9.7 and 8.5.
 int whole_tiles(int dtype, int head_dim) { return (dtype == DKV_BF16 ? 2304 : 640) / head_dim; }
 
+// Slices of one K/V head, all sequences together, that run at once: 32 workgroups on each XCD, `groups` query groups to a slice on 2^shift XCDs.
+int slices_at_once(int groups, int heads, int shift) { return kWorkgroups / 8 / ceil_div(groups, 1 << shift) * 8 / (heads << shift); }
+int best_spread(int groups, int heads) {
+    int best = 0;
+    for (int shift = 1; shift <= 3 && groups >> shift; ++shift)
+        if (slices_at_once(groups, heads, shift) > slices_at_once(groups, heads, best)) best = shift;
+    return best;
+}
+
 Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int dtype, int head_dim) {
     Plan p;
     max_rows = max_rows < rows ? max_rows : rows;
-    const int G = n_q_heads / c.n_kv_heads;
+    const int G = n_q_heads / c.n_kv_heads, heads = c.n_kv_heads;
     const int tiles = ceil_div(max_rows > 0 ? max_rows * G : 1, 16), key_tiles = ceil_div(c.max_pages << c.page_shift, PKT);
+    const int64_t keys = (int64_t)key_tiles * PKT;
+    // (sequence, K/V head, n query rows) at most: by the longest sequence's rows, or by the rows of all
+    auto blocks_of = [&](int n) {
+        const int64_t by_longest = (int64_t)c.batch * ceil_div(max_rows * G, n), by_all = c.batch + (int64_t)ceil_div(rows * G, n);
+        return (by_longest < by_all ? by_longest : by_all) * heads;
+    };
     p.nq = dtype == DKV_BF16 && tiles > 1 ? 2 : 1;
     p.q_groups = ceil_div(tiles, p.nq);
-    const int64_t whole = (int64_t)c.n_kv_heads * p.q_groups;             // workgroups of one slice for each sequence: batch times this
-    // Blocks of 128 query rows (paged_wide.h) where tiles of 32 would make more than one round of workgroups: 28/4 heads, 1024 keys, 1
-    // sequence of 300 rows (264 workgroups) 42 -> 22 us, 4 of 128 rows (448) 30 -> 23, but 4 of 64 rows (224) 16 -> 22. Also where the
+    p.wide = p.blocks = 0;
+    p.spread = best_spread(p.q_groups, heads);
+    p.slices.least = kLeast;
+    int want = slices_at_once(p.q_groups, heads, p.spread);
+    p.split = key_tiles > whole_tiles(dtype, head_dim) && want > c.batch;
+    // Blocks of 128 query rows (paged_wide.h) where tiles of 32 would make more than one round of workgroups (128 dims; 28/4 heads, 1024 keys: 1
+    // sequence of 300 rows, 264 workgroups, 42 -> 22 us, 4 of 128 rows, 448, 30 -> 23, but 4 of 64 rows, 224, 16 -> 22) or more than three (64
+    // dims, 32 heads, 8 sequences of 5600 keys: bf16, 80 rows, 768 workgroups, 60 -> 68, 128 rows, 1024, 81 -> 69, 250 rows, 122 -> 119; e4m3 65 ->
+    // 105, 93 -> 106, 146 -> 149, but with 700 keys 15.7 -> 18.6, 24.6 -> 19.4, 37.9 -> 22.6). Also where the
     // keys are so many that slices of them keep the compute units busy without those workgroups: 1536 keys each for tiles of 32 (28/4
     // heads, 1 sequence of 128 rows, 4096 keys 30.5 -> 27.2 us, 32768 keys 128 -> 82, but 32 rows, 4096 keys 16.5 -> 19.7, 8192 keys 20.8 -> 21.6),
     // of more than 4096 keys of 128 dims (64 dims, 2 sequences of 128 rows: 4096 keys 25.1 -> 28.7, 8192 keys 43.6 -> 40.6).
@@ -74,43 +95,40 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     // of 700 keys, 32/8 heads, 32 rows: 288 blocks, each of a sequence of its own, 37.7 -> 54).
     // Their keys are cut from 4096 on, where every sequence can have two slices: 8 heads, 300 rows (80 blocks of 64 dims), 2048 keys
     // 27.2 us whole and 27.9 in slices, 4096 keys 47.6 and 34.3; at 128 dims, 2048 keys 36.2 and 34.4, 4096 keys 62.3 and 43.8.
-    p.wide = p.blocks = 0;
-    int least = kLeast, share = 1;
-    p.split = key_tiles > whole_tiles(dtype, head_dim);
-    const int64_t keys = (int64_t)key_tiles * PKT;
-    if (dtype == DKV_BF16 && head_dim >= 64 && max_rows * G > (head_dim == 128 ? 32 : 64) &&
-        (c.batch * whole > kWorkgroups || (keys * head_dim >= 4096 * 128 && c.batch * whole * keys >= kWorkgroups * 1536))) {
-        const int64_t blocks = c.batch + (int64_t)ceil_div(rows * G, 128), bound = (int64_t)c.batch * ceil_div(max_rows * G, 128);
-        p.blocks = (int)((blocks < bound ? blocks : bound) * c.n_kv_heads);
-        // workgroups if each takes two blocks of a sequence, by either bound
-        const int64_t pairs = (int64_t)c.batch * c.n_kv_heads * ceil_div(max_rows * G, 256), fewer = (p.blocks + (int64_t)c.batch * c.n_kv_heads) / 2;
-        p.wide = p.blocks <= 320 && (pairs < fewer ? pairs : fewer) <= kWorkgroups && key_tiles > 16 ? 2 : 1;
-        p.nq = 8;
-        p.q_groups = ceil_div(tiles, p.nq);
-        least = kLeastWide;
-        share = 2;
-        p.split = p.wide == 2 && keys >= 4096;
+    // (In two rounds of slices, where one has no two for every sequence: 8 sequences of 5600 keys, 32 heads, 80 rows 119 -> 141.)
+    if (dtype == DKV_BF16 && head_dim >= 64 && max_rows * G > (head_dim == 128 ? 32 : 64)) {
+        const int64_t groups = blocks_of(32), blocks = blocks_of(128);
+        const int q_groups = ceil_div(tiles, 8), spread = best_spread(q_groups, heads), slices = slices_at_once(q_groups, heads, spread);
+        const int64_t two_by_two = (int64_t)c.batch * heads * ceil_div(max_rows * G, 256), other = (blocks + (int64_t)c.batch * heads) / 2;
+        const int wide = blocks <= 320 && (two_by_two < other ? two_by_two : other) <= kWorkgroups && key_tiles > 16 ? 2 : 1;
+        const bool cut = wide == 2 && keys >= 4096 && slices >= 2 * c.batch;
+        if (groups > (head_dim == 128 ? kWorkgroups : 3 * kWorkgroups) || (cut && keys * head_dim >= 4096 * 128 && groups * keys >= kWorkgroups * 1536)) {
+            p.wide = wide;
+            p.blocks = (int)blocks;
+            p.nq = 8;
+            p.q_groups = q_groups;
+            p.spread = spread;
+            p.slices.least = kLeastWide;
+            want = slices;
+            p.split = cut;
+        }
     }
     // Query groups on one XCD or several (see GroupMap): whatever allows most slices of a K/V head (all sequences together), with all workgroups
     // running at once, 32 to an XCD (28/4 heads, 32 rows, 8192 keys: 7 groups; 9 slices with 35 workgroups on some XCDs 29.6 us, 8 slices
     // with 28 on each 20.5; 300 rows, 16384 keys: 17 blocks, 2 slices on one XCD each 140 us, 3 on two each 105), and without slices
     // the fewest rounds (one K/V head, 33 groups of 6 sequences of 1006 keys: 6 XCDs 29 us, 8 XCDs 15.6; 150 groups of one of 1000 keys 67 and 15.7).
-    const int on_xcd = kWorkgroups / 8;
-    auto groups_of_part = [&](int shift) { return ceil_div(p.q_groups, 1 << shift); };
-    int want = 0, rounds = INT_MAX, spread_whole = 0;
-    p.spread = 0;
-    for (int shift = 0; shift <= 3 && p.q_groups >> shift; ++shift) {
-        const int slices = on_xcd / groups_of_part(shift) * 8 / (c.n_kv_heads << shift);
-        const int64_t fullest = (((int64_t)c.batch * c.n_kv_heads << shift) + 7) / 8 * groups_of_part(shift), r = (fullest + on_xcd - 1) / on_xcd;
-        if (slices > want) want = slices, p.spread = shift;
-        if (r < rounds) rounds = (int)r, spread_whole = shift;
+    if (!p.split) {
+        auto rounds = [&](int shift) {
+            const int64_t fullest = (((int64_t)c.batch * heads << shift) + 7) / 8 * ceil_div(p.q_groups, 1 << shift);
+            return (fullest + kWorkgroups / 8 - 1) / (kWorkgroups / 8);
+        };
+        p.spread = 0;
+        for (int shift = 1; shift <= 3 && p.q_groups >> shift; ++shift)
+            if (rounds(shift) < rounds(p.spread)) p.spread = shift;
     }
-    p.split = p.split && (share == 1 ? want > c.batch : want >= 2 * c.batch);
-    if (!p.split) p.spread = spread_whole;
     p.slices.split = p.split;
     p.slices.want = Divisor(p.split ? want : 1);
-    p.slices.least = least;
-    const int64_t most = (int64_t)c.batch * ceil_div(key_tiles, least);
+    const int64_t most = (int64_t)c.batch * ceil_div(key_tiles, p.slices.least);
     p.cap = !p.split ? c.batch : (int)(most < want ? most : want);      // see slice_length
     return p;
 }
