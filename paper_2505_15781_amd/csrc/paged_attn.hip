@@ -54,12 +54,13 @@ constexpr int kWorkgroups = 256, kLeast = 4, kLeastWide = 16;
 // eighth of the rate): 128 dims, 8 tiles 13.3 and 11.8; 64 dims, 8 tiles 7.4 and 8.4, 16 tiles 12.1 and 8.5; 32 dims, 16 tiles 7.5 and 8.2, 24 9.7 and 8.5.
 int whole_tiles(int dtype, int head_dim) { return (dtype == DKV_BF16 ? 2304 : 640) / head_dim; }
 
-// Slices of one K/V head, all sequences together, that run at once: 32 workgroups on each XCD, `groups` query groups to a slice on 2^shift XCDs.
-int slices_at_once(int groups, int heads, int shift) { return kWorkgroups / 8 / ceil_div(groups, 1 << shift) * 8 / (heads << shift); }
-int best_spread(int groups, int heads) {
+// Slices of one K/V head, all sequences together, that run at once: `per_cu` workgroups to a compute unit, `groups` query groups to a slice on
+// 2^shift XCDs.
+int slices_at_once(int groups, int heads, int shift, int per_cu) { return per_cu * (kWorkgroups / 8) / ceil_div(groups, 1 << shift) * 8 / (heads << shift); }
+int best_spread(int groups, int heads, int per_cu) {
     int best = 0;
     for (int shift = 1; shift <= 3 && groups >> shift; ++shift)
-        if (slices_at_once(groups, heads, shift) > slices_at_once(groups, heads, best)) best = shift;
+        if (slices_at_once(groups, heads, shift, per_cu) > slices_at_once(groups, heads, best, per_cu)) best = shift;
     return best;
 }
 
@@ -77,9 +78,9 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     p.nq = dtype == DKV_BF16 && tiles > 1 ? 2 : 1;
     p.q_groups = ceil_div(tiles, p.nq);
     p.wide = p.blocks = 0;
-    p.spread = best_spread(p.q_groups, heads);
+    p.spread = best_spread(p.q_groups, heads, 1);
     p.slices.least = kLeast;
-    int want = slices_at_once(p.q_groups, heads, p.spread);
+    int want = slices_at_once(p.q_groups, heads, p.spread, 1);
     p.split = key_tiles > whole_tiles(dtype, head_dim) && want > c.batch;
     // Blocks of 128 query rows (paged_wide.h) where tiles of 32 would make more than one round of workgroups (128 dims; 28/4 heads, 1024 keys: 1
     // sequence of 300 rows, 264 workgroups, 42 -> 22 us, 4 of 128 rows, 448, 30 -> 23, but 4 of 64 rows, 224, 16 -> 22) or more than three (64
@@ -95,13 +96,18 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     // of 700 keys, 32/8 heads, 32 rows: 288 blocks, each of a sequence of its own, 37.7 -> 54).
     // Their keys are cut from 4096 on, where every sequence can have two slices: 8 heads, 300 rows (80 blocks of 64 dims), 2048 keys
     // 27.2 us whole and 27.9 in slices, 4096 keys 47.6 and 34.3; at 128 dims, 2048 keys 36.2 and 34.4, 4096 keys 62.3 and 43.8.
+    // Slices of heads of 64 have one group of wavefronts, and three workgroups a compute unit, which hold more loads on their way than one of
+    // two groups (28/4 heads, 130 rows, 100000 keys: e4m3 214 -> 167 us, bf16 155 -> 151; 32/32 heads, 80 rows, 2 sequences of 31000
+    // 152 -> 123 and 116 -> 113; the other way 28/4 heads, 17 rows of 2 sequences of 31000 31.1 -> 32.8 and 28.4 -> 28.8).
     // (In two rounds of slices, where one has no two for every sequence: 8 sequences of 5600 keys, 32 heads, 80 rows 119 -> 141.)
     if (dtype == DKV_BF16 && head_dim >= 64 && max_rows * G > (head_dim == 128 ? 32 : 64)) {
         const int64_t groups = blocks_of(32), blocks = blocks_of(128);
-        const int q_groups = ceil_div(tiles, 8), spread = best_spread(q_groups, heads), slices = slices_at_once(q_groups, heads, spread);
+        const int per_cu = head_dim == 64 ? 3 : 1, q_groups = ceil_div(tiles, 8), spread = best_spread(q_groups, heads, per_cu);
+        const int slices = slices_at_once(q_groups, heads, spread, per_cu);
         const int64_t two_by_two = (int64_t)c.batch * heads * ceil_div(max_rows * G, 256), other = (blocks + (int64_t)c.batch * heads) / 2;
-        const int wide = blocks <= 320 && (two_by_two < other ? two_by_two : other) <= kWorkgroups && key_tiles > 16 ? 2 : 1;
-        const bool cut = wide == 2 && keys >= 4096 && slices >= 2 * c.batch;
+        int wide = blocks <= 320 && (two_by_two < other ? two_by_two : other) <= kWorkgroups && key_tiles > 16 ? 2 : 1;
+        const bool cut = (wide == 2 || head_dim == 64) && keys >= 4096 && slices >= 2 * c.batch;
+        if (cut && head_dim == 64) wide = 1;
         if (groups > (head_dim == 128 ? kWorkgroups : 3 * kWorkgroups) || (cut && keys * head_dim >= 4096 * 128 && groups * keys >= kWorkgroups * 1536)) {
             p.wide = wide;
             p.blocks = (int)blocks;

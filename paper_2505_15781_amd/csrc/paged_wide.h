@@ -112,14 +112,15 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
     WideItem item;
     int parts = 1, t0 = 0, t1 = INT_MAX, slices = 1;
     int64_t record = 0;                              // first record of this (slice, K/V head)
-    if (KS == 2 && plan.split) {                     // slices as in paged_attn_split, two groups to a block
+    constexpr bool CUT = (KS == 2) == (DH == 128);   // whether there are plans with slices
+    if (CUT && plan.split) {                     // slices as in paged_attn_split, all groups on one block
         int unit;
         map.find((int)blockIdx.x, unit, item.qb);
         const int at = heads.div(unit);
         item.kvh = heads.mod(unit);
         if (!find_slice(c, row_off, plan, at, item.seq)) return;
         slices = item.seq.n;
-        parts = 2;
+        parts = KS;
         const int tiles = (key_tiles(item.seq.keys, 1) + 1) / 2, per = __builtin_amdgcn_readfirstlane(ceil_div_fast(tiles, slices));
         t0 = (at - item.seq.first) * per;
         t1 = t0 + per;
@@ -132,13 +133,13 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
     // all of it the same in every lane, which the compiler does not see behind the two ways to an item
     auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
     parts = KS == 1 ? 1 : uniform(parts);
-    t0 = KS == 1 ? 0 : uniform(t0);
+    t0 = CUT ? uniform(t0) : 0;
     const int part = parts == 1 ? 0 : group_id, b = uniform(item.seq.b), r0 = uniform(item.seq.r0), kvh = uniform(item.kvh);
-    const int keys = uniform(item.seq.keys), tiles = (keys + KT2 - 1) / KT2, end = KS == 1 ? tiles : uniform(min(tiles, t1));
+    const int keys = uniform(item.seq.keys), tiles = (keys + KT2 - 1) / KT2, end = CUT ? uniform(min(tiles, t1)) : tiles;
     const int L = end < tiles ? end * KT2 : keys;                     // keys from here on are another slice's, or none
     const int n_tiles = (max(1, end - t0) + parts - 1) / parts;
     const int nq = uniform(min(item.seq.rows, max_rows)) * G.d, mb0 = (uniform(item.qb) + (parts == 1 ? group_id : 0)) * NW * 32;
-    if (KS == 2 && mb0 >= nq && parts == 2) return;                   // uniform for the workgroup
+    if (CUT && mb0 >= nq && parts == KS) return;                      // uniform for the workgroup
 
     // this lane's query row; rows beyond the host's bound have no slot in Q and out
     const int mq = mb0 + wave * 32 + qi, r = r0 + G.div(mq), h = kvh * G.d + G.mod(mq);
@@ -445,7 +446,7 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
         }
     }
     if (!q_ok) return;
-    if (KS == 2 && slices > 1) {                     // a record for paged_merge: m, l, -, -, o[DH]
+    if (CUT && slices > 1) {                     // a record for paged_merge: m, l, -, -, o[DH]
         float *rec = partial + (record + mq) * (DH + 4);
         if (g == 0) {
             rec[0] = m_run;
