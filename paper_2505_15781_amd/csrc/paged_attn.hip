@@ -94,8 +94,9 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     // Two groups of wavefronts to a workgroup where the blocks are few and the keys many enough to share (96 blocks of 1024 keys 24.8 ->
     // 22.5 us, 384 blocks 41 -> 47, 128 blocks of 256 keys 11.8 -> 12.6), and one round of workgroups holds them two by two (36 sequences
     // of 700 keys, 32/8 heads, 32 rows: 288 blocks, each of a sequence of its own, 37.7 -> 54).
-    // Their keys are cut from 4096 on, where every sequence can have two slices: 8 heads, 300 rows (80 blocks of 64 dims), 2048 keys
-    // 27.2 us whole and 27.9 in slices, 4096 keys 47.6 and 34.3; at 128 dims, 2048 keys 36.2 and 34.4, 4096 keys 62.3 and 43.8.
+    // Their keys are cut where every sequence can have two slices, from 2048 keys of 128 dims on (32/8 heads, 300 rows, 80 blocks: 1300 keys
+    // 28.7 us whole and 32.6 in slices, 2700 keys 47.8 and 40.2; 28/4 heads, 4 ragged sequences of 130 rows and 2000 keys at most 37.4 and 33.1),
+    // from 4096 of 64 dims (32/32 heads, 4 sequences of 300 rows, 2700 keys 69 and 85; 28/4 heads 77 and 80, 3500 keys 95 and 90).
     // Slices of heads of 64 have one group of wavefronts, and three workgroups a compute unit, which hold more loads on their way than one of
     // two groups (28/4 heads, 130 rows, 100000 keys: e4m3 214 -> 167 us, bf16 155 -> 151; 32/32 heads, 80 rows, 2 sequences of 31000
     // 152 -> 123 and 116 -> 113; the other way 28/4 heads, 17 rows of 2 sequences of 31000 31.1 -> 32.8 and 28.4 -> 28.8).
@@ -106,7 +107,7 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
         const int slices = slices_at_once(q_groups, heads, spread, per_cu);
         const int64_t two_by_two = (int64_t)c.batch * heads * ceil_div(max_rows * G, 256), other = (blocks + (int64_t)c.batch * heads) / 2;
         int wide = blocks <= 320 && (two_by_two < other ? two_by_two : other) <= kWorkgroups && key_tiles > 16 ? 2 : 1;
-        const bool cut = (wide == 2 || head_dim == 64) && keys >= 4096 && slices >= 2 * c.batch;
+        const bool cut = (wide == 2 || head_dim == 64) && keys >= (head_dim == 64 ? 4096 : 2048) && slices >= 2 * c.batch;
         if (cut && head_dim == 64) wide = 1;
         if (groups > (head_dim == 128 ? kWorkgroups : 3 * kWorkgroups) || (cut && keys * head_dim >= 4096 * 128 && groups * keys >= kWorkgroups * 1536)) {
             p.wide = wide;
