@@ -39,7 +39,7 @@ __device__ __align__(256) const u32x4 zero_row[16] = {};
 // heads go fastest: the blocks of a head, which read the same keys, are on one XCD (id % 8) with 8 heads, on two with 4.
 // With two groups of wavefronts a workgroup takes one block of a long sequence, a group each half of its key tiles (parts = 2), or two
 // blocks of a short one, a group each: as many sequences are long as `units` workgroups (one per compute unit) have room for.
-// (Where blocks are so few that compute units would be idle, the keys are cut into slices as for paged_attn_split instead.)
+// (Where blocks are so few that compute units would be idle and the keys many, these are cut into slices as for paged_attn_split instead.)
 struct WideItem {
     Slices seq;
     int kvh, qb, parts;                // qb: the first block
