@@ -285,7 +285,7 @@ int dkv_concat_reorder(const void *k_cached, const void *v_cached, const void *k
  *   seq_len (dev) [batch] positions of each sequence (attention only; taken as 0 below 0, as max_pages * page_size above)
  * page_size: a power of two, 16 to 65536; max_pages * page_size at most 2^30, n_pages * n_kv_heads * page_size at most 2^32; head_dim 32, 64 or 128; dtype DKV_BF16, DKV_FP32 or
  * DKV_E4M3. Nothing in the structure is kept by a call; the structure itself is host memory. Table, lengths, positions
- * and row offsets are read on the device, so a captured call follows them. */
+ * and row offsets are read on the device, so a captured call follows them. The current device is that of the cache and the stream. */
 typedef struct {
     void *k_pages, *v_pages;
     uint8_t *k_scale, *v_scale;
@@ -322,6 +322,8 @@ int dkv_paged_load(const dkv_paged_cache *cache, void *k_out, void *v_out, const
  *   row_off as above; max_rows_per_seq (host) bounds the rows of any one sequence (rows of a sequence beyond it are left out)
  *   workspace (dev), 16-byte aligned, of dkv_paged_attn_workspace_bytes for the same cache, heads, rows and bound; calls that may
  *     overlap need one each
+ * out overlaps none of the inputs. Results are finite where 2^8 times the sum of the magnitudes of V over a sequence's keys is below 2^128 (the
+ * sums are divided last).
  * Rows from min(rows, row_off[batch]) on are left as they are. dtype DKV_BF16 reads DKV_BF16 and DKV_E4M3 caches (products of bf16
  * operands, probabilities among them, sums in fp32; e4m3 elements with their scales are exact in bf16); DKV_FP32 reads
  * DKV_FP32 and DKV_E4M3 caches, in fp32 throughout. */

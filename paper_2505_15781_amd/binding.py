@@ -390,7 +390,8 @@ def paged_attn_workspace_bytes(cache, n_q_heads, rows, max_rows_per_seq, dtype=B
 
 def paged_attn(cache, q, row_off, out, max_rows_per_seq, workspace):
     """Attention of the rows of q [rows, n_q_heads, head_dim] over all positions of their sequences (below seq_len, on a
-    page) into `out`; row_off as in paged_store (None: one row per sequence)."""
+    page) into `out`; row_off as in paged_store (None: one row per sequence). max_rows_per_seq bounds the rows of any one
+    sequence; workspace: a tensor of paged_attn_workspace_bytes bytes, one for each call that may overlap."""
     _check(_marshal.paged_attn(cache, q, row_off, out, max_rows_per_seq, workspace))
 
 
