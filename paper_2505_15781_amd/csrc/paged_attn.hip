@@ -100,14 +100,19 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     // Slices of heads of 64 have one group of wavefronts, and three workgroups a compute unit, which hold more loads on their way than one of
     // two groups (28/4 heads, 130 rows, 100000 keys: e4m3 214 -> 167 us, bf16 155 -> 151; 32/32 heads, 80 rows, 2 sequences of 31000
     // 152 -> 123 and 116 -> 113; the other way 28/4 heads, 17 rows of 2 sequences of 31000 31.1 -> 32.8 and 28.4 -> 28.8).
-    // (In two rounds of slices, where one has no two for every sequence: 8 sequences of 5600 keys, 32 heads, 80 rows 119 -> 141.)
+    // With fewer slices the long sequences of a ragged batch are cut all the same: the host knows the rows, and takes it that keys go with
+    // them (28/4 heads, 8 sequences of up to 9000 keys and 80 rows, 12 slices 146 -> 91 us; 14 of up to 2100, 37 rows, 20 slices 40 -> 35.7; but
+    // 30 of up to 3000, 20 rows, 32 slices 57.5 -> 60.6). In two rounds of slices batches of one length lose (8 sequences of 5600 keys, 32 heads, 80
+    // rows 119 -> 141).
     if (dtype == DKV_BF16 && head_dim >= 64 && max_rows * G > (head_dim == 128 ? 32 : 64)) {
         const int64_t groups = blocks_of(32), blocks = blocks_of(128);
         const int per_cu = head_dim == 64 ? 3 : 1, q_groups = ceil_div(tiles, 8), spread = best_spread(q_groups, heads, per_cu);
         const int slices = slices_at_once(q_groups, heads, spread, per_cu);
         const int64_t two_by_two = (int64_t)c.batch * heads * ceil_div(max_rows * G, 256), other = (blocks + (int64_t)c.batch * heads) / 2;
         int wide = blocks <= 320 && (two_by_two < other ? two_by_two : other) <= kWorkgroups && key_tiles > 16 ? 2 : 1;
-        const bool cut = (wide == 2 || head_dim == 64) && keys >= (head_dim == 64 ? 4096 : 2048) && slices >= 2 * c.batch;
+        const bool ragged = 4 * (int64_t)rows <= 3 * (int64_t)c.batch * max_rows;
+        const bool cut = (wide == 2 || head_dim == 64) && keys >= (head_dim == 64 ? 4096 : 2048) &&
+                         (slices >= 2 * c.batch || (ragged && 4 * slices >= 5 * c.batch));
         if (cut && head_dim == 64) wide = 1;
         if (groups > (head_dim == 128 ? kWorkgroups : 3 * kWorkgroups) || (cut && keys * head_dim >= 4096 * 128 && groups * keys >= kWorkgroups * 1536)) {
             p.wide = wide;

@@ -187,7 +187,8 @@ ATTN = [  # lens, rows, page, kv heads, group, dh
     ([4500, 40, 2100], [100, 70, 129], 32, 2, 4, 128), ([9000, 0, 2081], [50, 257, 130], 64, 1, 4, 64), ([5000, 2081], [150, 257], 64, 8, 4, 64),
     ([1006, 900], [65, 64], 16, 1, 16, 128), ([4500, 3000], [32, 30], 16, 1, 12, 128), ([8230], [96], 16, 1, 16, 128),
     ([700, 90, 130, 64, 33, 600, 5], [40, 64, 33, 35, 1, 7, 62], 16, 24, 1, 128), ([800, 100, 500], [300, 17, 140], 32, 1, 16, 64),
-    ([6500, 40, 2100], [100, 70, 129], 32, 2, 4, 128), ([5000, 0, 4100], [257, 80, 300], 16, 4, 4, 64)]
+    ([6500, 40, 2100], [100, 70, 129], 32, 2, 4, 128), ([5000, 0, 4100], [257, 80, 300], 16, 4, 4, 64),
+    ([4200, 1, 1500, 64, 700, 0, 33], [75, 3, 40, 9, 20, 2, 1], 16, 8, 4, 128)]
 
 
 @pytest.mark.parametrize("types", ["bf16 bf16", "bf16 e4m3", "fp32 fp32", "fp32 e4m3"])
