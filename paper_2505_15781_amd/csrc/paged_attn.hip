@@ -47,7 +47,8 @@ struct Plan {
 // One workgroup of paged_attn_split holds a compute unit (its LDS): slices make up to that many, a second round costs what the first does
 // (two sequences of 131072 keys: 56 us with 256 workgroups, 67 with 512). A slice has 4 tiles of keys at least: what a compute unit
 // reads is bound to some 50 GB/s, so idle units cost more than wavefronts without a tile (28/4 heads, 4 sequences of 2000 keys in
-// bf16: 10.5 us with 4 tiles, 11.4 with 8, 17.2 with 32, 22.3 without slices).
+// bf16: 10.5 us with 4 tiles, 11.4 with 8, 17.2 with 32, 22.3 without slices). paged_attn_wide, whose groups take 64 keys at a time: 16
+// tiles of 32 (28/4 heads, 64 rows, 4096 keys 23.1 us with 8, 21.9 with 16, 26.7 with 32; 16384 keys 36.8, 35.4, 35.3).
 constexpr int kWorkgroups = 256, kLeast = 4, kLeastWide = 16;
 // Key tiles up to which a sequence stays whole: the launch that joins slices costs some 2 us. bf16, 128 dims: 16 tiles 8.6 us whole and 9.0
 // in slices, 24 tiles 11.5 and 9.3; 64 dims: 24 tiles 7.3 and 8.1, 47 tiles 10.8 and 9.0. fp32 (four wavefronts, matrix instructions of an
