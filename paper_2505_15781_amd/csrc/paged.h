@@ -109,3 +109,17 @@ __device__ __forceinline__ void store8(bf16_t *p, f32x8 x) {
 int dkv_paged_view(const dkv_paged_cache *cache, PagedCache &view);
 // Rows and row offsets as the entry points take them; `rows` > 0 on success says that there is work.
 int dkv_paged_check_rows(const dkv_paged_cache &cache, const int32_t *row_off, int32_t rows);
+
+// What a call of attention is routed to.
+struct PagedAttnPlan {
+    int nq, q_groups;       // query tiles of 16 rows per workgroup, groups of them
+    int wide;               // 0: paged_attn_split; paged_attn_wide: groups of wavefronts in a workgroup
+    int blocks;             // blocks of 128 query rows over all K/V heads at most: the workgroups of paged_attn_wide without slices
+    int cap;                // slices of the whole batch at most
+    int spread;             // log2 of the XCDs that the query groups of one (slice, K/V head) are on
+    int least, want;        // see SlicePlan
+    bool split;             // whether a sequence can have several slices
+};
+// What both entry points of the attention refuse, and the plan of what they do not.
+int dkv_paged_attn_plan(const dkv_paged_cache *cache, PagedCache &view, PagedAttnPlan &plan, int n_q_heads, int rows, int max_rows_per_seq,
+                        int dtype);

@@ -1,4 +1,4 @@
-// Attention of new rows over a paged K/V cache: plans and boundary (kernels in paged_split.h).
+// Attention of new rows over a paged K/V cache: plans and boundary (kernels in paged_split.h and paged_wide.h).
 #include <math.h>
 
 #include <atomic>
@@ -34,15 +34,7 @@ int allow_lds(const void *kernel, int bytes, std::atomic<uint64_t> &devices) {
     return DKV_OK;
 }
 
-struct Plan {
-    int nq, q_groups;       // query tiles of 16 rows per workgroup, groups of them
-    int wide;               // 0: paged_attn_split; paged_attn_wide: groups of wavefronts in a workgroup
-    int blocks;             // blocks of 128 query rows over all K/V heads at most: the workgroups of paged_attn_wide without slices
-    bool split;             // whether a sequence can have several slices
-    int cap;                // slices of the whole batch at most
-    int spread;             // log2 of the XCDs that the query groups of one (slice, K/V head) are on
-    SlicePlan slices;
-};
+typedef PagedAttnPlan Plan;
 
 // One workgroup of paged_attn_split holds a compute unit (its LDS): slices make up to that many, a second round costs what the first does
 // (two sequences of 131072 keys: 56 us with 256 workgroups, 67 with 512). A slice has 4 tiles of keys at least: what a compute unit
@@ -80,7 +72,7 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     p.q_groups = ceil_div(tiles, p.nq);
     p.wide = p.blocks = 0;
     p.spread = best_spread(p.q_groups, heads, 1);
-    p.slices.least = kLeast;
+    p.least = kLeast;
     int want = slices_at_once(p.q_groups, heads, p.spread, 1);
     p.split = key_tiles > whole_tiles(dtype, head_dim) && want > c.batch;
     // Blocks of 128 query rows (paged_wide.h) where tiles of 32 would make more than one round of workgroups (128 dims; 28/4 heads, 1024 keys: 1
@@ -121,7 +113,7 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
             p.nq = 8;
             p.q_groups = q_groups;
             p.spread = spread;
-            p.slices.least = kLeastWide;
+            p.least = kLeastWide;
             want = slices;
             p.split = cut;
         }
@@ -143,9 +135,8 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
         if (rounds(p.spread) > 1)
             while (((int64_t)c.batch * heads << p.spread) < kWorkgroups / 8 && p.spread < 3 && p.q_groups >> (p.spread + 1)) ++p.spread;
     }
-    p.slices.split = p.split;
-    p.slices.want = Divisor(p.split ? want : 1);
-    const int64_t most = (int64_t)c.batch * ceil_div(key_tiles, p.slices.least);
+    p.want = p.split ? want : 1;
+    const int64_t most = (int64_t)c.batch * ceil_div(key_tiles, p.least);
     p.cap = !p.split ? c.batch : (int)(most < want ? most : want);      // see slice_length
     return p;
 }
@@ -155,6 +146,7 @@ size_t meta_bytes(const PagedCache &c) { return align_up(c.batch * sizeof(int2),
 size_t partial_bytes(const Plan &p, const PagedCache &c, int head_dim) {
     return p.split ? meta_bytes(c) + (size_t)p.cap * c.n_kv_heads * (p.q_groups * p.nq * 16) * (head_dim + 4) * sizeof(float) : 0;
 }
+SlicePlan slice_plan(const Plan &p) { return SlicePlan{p.least, Divisor(p.want), p.split}; }
 GroupMap group_map(const Plan &p) { return GroupMap{Divisor(ceil_div(p.q_groups, 1 << p.spread)), p.spread, p.q_groups * p.nq * 16}; }
 int64_t split_grid(const Plan &p, const PagedCache &c) {
     return (((int64_t)p.cap * c.n_kv_heads << p.spread) + 7) / 8 * 8 * ceil_div(p.q_groups, 1 << p.spread);
@@ -179,7 +171,7 @@ int launch_split(const PagedCache &c, const Plan &p, const void *q, int64_t q_st
         static std::atomic<uint64_t> devices{0};                                                                                 \
         const int rc = allow_lds(reinterpret_cast<const void *>(&paged_attn_split<T, C, DH, NQ, NW, ONCE>), smem, devices);      \
         if (rc) return rc;                                                                                                       \
-        hipLaunchKernelGGL((paged_attn_split<T, C, DH, NQ, NW, ONCE>), dim3((unsigned)split_grid(p, c)), dim3(64 * NW), smem, s, c, p.slices, \
+        hipLaunchKernelGGL((paged_attn_split<T, C, DH, NQ, NW, ONCE>), dim3((unsigned)split_grid(p, c)), dim3(64 * NW), smem, s, c, slice_plan(p), \
                            (const T *)q, q_stride, row_off, (T *)out, (int2 *)part, (float *)((char *)part + meta_bytes(c)), rows, max_rows, \
                            group_map(p), Divisor(c.n_kv_heads), Divisor(Hq / c.n_kv_heads), scale_log2e);                \
     } while (0)
@@ -197,7 +189,7 @@ int launch_wide(const PagedCache &c, const Plan &p, const void *q, int64_t q_str
     const int rc = allow_lds(reinterpret_cast<const void *>(&paged_attn_wide<C, DH, KS>), KS * kWideLds<DH>, devices);
     if (rc) return rc;
     hipLaunchKernelGGL((paged_attn_wide<C, DH, KS>), dim3((unsigned)(p.split ? split_grid(p, c) : p.blocks)), dim3(256 * KS), KS * kWideLds<DH>, s, c,
-                       (const bf16_t *)q, q_stride, row_off, (bf16_t *)out, rows, (int2 *)part, (float *)((char *)part + meta_bytes(c)), p.slices,
+                       (const bf16_t *)q, q_stride, row_off, (bf16_t *)out, rows, (int2 *)part, (float *)((char *)part + meta_bytes(c)), slice_plan(p),
                        max_rows, group_map(p), Divisor(c.n_kv_heads), Divisor(Hq / c.n_kv_heads), kWorkgroups / c.n_kv_heads,
                        1.4426950408889634f / sqrtf((float)DH));
     DKV_LAUNCH_CHECK();
@@ -223,9 +215,10 @@ template <typename T, typename C, typename... A> int launch_attn(int head_dim, A
     return head_dim == 32 ? launch_heads<T, C, 32>(a...) : head_dim == 64 ? launch_heads<T, C, 64>(a...) : launch_heads<T, C, 128>(a...);
 }
 
-// What both entry points refuse, and the plan of what they do not.
-int attn_call(const dkv_paged_cache *cache, PagedCache &view, Plan &plan, int32_t n_q_heads, int32_t rows, int32_t max_rows_per_seq,
-              int32_t dtype) {
+}  // namespace
+
+int dkv_paged_attn_plan(const dkv_paged_cache *cache, PagedCache &view, PagedAttnPlan &plan, int n_q_heads, int rows, int max_rows_per_seq,
+                        int dtype) {
     const int rc = dkv_paged_view(cache, view);
     if (rc) return rc;
     if (!cache->seq_len) { dkv_set_error("null argument"); return DKV_E_INVALID_ARG; }
@@ -243,13 +236,11 @@ int attn_call(const dkv_paged_cache *cache, PagedCache &view, Plan &plan, int32_
     return DKV_E_UNSUPPORTED;
 }
 
-}  // namespace
-
 extern "C" size_t dkv_paged_attn_workspace_bytes(const dkv_paged_cache *cache, int32_t n_q_heads, int32_t rows,
                                                  int32_t max_rows_per_seq, int32_t dtype) {
     PagedCache c;
     Plan p;
-    if (attn_call(cache, c, p, n_q_heads, rows, max_rows_per_seq, dtype)) return 0;
+    if (dkv_paged_attn_plan(cache, c, p, n_q_heads, rows, max_rows_per_seq, dtype)) return 0;
     return align_up(partial_bytes(p, c, cache->head_dim) + 256, 256);
 }
 
@@ -258,7 +249,7 @@ extern "C" int dkv_paged_attn(const dkv_paged_cache *cache, const void *q, int64
                               size_t workspace_bytes, void *stream) {
     PagedCache c;
     Plan p;
-    int rc = attn_call(cache, c, p, n_q_heads, rows, max_rows_per_seq, dtype);
+    int rc = dkv_paged_attn_plan(cache, c, p, n_q_heads, rows, max_rows_per_seq, dtype);
     if (rc || (rc = dkv_paged_check_rows(*cache, row_off, rows))) return rc;
     const int dh = cache->head_dim;
     if (q_stride < (int64_t)n_q_heads * dh) { dkv_set_error("row stride %lld is less than a row", (long long)q_stride); return DKV_E_INVALID_ARG; }

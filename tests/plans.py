@@ -119,3 +119,23 @@ def gather_rows(src, picks, counts, dst):
     f.restype, f.argtypes = C.c_int, [C.c_int, C.c_void_p, C.c_int] + [C.c_void_p] * 4 + [C.c_int]
     b._check(f(0 if src.dtype == torch.bfloat16 else 1, b._stream(), dst.shape[0], src.data_ptr(), picks.data_ptr(), counts.data_ptr(),
                dst.data_ptr(), dst.shape[1]))
+
+
+class PagedAttnPlan(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("q_tiles", "q_groups", "wide", "blocks", "cap", "spread", "least", "want")] + [("split", C.c_bool)]
+
+    @property
+    def kernel(self):
+        """'split' or 'wide' with the groups of wavefronts of a workgroup, and whether the keys of a sequence can be cut: 'split+', 'wide2', ..."""
+        return (f"wide{self.wide}" if self.wide else "split") + ("+" if self.split else "")
+
+
+def paged_plan(n_q_heads, rows, most, dtype, batch, max_pages, page_size, n_kv_heads, head_dim, cache_dtype, n_pages=None):
+    """The plan of dkv_paged_attn for a cache of these sizes."""
+    from paper_2505_15781_amd import binding as b
+    d = b.PagedCacheDesc(16, 16, 16, 16, 16, 16, batch, n_pages or batch * max_pages, max_pages, page_size, n_kv_heads, head_dim, cache_dtype)
+    f = b.lib._Z19dkv_paged_attn_planPK15dkv_paged_cacheR10PagedCacheR13PagedAttnPlaniiii
+    f.restype, f.argtypes = C.c_int, [C.POINTER(b.PagedCacheDesc), C.c_void_p, C.POINTER(PagedAttnPlan)] + [C.c_int] * 4
+    view, plan = C.create_string_buffer(256), PagedAttnPlan()           # the kernels' view of the cache is not looked at
+    b._check(f(C.byref(d), view, C.byref(plan), n_q_heads, rows, most, dtype))
+    return plan

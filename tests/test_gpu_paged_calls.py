@@ -1,0 +1,97 @@
+"""Attention over the paged cache on every kernel (the calls of paged_shapes.py, each checked to be planned to its own), with data that
+unit normal values do not bring: scores that keep growing, large ones, infinities and NaN, odd addresses. Bars as in test_gpu_paged.py."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2505_15781_amd as P
+from oracle import paged as O
+from paged_shapes import BLOCKS, CALLS, plan_of
+from test_gpu_paged import Cache, check_attn, dev, rows
+
+pytestmark = pytest.mark.gpu
+
+EVERY = [(name, types) for name in CALLS for types in (("bf16 bf16", "bf16 e4m3") if name in BLOCKS else ("bf16 bf16", "bf16 e4m3", "fp32 fp32", "fp32 e4m3"))]
+every_call = pytest.mark.parametrize("name,types", EVERY, ids=[n + "-" + t.replace(" ", "-") for n, t in EVERY])
+
+
+def make(name, types, seed, size=1.0):
+    """(cache with all positions stored, q with two rows behind the last sequence where the call takes them, rows of each sequence)"""
+    act, dtype = types.split()
+    lens, counts, page, heads, group, dh, kernel = CALLS[name]
+    if act == "bf16":
+        assert plan_of(name, {"bf16": P.BF16, "e4m3": P.E4M3}[dtype]).kernel == kernel
+    c = Cache(lens, page, heads, dh, dtype, seed=seed).fill(act, size=size)
+    extra = min(2, len(counts) * max(counts) - sum(counts))
+    return c, rows(np.random.default_rng(seed), (sum(counts) + extra, heads * group, dh), act), counts
+
+
+def store(c, b, positions, k, v):
+    """Rows of sequence b on both sides."""
+    n = c.o["table"].shape[0]
+    off = np.concatenate([np.zeros(b + 1, int), np.full(n - b, len(positions))])
+    P.paged_store(c.t, k, v, dev(positions), dev(off))
+    with np.errstate(over="ignore"):
+        O.store(c.o, k.double().cpu().numpy(), v.double().cpu().numpy(), np.asarray(positions), off, c.dtype)
+
+
+@every_call
+def test_scores_of_hundreds(name, types):
+    c, q, counts = make(name, types, 31, size=20.0)
+    check_attn(c, q, counts)
+
+
+@every_call
+def test_scores_that_grow_and_fall_along_a_sequence(name, types):
+    """Queries whose scores grow by some 60 (a factor of 2^86) from a sequence's first key to its last, others whose scores fall, and others that
+    hardly move: the reference of the exponentials follows, a little at nearly every tile, and what was summed before is brought along."""
+    c, q, counts = make(name, types, 32)
+    heads, dh = c.heads, c.dh
+    for b, n in enumerate(c.o["lengths"]):
+        k, v = (rows(np.random.default_rng(b + i), (n, heads, dh), types.split()[0]) for i in (40, 50))
+        k[:, :, 0] = (torch.arange(n, device="cuda")[:, None] * (8.0 / n)).to(k.dtype)
+        store(c, b, np.arange(n), k, v)
+    q[:, :, 0] = torch.tensor([7.5, -7.5, 0.5, 2.0], device="cuda").repeat(len(q) // 4 + 1)[:len(q), None].to(q.dtype) * dh ** 0.5
+    check_attn(c, q, counts)
+
+
+@every_call
+def test_infinities_and_nan_act_where_they_are_seen(name, types):
+    """Keys of -infinity, infinite and NaN values in the longest sequence and the last one, some in its first tile and some in its last."""
+    act, dtype = types.split()
+    c, q, counts = make(name, types, 33, size=0.5)            # no probability vanishes
+    heads, dh = c.heads, c.dh
+    for b in {int(np.argmax(c.o["lengths"])), len(counts) - 1}:
+        n = int(c.o["lengths"][b])
+        at = np.unique([3, n // 3, n // 2, n - 2])
+        k = torch.full((len(at), heads, dh), 0.25, dtype=q.dtype, device="cuda")
+        v = torch.ones_like(k)
+        k[0] = k[-1] = float("-inf")
+        v[0] = 1.0
+        v[1, 0, 5], v[2, heads - 1, dh - 1] = float("inf"), float("nan")
+        store(c, b, at, k, v)
+    with np.errstate(invalid="ignore"):
+        check_attn(c, q.abs(), counts)
+
+
+@every_call
+def test_addresses_of_any_element(name, types):
+    c, q, counts = make(name, types, 34)
+    room = torch.zeros(q.numel() + 8, dtype=q.dtype, device="cuda")
+    inside = room[5:5 + q.numel()].view(q.shape).copy_(q)
+    out = torch.full((q.numel() + 8,), 7.0, dtype=q.dtype, device="cuda")
+    check_attn(c, inside, counts, out=out[3:3 + q.numel()].view(q.shape))
+    assert (out[:3] == 7.0).all() and (out[3 + q.numel():] == 7.0).all()
+
+
+@every_call
+def test_pages_that_are_missing(name, types):
+    """A table with a quarter of its pages gone, the first and the last of the longest sequence among them."""
+    act, dtype = types.split()
+    lens, counts, page, heads, group, dh, _ = CALLS[name]
+    c = Cache(lens, page, heads, dh, dtype, seed=35, holes=0.25)
+    b = int(np.argmax(lens))
+    c.o["table"][b, [0, -(-lens[b] // page) - 1]] = -1
+    c.t.page_table.copy_(dev(c.o["table"]))
+    c.fill(act)
+    check_attn(c, rows(np.random.default_rng(35), (sum(counts), heads * group, dh), act), counts)
