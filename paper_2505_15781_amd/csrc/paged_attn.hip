@@ -8,15 +8,18 @@
 
 namespace {
 
-// Four dims of a result from their sums; a sum of exponentials of zero (nothing seen, or scores of -infinity only) gives zeros.
+// An element of a result from its sums. A sum of exponentials of zero (nothing seen, or scores of -infinity only) gives zero, chosen and not
+// multiplied: the products of zero probabilities with infinite or NaN values are NaN. `inv`: 1 / l.
+__device__ __forceinline__ float result(float o, float l, float inv) { return l == 0.f ? 0.f : o * inv; }
+// Four dims of a result.
 __device__ __forceinline__ void store_result(float *p, f32x4 o, float l) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    *reinterpret_cast<f32x4_el *>(p) = o * inv;
+    const float inv = 1.f / l;
+    *reinterpret_cast<f32x4_el *>(p) = f32x4{result(o[0], l, inv), result(o[1], l, inv), result(o[2], l, inv), result(o[3], l, inv)};
 }
 __device__ __forceinline__ void store_result(bf16_t *p, f32x4 o, float l) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    *reinterpret_cast<bf16x4_el *>(p) = u32x2{(uint32_t)f2bf(o[0] * inv) | ((uint32_t)f2bf(o[1] * inv) << 16),
-                                              (uint32_t)f2bf(o[2] * inv) | ((uint32_t)f2bf(o[3] * inv) << 16)};
+    const float inv = 1.f / l;
+    *reinterpret_cast<bf16x4_el *>(p) = u32x2{(uint32_t)f2bf(result(o[0], l, inv)) | ((uint32_t)f2bf(result(o[1], l, inv)) << 16),
+                                              (uint32_t)f2bf(result(o[2], l, inv)) | ((uint32_t)f2bf(result(o[3], l, inv)) << 16)};
 }
 
 #include "paged_split.h"

@@ -458,7 +458,7 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
                 f32x4{acc[i >> 2][4 * (i & 3)], acc[i >> 2][4 * (i & 3) + 1], acc[i >> 2][4 * (i & 3) + 2], acc[i >> 2][4 * (i & 3) + 3]};
         return;
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const float inv = 1.f / sum;
     bf16_t *op = out + ((size_t)r * (c.n_kv_heads * G.d) + h) * DH + 8 * g;
 #pragma unroll
     for (int mt = 0; mt < DH / 32; ++mt)
@@ -470,7 +470,7 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int v = 4 * c + (e >> 1) * 4 + (e & 1) * 2;
-                y[e] = (uint32_t)f2bf(acc[mt][v] * inv) | ((uint32_t)f2bf(acc[mt][v + 1] * inv) << 16);
+                y[e] = (uint32_t)f2bf(result(acc[mt][v], sum, inv)) | ((uint32_t)f2bf(result(acc[mt][v + 1], sum, inv)) << 16);
             }
             const auto p0 = __builtin_amdgcn_permlane32_swap(y[0], y[2], false, false);
             const auto p1 = __builtin_amdgcn_permlane32_swap(y[1], y[3], false, false);

@@ -7,7 +7,7 @@ import torch
 import paper_2505_15781_amd as P
 from oracle import paged as O
 from paged_shapes import BLOCKS, CALLS, plan_of
-from test_gpu_paged import Cache, check_attn, dev, rows
+from test_gpu_paged import Cache, bars, check_attn, dev, rows, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -95,3 +95,30 @@ def test_pages_that_are_missing(name, types):
     c.t.page_table.copy_(dev(c.o["table"]))
     c.fill(act)
     check_attn(c, rows(np.random.default_rng(35), (sum(counts), heads * group, dh), act), counts)
+
+
+@every_call
+def test_scores_of_minus_infinity_only_give_zeros_whatever_the_values(name, types):
+    """A query with -infinity where all keys are 1: its scores are -infinity, the sum of its exponentials is zero, and so is the result, also where
+    the values that it sees are infinite or NaN. The other queries see those values."""
+    act, dtype = types.split()
+    c, q, counts = make(name, types, 36, size=0.5)
+    for b, n in enumerate(c.o["lengths"]):
+        k, v = (rows(np.random.default_rng(b + i), (n, c.heads, c.dh), act) for i in (60, 70))
+        k[:, :, 1] = 1.0
+        v[0, :, 0], v[n // 2, :, 2], v[n - 1, :, 3] = float("inf"), float("nan"), float("-inf")
+        store(c, b, np.arange(n), 0.5 * k, v)
+    most = float(q.double().norm(dim=-1).max() * torch.from_numpy(c.o["k"][np.isfinite(c.o["k"])]).abs().max()) * 1.01     # at least |q| |k| / sqrt(dh)
+    q[::3, :, 1] = float("-inf")
+    none = np.arange(len(q)) % 3 == 0
+    offsets = np.concatenate([[0], np.cumsum(counts)])
+    out = torch.full_like(q, 7.0)
+    P.paged_attn(c.t, q, dev(offsets), out, max(counts), workspace(c, q, max(counts)))
+    with np.errstate(invalid="ignore"):
+        ref, spread, _ = O.attn(c.o, q.double().cpu().numpy(), offsets)
+    mine = np.arange(len(q)) < offsets[-1]
+    got, ref, spread = out.double().cpu().numpy()[mine], ref[mine], spread[mine]
+    assert (got[none[mine]] == 0).all() and (ref[none[mine]] == 0).all()
+    assert np.array_equal(np.isnan(got), np.isnan(ref)) and np.array_equal(got[np.isinf(ref)], ref[np.isinf(ref)])
+    fine = np.isfinite(ref)
+    assert (np.abs(got[fine] - ref[fine]) <= bars(q, c, ref, spread, most)[fine]).all()
