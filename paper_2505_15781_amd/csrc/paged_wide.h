@@ -12,7 +12,7 @@
 // 4 sequences of 1536 rows and keys, 32 heads of 128, e4m3 (155 GFLOP): 174-182 us by card, 850-890 TFLOP/s. Bound by power: with zeros
 // for data the same launch takes 160 us. Softmax, products and LDS reads hide behind each other: without its exponentials it takes
 // 5 % less, without the maximum 2 %, without the reads of V 4 %. Measured and not kept there: the maximum inside the stretch (193 us), 64 query rows
-// per wavefront (227), row sums by products with ones (182 against 179), e4m3 conversion spread over the stretch (no gain;
+// per wavefront (227), e4m3 conversion spread over the stretch (no gain;
 // 64 dims 125 -> 150), two groups of wavefronts (187-209), blocks of 256 query rows with eight
 // wavefronts behind one barrier, which halves the fills (201 against 183: two workgroups to a compute unit drift apart and fill each other's
 // gaps), LDS reads 9 and 12 ahead instead of 6 (no change).
@@ -266,7 +266,15 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
     // lowest finite start: scores of -inf then give probabilities of zero, also where a whole half tile is masked
     float m_run = -3.0e38f, alpha = 1.f;
     bool behind = false;
-    float l[2] = {0.f, 0.f};                     // sums of this lane's probabilities
+    // Sum of exactly the rounded probabilities that weigh the values, so that a weight is off by at most half a step however few keys share it:
+    // with the unrounded ones the largest error of peaked scores is half as large again (0.024 against 0.016; 4 x 32 heads, 1536 rows and keys 184 us
+    // against 187). A product with a tile whose row 0 is ones: element 0 of the lanes below 32 is the sum of query qi, everything else stays zero.
+    f32x16 l_acc;
+    bf16x8 ones;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) l_acc[v] = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = qi == 0 ? (__bf16)1.0f : (__bf16)0.0f;
     f32x16 acc[DH / 32], stA, stB;               // stA, stB: scores of the first and the second 32 keys of a tile
     bf16x8 pA[2], pB[2];                         // their probabilities
 #pragma unroll
@@ -295,28 +303,28 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
         f32x8 p[2];
         constexpr int MT = DH / 32, N = DH / 16, PER = 16 / N;        // products of the scores, and of the output; exponentials next to each two
 #pragma unroll
+        for (int ks = 0; ks < 2; ++ks) l_acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ones, pv[ks], l_acc, 0, 0, 0);
+#pragma unroll
         for (int i = 0; i < N; ++i) {
             sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(i, kstage, khalf), qf[i], sn, 0, 0, 0);
             acc[i % MT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(i % MT, i / MT, vstage, vhalf), pv[i / MT], acc[i % MT], 0, 0, 0);
 #pragma unroll
-            for (int e = PER * i; e < PER * (i + 1); ++e) {
-                p[e >> 3][e & 7] = __builtin_amdgcn_exp2f(fmaf(so[e], scale_log2e, -m_run));
-                l[e & 1] += p[e >> 3][e & 7];
-            }
+            for (int e = PER * i; e < PER * (i + 1); ++e) p[e >> 3][e & 7] = __builtin_amdgcn_exp2f(fmaf(so[e], scale_log2e, -m_run));
         }
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) pn[ks] = __builtin_convertvector(p[ks], bf16x8);
         asm volatile("" : "+v"(pn[0]), "+v"(pn[1]));        // here, not behind the branches of maximum()
         __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x002, 3 * PER / 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, PER, 0);
             __builtin_amdgcn_sched_group_barrier(0x400, PER / 2, 0);
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-            __builtin_amdgcn_sched_group_barrier(0x002, 3 * PER / 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, PER, 0);
             __builtin_amdgcn_sched_group_barrier(0x400, PER / 2, 0);
         }
     };
@@ -325,6 +333,7 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
         if (!behind) return;
 #pragma unroll
         for (int mt = 0; mt < DH / 32; ++mt) acc[mt] *= alpha;
+        l_acc[0] *= alpha;
     };
     // Maximum of half `half` of tile t. The reference of the exponentials follows it only where it gets more than 2^8 ahead: probabilities
     // go up to 2^8 then, which costs fp32 sums and the rounding to bf16 (half a step of the value, whatever its size) nothing but that
@@ -351,8 +360,6 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
         const float m_new = fmaxf(m_run, mx);
         alpha = __builtin_amdgcn_exp2f(m_run - m_new);
         m_run = m_new;
-        l[0] *= alpha;
-        l[1] *= alpha;
     };
     auto tile_barrier = [&]() {
         asm volatile("" ::: "memory");
@@ -417,11 +424,13 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
     const int last = (n_tiles - 1) & 1;
     rescale();
 #pragma unroll
+    for (int ks = 0; ks < 2; ++ks) l_acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ones, pB[ks], l_acc, 0, 0, 0);
+#pragma unroll
     for (int i = 0; i < DH / 16; ++i)
         acc[i % (DH / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(i % (DH / 32), i / (DH / 32), last, 1), pB[i / (DH / 32)], acc[i % (DH / 32)], 0, 0, 0);
 
     float u, w;
-    swap_rows32(l[0] + l[1], u, w);
+    swap_rows32(l_acc[0], u, w);
     float sum = u + w;
     if (KS == 2 && parts == 2) {                 // the second group's state goes through LDS to the same lanes of the first
         f32x4 *parked = reinterpret_cast<f32x4 *>(smem_all + kWideLds<DH>);
