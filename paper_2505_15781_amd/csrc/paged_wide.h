@@ -20,7 +20,6 @@
 
 typedef __attribute__((address_space(3))) void *lds_ptr_t;
 template <int V> struct StageC { static constexpr int value = V; };
-constexpr float kLag = 8.f;                          // log2 of the largest probability
 template <int DH> constexpr int kWideLds = 4 * 64 * DH * 2;       // K0 K1 V0 V1
 
 // Place of the 16-byte chunk c of row r: c ^ wide_swizzle(r). 16 consecutive rows put a chunk (score operands) into 16 different places of
@@ -335,12 +334,16 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
         for (int mt = 0; mt < DH / 32; ++mt) acc[mt] *= alpha;
         l_acc[0] *= alpha;
     };
-    // Maximum of half `half` of tile t. The reference of the exponentials follows it only where it gets more than 2^8 ahead: probabilities
-    // go up to 2^8 then, which costs fp32 sums and the rounding to bf16 (half a step of the value, whatever its size) nothing but that
-    // the largest one is no longer exact, and of a wavefront's vector instructions a third, the rescaling of the output at
-    // nearly every half tile (32 queries, each with a new maximum now and then): 4 sequences x 32 heads, 1536 rows and keys 205 -> 193 us.
+    // Maximum of half `half` of tile t. bf16 caches: the running maximum is the reference of the exponentials, so that the largest
+    // probability is exactly 1, as in attn_wide.h. e4m3 caches: the reference follows only where the maximum gets more than 2^8 ahead. That saves the
+    // rescaling of the output at nearly every half tile (32 queries, each with a new maximum now and then), a third of a wavefront's vector
+    // instructions: 4 sequences x 32 heads, 1536 rows and keys 199 -> 187 us. The largest probability is then rounded as all others are (half a step of
+    // the value, whatever its size): relative error against float64 of the held values 0.0023 instead of 0.0022, with scores three times as large 0.0020
+    // instead of 0.0018, next to the 2^-4 by which e4m3 rounds the elements themselves. A bf16 cache has no such rounding: what is read from it
+    // is as exact as what dkv_attn_update reads (the reference that lags: 8 sequences x 32 heads, 512 rows, 1024 keys 98 us instead of 105).
     // The probabilities of the half tile before still wait for their product: the output is rescaled to the new reference
     // only behind that product, at the next call.
+    constexpr float LAG = E4M3 ? 8.f : 0.f;
     auto maximum = [&](f32x16 &st, int t, int half, int tile_pages) {
         rescale();
         if (!whole(t, tile_pages)) {                                   // uniform
@@ -355,7 +358,7 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
         float u, w;
         swap_rows32(mx, u, w);
         mx = fmaxf(u, w) * scale_log2e;
-        behind = __builtin_amdgcn_ballot_w64(mx > m_run + kLag) != 0;
+        behind = __builtin_amdgcn_ballot_w64(mx > m_run + LAG) != 0;
         if (!behind) return;
         const float m_new = fmaxf(m_run, mx);
         alpha = __builtin_amdgcn_exp2f(m_run - m_new);

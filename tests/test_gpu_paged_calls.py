@@ -154,3 +154,45 @@ def test_the_probabilities_that_weigh_the_values_sum_to_one(name, types):
         assert torch.equal(got, want), int((got != want).sum())
     else:
         assert ((got - want).abs() <= (int(c.o["lengths"].max()) + 64) * 2.0 ** -23 * want.abs()).all()
+
+
+def in_parts(x, n):
+    """x as the sum of a[i] * 8^-i, each a[i] of 4 significant bits."""
+    a = []
+    for i in range(n):
+        step = 2.0 ** (np.floor(np.log2(x)) - 3)
+        a.append(float(np.floor(x / step) * step))
+        x = 8 * (x - a[-1])
+        if x < 2.0 ** -6:
+            break
+    return a + [0.0] * (n - len(a))
+
+
+@every_call
+def test_the_largest_probability_is_exactly_one(name, types):
+    """Two keys with probabilities of 1 : 9 / 64 and values of 9 / 64 and -1, all others with a probability of zero: the result is zero, for
+    1 and 9 / 64 are bf16 numbers. What is left are the errors of fp32 scores: sums of 9 products of at most 32, 9 * 2^-24 of the exponent 2.8, the
+    same again for its scale, reference and exponential, of 9 / 73: below 1e-6. With the smaller one for reference the larger would be 64 / 9, which bf16 holds as
+    228 / 32, and the result 2.4e-4; blocks of 128 rows over an e4m3 cache do that, and are off by half a step of the larger at most, 2^-8 (64 / 73) (9 / 64). The
+    larger score comes last in even heads, first in odd ones."""
+    act, dtype = types.split()
+    c, q, counts = make(name, types, 38)
+    heads, dh = c.heads, c.dh
+    q[:] = 0.0
+    q[:, :, :8] = 8.0 ** -torch.arange(8.0, device="cuda").to(q.dtype)
+    q[:, :, 8] = 1.0
+    larger = torch.tensor(in_parts(np.log(64 / 9) * dh ** 0.5, 8), device="cuda").to(q.dtype)
+    for b, n in enumerate(c.o["lengths"]):
+        k, v = torch.zeros((n, heads, dh), dtype=q.dtype, device="cuda"), rows(np.random.default_rng(90 + b), (n, heads, dh), act)
+        k[:, :, 8] = -4096.0
+        for h in range(heads):
+            first, last = (n // 4, 3 * n // 4) if h % 2 == 0 else (3 * n // 4, n // 4)
+            k[first, h], k[last, h] = 0.0, 0.0
+            k[last, h, :8] = larger
+            v[first, h], v[last, h] = -1.0, 9 / 64
+        store(c, b, np.arange(n), k, v)
+    out = torch.full_like(q, 7.0)
+    n = sum(counts)
+    P.paged_attn(c.t, q, dev(np.concatenate([[0], np.cumsum(counts)])), out, max(counts), workspace(c, q, max(counts)))
+    half_a_step = 2.0 ** -8 * 9 / 73 if name in BLOCKS and dtype == "e4m3" else 0.0
+    assert float(out[:n].abs().max()) <= 1e-6 + half_a_step
