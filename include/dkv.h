@@ -283,8 +283,8 @@ int dkv_concat_reorder(const void *k_cached, const void *v_cached, const void *k
  *                    power of two (E8M0): element = code * 2^(scale - 127)
  *   page_table (dev) [batch][max_pages]
  *   seq_len (dev) [batch] positions of each sequence (attention only; taken as 0 below 0, as max_pages * page_size above)
- * page_size: a power of two, 16 to 65536; max_pages * page_size at most 2^30, n_pages * n_kv_heads * page_size at most 2^32; head_dim 32, 64 or 128; dtype DKV_BF16, DKV_FP32 or
- * DKV_E4M3. Nothing in the structure is kept by a call; the structure itself is host memory. Table, lengths, positions
+ * page_size: a power of two, 16 to 65536; max_pages * page_size at most 2^30, n_pages * n_kv_heads * page_size at most 2^32, n_kv_heads * head_dim
+ * below 2^31; head_dim 32, 64 or 128; dtype DKV_BF16, DKV_FP32 or DKV_E4M3. Nothing in the structure is kept by a call; the structure itself is host memory. Table, lengths, positions
  * and row offsets are read on the device, so a captured call follows them. The current device is that of the cache and the stream. */
 typedef struct {
     void *k_pages, *v_pages;

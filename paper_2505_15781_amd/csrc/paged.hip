@@ -168,6 +168,7 @@ int dkv_paged_view(const dkv_paged_cache *c, PagedCache &view) {
     if (c->page_size < 16 || c->page_size > 65536 || (c->page_size & (c->page_size - 1))) {
         dkv_set_error("page_size %d not supported (a power of two, 16 to 65536)", c->page_size); return DKV_E_UNSUPPORTED;
     }
+    if ((int64_t)c->n_kv_heads * c->head_dim >= 1ll << 31) { dkv_set_error("rows of 2^31 elements and more are not supported"); return DKV_E_UNSUPPORTED; }
     if ((int64_t)c->max_pages * c->page_size > 1 << 30) { dkv_set_error("the table covers more than 2^30 positions"); return DKV_E_UNSUPPORTED; }
     if ((int64_t)c->n_pages * c->n_kv_heads > (1ll << 32) / c->page_size) { dkv_set_error("more than 2^32 rows of keys in one cache"); return DKV_E_UNSUPPORTED; }
     if ((reinterpret_cast<uintptr_t>(c->k_pages) | reinterpret_cast<uintptr_t>(c->v_pages)) % 16) { dkv_set_error("pages must be 16-byte aligned"); return DKV_E_INVALID_ARG; }

@@ -147,3 +147,11 @@ def test_rows_that_are_parts_of_longer_ones_are_taken():
     """Slices of a fused projection's rows pass every check but the last (these tensors are not on a GPU)."""
     qkv = torch.zeros((6, 8, 64), dtype=torch.bfloat16)
     refused(("store", "attn"), tensors(), "not on a GPU", k=qkv[:, 4:6], q=qkv[:, :4])
+
+
+def test_rows_longer_than_an_index_are_refused():
+    """2^24 K/V heads of 128 in one page of 16: 2^28 rows of keys, within the cache's limits, but a row of 2^31 elements, which the kernels index in 32 bits."""
+    many = dict(n_kv_heads=1 << 24, head_dim=128, n_pages=1, max_pages=1)
+    assert store(stride=1 << 31, **many) == -3 and "2^31" in B.last_error()
+    assert load(**many) == -3 and "2^31" in B.last_error()
+    assert B.lib.dkv_paged_attn_workspace_bytes(C.byref(desc(**many)), 1 << 24, 3, 2, 0) == 0
