@@ -176,6 +176,19 @@ typedef struct {
     int n_dims, dtype, device, whole;     /* dtype: T_*, or -1; device: -1 on the host */
 } tensor_info;
 
+/* where it is, and whether it is contiguous */
+static int look_memory(PyObject *t, tensor_info *i) {
+    PyObject *v = PyObject_CallMethodObjArgs(t, s_is_contiguous, NULL);
+    if (!v) return -1;
+    i->whole = (int)PyLong_AsLong(v);      /* a bool is a whole number */
+    Py_DECREF(v);
+    if (!(v = PyObject_CallMethodObjArgs(t, s_get_device, NULL))) return -1;
+    i->device = (int)PyLong_AsLong(v);
+    Py_DECREF(v);
+    if (PyErr_Occurred()) return -1;
+    return get_ptr(t, &i->ptr);
+}
+
 static int look(PyObject *t, tensor_info *i) {
     const Py_ssize_t d = get_shape(t, i->dims, 4);
     if (d < 0) return -1;
@@ -184,14 +197,7 @@ static int look(PyObject *t, tensor_info *i) {
     if (!v) return -1;
     for (i->dtype = T_COUNT - 1; i->dtype >= 0 && dtypes[i->dtype] != v; --i->dtype);
     Py_DECREF(v);
-    if (!(v = PyObject_CallMethodObjArgs(t, s_is_contiguous, NULL))) return -1;
-    i->whole = (int)PyLong_AsLong(v);      /* a bool is a whole number */
-    Py_DECREF(v);
-    if (!(v = PyObject_CallMethodObjArgs(t, s_get_device, NULL))) return -1;
-    i->device = (int)PyLong_AsLong(v);
-    Py_DECREF(v);
-    if (PyErr_Occurred()) return -1;
-    return get_ptr(t, &i->ptr);
+    return look_memory(t, i);
 }
 
 static int refuse(const char *name, const char *text) {
@@ -365,7 +371,7 @@ static PyObject *py_paged_attn(PyObject *self, PyObject *const *a, Py_ssize_t n)
         look_whole(a[3], "out", q.dtype, 3, q.dims, device, &out) || get_i32(a[4], &most))
         return NULL;
     if (a[5] != Py_None) {
-        if (look(a[5], &ws)) return NULL;
+        if (look_memory(a[5], &ws)) return NULL;      /* of any type and shape: its sizes may pass 32 bits */
         if (!ws.whole || ws.device != device) {
             refuse("workspace", "a contiguous tensor on the device of the cache is expected");
             return NULL;

@@ -155,3 +155,11 @@ def test_rows_longer_than_an_index_are_refused():
     assert store(stride=1 << 31, **many) == -3 and "2^31" in B.last_error()
     assert load(**many) == -3 and "2^31" in B.last_error()
     assert B.lib.dkv_paged_attn_workspace_bytes(C.byref(desc(**many)), 1 << 24, 3, 2, 0) == 0
+
+
+@pytest.mark.parametrize("elements,dtype", [(2 ** 31, torch.uint8), (2 ** 32 + 16, torch.uint8), (2 ** 31, torch.float32)])
+def test_a_workspace_may_be_a_large_arena(elements, dtype):
+    """Only its address, bytes and device are asked for: it passes every check but the last (these tensors are not on a GPU)."""
+    refused(("attn",), tensors(), "not on a GPU", ws=torch.empty(elements, dtype=dtype, device="meta"))
+    with pytest.raises(ValueError, match="workspace"):
+        calls(tensors(), ws=torch.empty((elements // 2, 2), dtype=dtype, device="meta")[:, 0])["attn"]()
