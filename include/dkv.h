@@ -320,8 +320,8 @@ int dkv_paged_load(const dkv_paged_cache *cache, void *k_out, void *v_out, const
  *   q (dev) [rows] rows of [n_q_heads][head_dim], `q_stride` elements apart (at least n_q_heads * head_dim); out (dev)
  *     [rows][n_q_heads][head_dim]; elements of `dtype`
  *   row_off as above; max_rows_per_seq (host) bounds the rows of any one sequence (rows of a sequence beyond it are left out)
- *   workspace (dev), 16-byte aligned, of dkv_paged_attn_workspace_bytes for the same cache, heads, rows and bound; calls that may
- *     overlap need one each
+ *   workspace (dev), 16-byte aligned, of dkv_paged_attn_workspace_bytes for the same cache and heads and at least as many rows and as large a
+ *     bound; calls that may overlap need one each
  * out overlaps none of the inputs. Results are finite where the sum of the magnitudes of V over a sequence's keys is below 2^128 (DKV_E4M3: 2^120; the
  * sums are divided last).
  * Rows from min(rows, row_off[batch]) on are left as they are. dtype DKV_BF16 reads DKV_BF16 and DKV_E4M3 caches (products of bf16

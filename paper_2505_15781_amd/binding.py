@@ -384,7 +384,8 @@ def paged_load(cache, k_out, v_out, positions, row_off=None):
 
 
 def paged_attn_workspace_bytes(cache, n_q_heads, rows, max_rows_per_seq, dtype=BF16):
-    """Bytes of workspace that paged_attn needs for this many rows of `dtype` (0 where it would refuse them)."""
+    """Bytes of workspace that paged_attn needs for this many rows of `dtype` at most, and for this bound at most (0 where it would
+    refuse them)."""
     return _marshal.paged_attn_workspace_bytes(cache, n_q_heads, rows, max_rows_per_seq, dtype)
 
 

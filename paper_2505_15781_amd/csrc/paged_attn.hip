@@ -2,6 +2,7 @@
 #include <math.h>
 
 #include <atomic>
+#include <initializer_list>
 
 #include "attn_common.h"
 #include "paged.h"
@@ -60,18 +61,27 @@ int best_spread(int groups, int heads, int per_cu) {
     return best;
 }
 
+// Groups of n query rows, each of one (sequence, K/V head), at most: by the longest sequence's rows, or by the rows of all.
+int64_t row_groups(const PagedCache &c, int rows, int max_rows, int G, int n) {
+    const int64_t by_longest = (int64_t)c.batch * ceil_div(max_rows * G, n), by_all = c.batch + (int64_t)ceil_div(rows * G, n);
+    return (by_longest < by_all ? by_longest : by_all) * c.n_kv_heads;
+}
+// Blocks of 128 query rows, see make_plan: whether there are rows enough, whether groups of 32 are so many or the keys that are cut so long, and
+// whether keys are cut. None of them turns back with more rows.
+bool rows_for_blocks(int dtype, int head_dim, int query_rows) { return dtype == DKV_BF16 && head_dim >= 64 && query_rows > (head_dim == 128 ? 32 : 64); }
+bool blocks_for_rounds(int head_dim, int64_t groups) { return groups > (head_dim == 128 ? kWorkgroups : 3 * kWorkgroups); }
+bool blocks_for_keys(int head_dim, int64_t groups, int64_t keys) { return keys * head_dim >= 4096 * 128 && groups * keys >= kWorkgroups * 1536; }
+bool keys_to_cut(int head_dim, int64_t keys) { return keys >= (head_dim == 64 ? 4096 : 2048); }
+int block_workgroups_per_cu(int head_dim) { return head_dim == 64 ? 3 : 1; }
+int split_tiles(int dtype, int tiles) { return dtype == DKV_BF16 && tiles > 1 ? 2 : 1; }
+
 Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int dtype, int head_dim) {
     Plan p;
     max_rows = max_rows < rows ? max_rows : rows;
     const int G = n_q_heads / c.n_kv_heads, heads = c.n_kv_heads;
     const int tiles = ceil_div(max_rows > 0 ? max_rows * G : 1, 16), key_tiles = ceil_div(c.max_pages << c.page_shift, PKT);
     const int64_t keys = (int64_t)key_tiles * PKT;
-    // (sequence, K/V head, n query rows) at most: by the longest sequence's rows, or by the rows of all
-    auto blocks_of = [&](int n) {
-        const int64_t by_longest = (int64_t)c.batch * ceil_div(max_rows * G, n), by_all = c.batch + (int64_t)ceil_div(rows * G, n);
-        return (by_longest < by_all ? by_longest : by_all) * heads;
-    };
-    p.nq = dtype == DKV_BF16 && tiles > 1 ? 2 : 1;
+    p.nq = split_tiles(dtype, tiles);
     p.q_groups = ceil_div(tiles, p.nq);
     p.wide = p.blocks = 0;
     p.spread = best_spread(p.q_groups, heads, 1);
@@ -100,17 +110,17 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     // them (28/4 heads, 8 sequences of up to 9000 keys and 80 rows, 12 slices 146 -> 91 us; 14 of up to 2100, 37 rows, 20 slices 40 -> 35.7; but
     // 30 of up to 3000, 20 rows, 32 slices 57.5 -> 60.6). In two rounds of slices batches of one length lose (8 sequences of 5600 keys, 32 heads, 80
     // rows 119 -> 141).
-    if (dtype == DKV_BF16 && head_dim >= 64 && max_rows * G > (head_dim == 128 ? 32 : 64)) {
-        const int64_t groups = blocks_of(32), blocks = blocks_of(128);
-        const int per_cu = head_dim == 64 ? 3 : 1, q_groups = ceil_div(tiles, 8), spread = best_spread(q_groups, heads, per_cu);
+    if (rows_for_blocks(dtype, head_dim, max_rows * G)) {
+        const int64_t groups = row_groups(c, rows, max_rows, G, 32), blocks = row_groups(c, rows, max_rows, G, 128);
+        const int per_cu = block_workgroups_per_cu(head_dim), q_groups = ceil_div(tiles, 8), spread = best_spread(q_groups, heads, per_cu);
         const int slices = slices_at_once(q_groups, heads, spread, per_cu);
         const int64_t two_by_two = (int64_t)c.batch * heads * ceil_div(max_rows * G, 256), other = (blocks + (int64_t)c.batch * heads) / 2;
         int wide = blocks <= 320 && (two_by_two < other ? two_by_two : other) <= kWorkgroups && key_tiles > 16 ? 2 : 1;
         const bool ragged = 4 * (int64_t)rows <= 3 * (int64_t)c.batch * max_rows;
-        const bool cut = (wide == 2 || head_dim == 64) && keys >= (head_dim == 64 ? 4096 : 2048) &&
+        const bool cut = (wide == 2 || head_dim == 64) && keys_to_cut(head_dim, keys) &&
                          (slices >= 2 * c.batch || (ragged && 4 * slices >= 5 * c.batch));
         if (cut && head_dim == 64) wide = 1;
-        if (groups > (head_dim == 128 ? kWorkgroups : 3 * kWorkgroups) || (cut && keys * head_dim >= 4096 * 128 && groups * keys >= kWorkgroups * 1536)) {
+        if (blocks_for_rounds(head_dim, groups) || (cut && blocks_for_keys(head_dim, groups, keys))) {
             p.wide = wide;
             p.blocks = (int)blocks;
             p.nq = 8;
@@ -148,6 +158,29 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
 size_t meta_bytes(const PagedCache &c) { return align_up(c.batch * sizeof(int2), 16); }
 size_t partial_bytes(const Plan &p, const PagedCache &c, int head_dim) {
     return p.split ? meta_bytes(c) + (size_t)p.cap * c.n_kv_heads * (p.q_groups * p.nq * 16) * (head_dim + 4) * sizeof(float) : 0;
+}
+// What no plan of this many rows and fewer exceeds, so that one workspace serves an active set that shrinks (fewer rows can have more slices: 28/4
+// heads, 8 sequences of 4096 keys, none with 128 rows each, 17 MB with 64, 4 with 8). The slices of a plan times its K/V heads and query groups are
+// one round of workgroups at most (slices_at_once), and no sequence has slices of less than `least` tiles.
+size_t most_partial_bytes(const PagedCache &c, int n_q_heads, int rows, int max_rows, int dtype, int head_dim) {
+    max_rows = max_rows < rows ? max_rows : rows;
+    const int G = n_q_heads / c.n_kv_heads, tiles = ceil_div(max_rows > 0 ? max_rows * G : 1, 16), key_tiles = ceil_div(c.max_pages << c.page_shift, PKT);
+    if (key_tiles <= whole_tiles(dtype, head_dim)) return 0;
+    auto bytes = [&](int nq, int least, int per_cu) {
+        int64_t n = 1;
+        for (int64_t factor : {(int64_t)c.batch * ceil_div(key_tiles, least), (int64_t)c.n_kv_heads, (int64_t)ceil_div(tiles, nq)}) {
+            n *= factor;
+            if (n > per_cu * kWorkgroups) n = per_cu * kWorkgroups;
+        }
+        return meta_bytes(c) + (size_t)n * (nq * 16) * (head_dim + 4) * sizeof(float);
+    };
+    const size_t split = bytes(split_tiles(dtype, tiles), kLeast, 1);
+    const int64_t groups = row_groups(c, rows, max_rows, G, 32), keys = (int64_t)key_tiles * PKT;
+    if (!rows_for_blocks(dtype, head_dim, max_rows * G) || !keys_to_cut(head_dim, keys) ||
+        !(blocks_for_rounds(head_dim, groups) || blocks_for_keys(head_dim, groups, keys)))
+        return split;
+    const size_t blocks = bytes(8, kLeastWide, block_workgroups_per_cu(head_dim));
+    return blocks > split ? blocks : split;
 }
 SlicePlan slice_plan(const Plan &p) { return SlicePlan{p.least, Divisor(p.want), p.split}; }
 GroupMap group_map(const Plan &p) { return GroupMap{Divisor(ceil_div(p.q_groups, 1 << p.spread)), p.spread, p.q_groups * p.nq * 16}; }
@@ -244,7 +277,7 @@ extern "C" size_t dkv_paged_attn_workspace_bytes(const dkv_paged_cache *cache, i
     PagedCache c;
     Plan p;
     if (dkv_paged_attn_plan(cache, c, p, n_q_heads, rows, max_rows_per_seq, dtype)) return 0;
-    return align_up(partial_bytes(p, c, cache->head_dim) + 256, 256);
+    return align_up(most_partial_bytes(c, n_q_heads, rows, max_rows_per_seq, dtype, cache->head_dim) + 256, 256);
 }
 
 extern "C" int dkv_paged_attn(const dkv_paged_cache *cache, const void *q, int64_t q_stride, const int32_t *row_off, void *out,

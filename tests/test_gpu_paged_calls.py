@@ -196,3 +196,19 @@ def test_the_largest_probability_is_exactly_one(name, types):
     P.paged_attn(c.t, q, dev(np.concatenate([[0], np.cumsum(counts)])), out, max(counts), workspace(c, q, max(counts)))
     half_a_step = 2.0 ** -8 * 9 / 73 if name in BLOCKS and dtype == "e4m3" else 0.0
     assert float(out[:n].abs().max()) <= 1e-6 + half_a_step
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+def test_an_active_set_that_shrinks_keeps_its_workspace(dtype):
+    """One workspace, asked for once for the most rows, whose plan has no slices; calls of fewer rows are cut into some."""
+    lens = [4200, 300, 2100]
+    c = Cache(lens, 32, 4, 128, dtype, seed=39).fill()
+    q = rows(np.random.default_rng(39), (3 * 400, 16, 128), "bf16")
+    ws = workspace(c, q, 400)
+    for counts in ([400, 400, 400], [200, 200, 200], [130, 7, 200], [64, 64, 64], [33, 1, 20], [8, 8, 8], [1, 0, 1], [0, 0, 1]):
+        n, most = sum(counts), max(counts)
+        out = torch.full((n, 16, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+        offsets = np.concatenate([[0], np.cumsum(counts)])
+        P.paged_attn(c.t, q[:n], dev(offsets), out, most, ws)
+        ref, spread, size = O.attn(c.o, q[:n].double().cpu().numpy(), offsets)
+        assert (np.abs(out.double().cpu().numpy() - ref) <= bars(q, c, ref, spread, size)).all()
