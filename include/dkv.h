@@ -280,7 +280,8 @@ int dkv_concat_reorder(const void *k_cached, const void *v_cached, const void *k
  * page can be given back before its sequence ends). Pages may be shared by sequences that only read them.
  *   k_pages, v_pages (dev) [n_pages][n_kv_heads][page_size][head_dim], elements of `dtype`, 16-byte aligned
  *   k_scale, v_scale (dev) [n_pages][n_kv_heads][page_size], DKV_E4M3 only: scale of a row as the biased exponent of a
- *                    power of two (E8M0): element = code * 2^(scale - 127)
+ *                    power of two (E8M0): element = code * 2^(scale - 127), of 17 to 247, which are those that a store writes; what
+ *                    is read from a row with another one is not defined
  *   page_table (dev) [batch][max_pages]
  *   seq_len (dev) [batch] positions of each sequence (attention only; taken as 0 below 0, as max_pages * page_size above)
  * page_size: a power of two, 16 to 65536; max_pages * page_size at most 2^30, n_pages * n_kv_heads * page_size at most 2^32, n_kv_heads * head_dim
@@ -319,14 +320,16 @@ int dkv_paged_load(const dkv_paged_cache *cache, void *k_out, void *v_out, const
  * never used, whatever it holds.
  *   q (dev) [rows] rows of [n_q_heads][head_dim], `q_stride` elements apart (at least n_q_heads * head_dim); out (dev)
  *     [rows][n_q_heads][head_dim]; elements of `dtype`
- *   row_off as above; max_rows_per_seq (host) bounds the rows of any one sequence (rows of a sequence beyond it are left out)
+ *   row_off as above; max_rows_per_seq (host) bounds the rows of any one sequence (rows of a sequence beyond it are left out); rows is at most
+ *     batch * max_rows_per_seq, a larger one is refused
  *   workspace (dev), 16-byte aligned, of dkv_paged_attn_workspace_bytes for the same cache and heads and at least as many rows and as large a
  *     bound; calls that may overlap need one each
  * out overlaps none of the inputs. Results are finite where the sum of the magnitudes of V over a sequence's keys is below 2^128 (DKV_E4M3: 2^120; the
  * sums are divided last).
- * Rows from min(rows, row_off[batch]) on are left as they are. dtype DKV_BF16 reads DKV_BF16 and DKV_E4M3 caches (products of bf16
- * operands, probabilities among them, sums in fp32; e4m3 elements with their scales are exact in bf16); DKV_FP32 reads
- * DKV_FP32 and DKV_E4M3 caches, in fp32 throughout. */
+ * Rows from min(rows, row_off[batch]) on are left as they are. Kernels and slices are planned from the table's width, as if all of it were in
+ * use: a call whose table is much wider than its lengths may take longer than with a narrow one, with the same results but for the order of sums.
+ * dtype DKV_BF16 reads DKV_BF16 and DKV_E4M3 caches (products of bf16 operands, probabilities among them, sums in fp32; e4m3 elements with
+ * their scales are exact in bf16); DKV_FP32 reads DKV_FP32 and DKV_E4M3 caches, in fp32 throughout. */
 size_t dkv_paged_attn_workspace_bytes(const dkv_paged_cache *cache, int32_t n_q_heads, int32_t rows, int32_t max_rows_per_seq,
                                       int32_t dtype);
 int dkv_paged_attn(const dkv_paged_cache *cache, const void *q, int64_t q_stride, const int32_t *row_off, void *out,

@@ -361,7 +361,8 @@ class PagedCache(NamedTuple):
     k_pages, v_pages  [n_pages, n_kv_heads, page_size, head_dim], bfloat16, float32 or float8_e4m3fn
     page_table        [batch, max_pages] int32; entries outside [0, n_pages): no page
     seq_len           [batch] int32, positions of each sequence (paged_attn only)
-    k_scale, v_scale  [n_pages, n_kv_heads, page_size] float8_e8m0fnu, with float8_e4m3fn pages only
+    k_scale, v_scale  [n_pages, n_kv_heads, page_size] float8_e8m0fnu, with float8_e4m3fn pages only: 2^-110 to 2^120, as paged_store
+                      writes them
     """
     k_pages: torch.Tensor
     v_pages: torch.Tensor
@@ -392,7 +393,7 @@ def paged_attn_workspace_bytes(cache, n_q_heads, rows, max_rows_per_seq, dtype=B
 def paged_attn(cache, q, row_off, out, max_rows_per_seq, workspace):
     """Attention of the rows of q [rows, n_q_heads, head_dim] over all positions of their sequences (below seq_len, on a
     page) into `out`; row_off as in paged_store (None: one row per sequence). max_rows_per_seq bounds the rows of any one
-    sequence; workspace: a tensor of paged_attn_workspace_bytes bytes, one for each call that may overlap."""
+    sequence, and q has at most that many for each; workspace: a tensor of paged_attn_workspace_bytes bytes, one for each call that may overlap."""
     _check(_marshal.paged_attn(cache, q, row_off, out, max_rows_per_seq, workspace))
 
 
