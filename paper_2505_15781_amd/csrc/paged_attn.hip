@@ -107,8 +107,10 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     // two groups (28/4 heads, 130 rows, 100000 keys: e4m3 214 -> 167 us, bf16 155 -> 151; 32/32 heads, 80 rows, 2 sequences of 31000
     // 152 -> 123 and 116 -> 113; the other way 28/4 heads, 17 rows of 2 sequences of 31000 31.1 -> 32.8 and 28.4 -> 28.8).
     // With fewer slices the long sequences of a ragged batch are cut all the same: the host knows the rows, and takes it that keys go with
-    // them (28/4 heads, 8 sequences of up to 9000 keys and 80 rows, 12 slices 146 -> 91 us; 14 of up to 2100, 37 rows, 20 slices 40 -> 35.7; but
-    // 30 of up to 3000, 20 rows, 32 slices 57.5 -> 60.6). In two rounds of slices batches of one length lose (8 sequences of 5600 keys, 32 heads, 80
+    // them: ragged is a batch with at most 3/4 of the rows that the longest sequence's would make (28/4 heads, 8 sequences of up to 9000 keys and 80 rows, 12
+    // slices: 0.6 of them 159 -> 102 us, 0.75 158 -> 130, 1 161 -> 166; 14 of up to 2100, 37 rows, 20 slices: 0.6 45 -> 41, 0.75 46 -> 48, 0.8 46 -> 49), and
+    // from four slices for three sequences on (9 sequences, 12 slices 158 -> 133, 10 158 -> 162; of up to 3000 keys, 40 rows, 20 slices for 13 sequences
+    // 59 -> 44, 15 59.5 -> 59.5, 16 59.8 -> 63; 16/1 heads, 6000 keys, 64 rows, 32 slices for 24 109 -> 105, 26 109 -> 114). In two rounds of slices batches of one length lose (8 sequences of 5600 keys, 32 heads, 80
     // rows 119 -> 141).
     if (rows_for_blocks(dtype, head_dim, max_rows * G)) {
         const int64_t groups = row_groups(c, rows, max_rows, G, 32), blocks = row_groups(c, rows, max_rows, G, 128);
@@ -118,7 +120,7 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
         int wide = blocks <= 320 && (two_by_two < other ? two_by_two : other) <= kWorkgroups && key_tiles > 16 ? 2 : 1;
         const bool ragged = 4 * (int64_t)rows <= 3 * (int64_t)c.batch * max_rows;
         const bool cut = (wide == 2 || head_dim == 64) && keys_to_cut(head_dim, keys) &&
-                         (slices >= 2 * c.batch || (ragged && 4 * slices >= 5 * c.batch));
+                         (slices >= 2 * c.batch || (ragged && 3 * slices >= 4 * c.batch));
         if (cut && head_dim == 64) wide = 1;
         if (blocks_for_rounds(head_dim, groups) || (cut && blocks_for_keys(head_dim, groups, keys))) {
             p.wide = wide;

@@ -212,3 +212,24 @@ def test_an_active_set_that_shrinks_keeps_its_workspace(dtype):
         P.paged_attn(c.t, q[:n], dev(offsets), out, most, ws)
         ref, spread, size = O.attn(c.o, q[:n].double().cpu().numpy(), offsets)
         assert (np.abs(out.double().cpu().numpy() - ref) <= bars(q, c, ref, spread, size)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rows_of_any_bits_are_held_and_read_back(dtype):
+    """Random bit patterns, denormal numbers, infinities and NaN among them, in caches that are not quantised: the nearest value of the type."""
+    g = np.random.default_rng(40)
+    x = torch.from_numpy(g.integers(0, 2 ** 32, (2, 200, 64), dtype=np.uint64).astype(np.uint32).view(np.float32)).cuda()
+    tiny = torch.from_numpy((g.integers(0, 2 ** 23, (2, 200, 32)) | g.integers(0, 2, (2, 200, 32)) << 31).astype(np.uint32).view(np.float32)).cuda()
+    x[:, :, 32:] = tiny
+    c = Cache([2], 16, 200, 64, dtype)
+    P.paged_store(c.t, x, x, dev([0, 1]), dev([0, 2]))
+    y = x.double().cpu().numpy()
+    O.store(c.o, y, y, np.array([0, 1]), np.array([0, 2]), dtype)
+    assert c.same()
+    for out in ("bf16", "fp32"):
+        k, v = (torch.zeros(x.shape, dtype={"bf16": torch.bfloat16, "fp32": torch.float32}[out], device="cuda") for _ in "kv")
+        P.paged_load(c.t, k, v, dev([1, 0]), dev([0, 2]))
+        page = int(c.o["table"][0, 0])
+        want = c.o["k"][page, :, :2].transpose(1, 0, 2)[::-1]
+        want = O.round_bf16(want) if out == "bf16" else want
+        assert np.array_equal(k.double().cpu().numpy(), want, equal_nan=True) and np.array_equal(v.double().cpu().numpy(), want, equal_nan=True)

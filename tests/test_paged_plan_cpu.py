@@ -50,3 +50,11 @@ def test_a_workspace_for_many_rows_is_enough_for_fewer(group, heads, dh, batch, 
         assert B.lib.dkv_paged_attn_workspace_bytes(C.byref(d), group * heads, batch * m, m, dtype) >= largest, m
         assert B.lib.dkv_paged_attn_workspace_bytes(C.byref(d), group * heads, batch * 1000, 1000, dtype) < 32 << 20
     assert largest > 0
+
+
+@pytest.mark.parametrize("batch,cut", [(13, True), (14, True), (15, True), (16, False), (19, False)])
+def test_long_sequences_of_a_ragged_batch_are_cut_where_it_gains(batch, cut):
+    """28/4 heads, up to 40 rows and 3000 keys: 20 slices run at once, and cutting gains down to four for three sequences."""
+    rows = sum(-(-40 * (batch - b) // batch) for b in range(batch))
+    p = paged_plan(28, rows, 40, P.BF16, batch, 48, 64, 4, 128, P.E4M3)
+    assert p.kernel == ("wide2+" if cut else "wide2" if p.wide == 2 else "wide1")
