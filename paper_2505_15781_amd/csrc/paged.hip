@@ -98,8 +98,8 @@ struct RowWork {
 };
 
 // A lane writes 16 bytes. It loads its elements before the row's place is known: many rows are bound by the traffic, few by the chain
-// of offsets, page number and store. 6144 rows of 32 heads of 128 from bf16 into e4m3 33 us (4.6 TB/s; a large copy
-// 4.4), 64 rows 2.8 us. Four pieces of a lane at once gain nothing here and lose up to 45 % with few rows.
+// of offsets, page number and store. 6144 rows of 32 heads of 128 from bf16 into e4m3 31 us (4.8 TB/s; a large copy 4.45), into bf16 39
+// (5.1), from fp32 into fp32 71 (5.7), 64 rows 2.8 us. Four pieces of a lane at once gain nothing here and lose up to 45 % with few rows.
 template <typename T, typename C, int DH>
 __global__ __launch_bounds__(256) void paged_store_kernel(PagedCache c, const T *__restrict__ k_new, const T *__restrict__ v_new,
                                                           int64_t row_stride, const int *__restrict__ positions,
@@ -115,8 +115,10 @@ __global__ __launch_bounds__(256) void paged_store_kernel(PagedCache c, const T 
 }
 
 // A lane writes N times 16 bytes. Its loads are short where the cache is e4m3 (8 bytes for bf16 rows, 4 for fp32), and wait for the
-// row's place: with many rows four at once are ahead, 16384 rows of 32 heads 87 us against 105, 64 rows 3.2 against 2.5;
-// from bf16 and fp32 caches one is. 6144 rows from e4m3 to bf16 36 us (4.2 TB/s).
+// row's place: with many rows four at once are ahead, 16384 rows of 32 heads 87 us against 105, 64 rows 3.2 against 2.5. They meet at
+// 4096 wavefronts of four pieces a lane (32 heads of 128 to bf16: 512 rows 5.6 against 4.9, 1024 rows 7.3 and 7.5, 2048 rows 14.2 and 16.4; 8 heads of 64 to fp32,
+// 4096 rows 6.6 and 7.3). From bf16 and fp32 caches one is. 6144 rows from e4m3 to bf16 35 us (4.3 TB/s), from bf16 to bf16 42 (4.8), to fp32 75 (4.0), from fp32
+// to fp32 72 (5.6).
 template <typename T, typename C, int DH, int N>
 __global__ __launch_bounds__(256) void paged_load_kernel(PagedCache c, T *__restrict__ k_out, T *__restrict__ v_out,
                                                          const int *__restrict__ positions, const int *__restrict__ row_off, int rows,

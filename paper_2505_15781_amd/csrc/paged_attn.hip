@@ -40,13 +40,16 @@ int allow_lds(const void *kernel, int bytes, std::atomic<uint64_t> &devices) {
 
 typedef PagedAttnPlan Plan;
 
-// One workgroup of paged_attn_split holds a compute unit (its LDS): slices make up to that many, a second round costs what the first does
-// (two sequences of 131072 keys: 56 us with 256 workgroups, 67 with 512). A slice has 4 tiles of keys at least: what a compute unit
+// Slices of paged_attn_split make up to one workgroup for each compute unit. With 128 dims that is all that a unit's LDS holds, and a second round costs
+// what the first does (two sequences of 131072 keys: 56 us with 256 workgroups, 67 with 512). Smaller heads would leave room for two and more, which
+// is not made use of: nothing gained over bf16 and fp32 caches but for a few calls, 10 to 30 % over e4m3 ones (two sequences of 131072 keys of 28/4 heads, one
+// workgroup and two a unit: 64 dims, bf16 47.8 us and 48.7, e4m3 33.1 and 30.5; 32 dims, e4m3 28.1 and 21.9; 16 ragged ones of 4096, 64 dims, bf16 13.2
+// and 13.9). A slice has 4 tiles of keys at least: what a compute unit
 // reads is bound to some 50 GB/s, so idle units cost more than wavefronts without a tile (28/4 heads, 4 sequences of 2000 keys in
 // bf16: 10.5 us with 4 tiles, 11.4 with 8, 17.2 with 32, 22.3 without slices). paged_attn_wide, whose groups take 64 keys at a time: 16
 // tiles of 32 (28/4 heads, 64 rows, 4096 keys 23.1 us with 8, 21.9 with 16, 26.7 with 32; 16384 keys 36.8, 35.4, 35.3).
 constexpr int kWorkgroups = 256, kLeast = 4, kLeastWide = 16;
-// Key tiles up to which a sequence stays whole: the launch that joins slices costs some 2 us. bf16, 128 dims: 16 tiles 8.6 us whole and 9.0
+// Key tiles of a table (the host does not know the lengths) up to which sequences stay whole: the launch that joins slices costs some 2 us. bf16, 128 dims: 16 tiles 8.6 us whole and 9.0
 // in slices, 24 tiles 11.5 and 9.3; 64 dims: 24 tiles 7.3 and 8.1, 47 tiles 10.8 and 9.0. fp32 (four wavefronts, matrix instructions of an
 // eighth of the rate): 128 dims, 8 tiles 13.3 and 11.8; 64 dims, 8 tiles 7.4 and 8.4, 16 tiles 12.1 and 8.5; 32 dims, 16 tiles 7.5 and 8.2, 24 9.7 and 8.5.
 int whole_tiles(int dtype, int head_dim) { return (dtype == DKV_BF16 ? 2304 : 640) / head_dim; }
@@ -89,25 +92,27 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     int want = slices_at_once(p.q_groups, heads, p.spread, 1);
     p.split = key_tiles > whole_tiles(dtype, head_dim) && want > c.batch;
     // Blocks of 128 query rows (paged_wide.h) where tiles of 32 would make more than one round of workgroups (128 dims; 28/4 heads, 1024 keys: 1
-    // sequence of 300 rows, 264 workgroups, 42 -> 22 us, 4 of 128 rows, 448, 30 -> 23, but 4 of 64 rows, 224, 16 -> 22) or more than three (64
-    // dims, 32 heads, 8 sequences of 5600 keys: bf16, 80 rows, 768 workgroups, 60 -> 68, 128 rows, 1024, 81 -> 69, 250 rows, 122 -> 119; e4m3 65 ->
-    // 105, 93 -> 106, 146 -> 149, but with 700 keys 15.7 -> 18.6, 24.6 -> 19.4, 37.9 -> 22.6). Also where the
+    // sequence of 300 rows, 264 workgroups, 29 -> 26 us, 4 of 128 rows, 448, 30 -> 27, but 4 of 64 rows, 224, 17 -> 26) or more than three (64
+    // dims, 32 heads, 8 ragged sequences of up to 5600 keys: bf16, 80 rows 61 -> 61, 128 rows 81 -> 70, 250 rows, 119 -> 104; e4m3 65 ->
+    // 68, 94 -> 77, 144 -> 125; of 700 keys each 24.1 -> 21, 32 -> 22, 59 -> 32). Also where the
     // keys are so many that slices of them keep the compute units busy without those workgroups: 1536 keys each for tiles of 32 (28/4
-    // heads, 1 sequence of 128 rows, 4096 keys 30.5 -> 27.2 us, 32768 keys 128 -> 82, but 32 rows, 4096 keys 16.5 -> 19.7, 8192 keys 20.8 -> 21.6),
-    // of more than 4096 keys of 128 dims (64 dims, 2 sequences of 128 rows: 4096 keys 25.1 -> 28.7, 8192 keys 43.6 -> 40.6).
-    // More than 32 query rows to a sequence, which two of the four wavefronts work on (19 sequences of 700 keys, 32/32 heads, 40 rows 72 -> 57 us,
-    // 32/8 heads, 10 rows 27.6 -> 22.9); with 64 dims more than 64 (32/32 heads, 64 rows, 12 sequences of 8192 keys 160 -> 198, e4m3 156 -> 245).
-    // Two groups of wavefronts to a workgroup where the blocks are few and the keys many enough to share (96 blocks of 1024 keys 24.8 ->
-    // 22.5 us, 384 blocks 41 -> 47, 128 blocks of 256 keys 11.8 -> 12.6), and one round of workgroups holds them two by two (36 sequences
-    // of 700 keys, 32/8 heads, 32 rows: 288 blocks, each of a sequence of its own, 37.7 -> 54).
+    // heads, 1 sequence of 128 rows, 4096 keys 30.3 -> 28.9 us, 32768 keys 131 -> 98, but 32 rows, 4096 keys 15.9 -> 21.4, 8192 keys 21.0 -> 23.3),
+    // of more than 4096 keys of 128 dims (64 dims, 28/4 heads, 2 sequences of 128 rows: 4096 keys 27.6 -> 34.4 over e4m3, 8192 keys 48.3 -> 46.9, bf16 42.8 -> 44.6).
+    // More than 32 query rows to a sequence, which two of the four wavefronts work on (19 sequences of 700 keys, 32/32 heads, 40 rows 73 -> 59 us,
+    // 32/8 heads, 10 rows 27.9 -> 25.1); with 64 dims more than 64 (32/32 heads, 64 rows, 12 sequences of 8192 keys 160 -> 198, e4m3 156 -> 245).
+    // Two groups of wavefronts to a workgroup where the blocks are few and the keys many enough to share (96 blocks of 1024 keys 28.6 -> 26.0 us,
+    // 128 blocks of 256 keys 12.8 -> 13.6), and one round of workgroups holds them two by two (36 sequences
+    // of 700 keys, 32/8 heads, 32 rows: 288 blocks, each of a sequence of its own, 43 -> 58). Few are 320 at most, for the longest sequences of ragged batches
+    // are then shared and the shorter ones paired (28/4 heads, 129 rows and 1536 keys at most: at most 308 blocks 45.8 -> 42.3, 344 47.2 -> 46.5, 380 50.8 -> 52.9);
+    // batches of one length gain up to 256 and lose a little from there (32/32 heads, 1536 keys: 256 blocks 45.9 -> 43.9, 288 60.2 -> 63.4).
     // Their keys are cut where every sequence can have two slices, from 2048 keys of 128 dims on (32/8 heads, 300 rows, 80 blocks: 1300 keys
-    // 28.7 us whole and 32.6 in slices, 2700 keys 47.8 and 40.2; 28/4 heads, 4 ragged sequences of 130 rows and 2000 keys at most 37.4 and 33.1),
-    // from 4096 of 64 dims (32/32 heads, 4 sequences of 300 rows, 2700 keys 69 and 85; 28/4 heads 77 and 80, 3500 keys 95 and 90).
+    // 32.9 us whole and 33.8 in slices, 2700 keys 55.9 and 43.0; 28/4 heads, 4 ragged sequences of 130 rows and 2000 keys at most 43.8 and 35.4),
+    // from 4096 of 64 dims (4 sequences of 300 rows, 2700 keys: 32/32 heads 69 and 86, 28/4 heads 69 and 79, 3500 keys 85 and 89).
     // Slices of heads of 64 have one group of wavefronts, and three workgroups a compute unit, which hold more loads on their way than one of
     // two groups (28/4 heads, 130 rows, 100000 keys: e4m3 214 -> 167 us, bf16 155 -> 151; 32/32 heads, 80 rows, 2 sequences of 31000
     // 152 -> 123 and 116 -> 113; the other way 28/4 heads, 17 rows of 2 sequences of 31000 31.1 -> 32.8 and 28.4 -> 28.8).
-    // With fewer slices the long sequences of a ragged batch are cut all the same: the host knows the rows, and takes it that keys go with
-    // them: ragged is a batch with at most 3/4 of the rows that the longest sequence's would make (28/4 heads, 8 sequences of up to 9000 keys and 80 rows, 12
+    // With fewer slices the long sequences of a ragged batch are cut all the same. The host knows the rows, and takes it that keys go with
+    // them (a batch of equal rows over ragged lengths is not seen): ragged is a batch with at most 3/4 of the rows that the longest sequence's would make (28/4 heads, 8 sequences of up to 9000 keys and 80 rows, 12
     // slices: 0.6 of them 159 -> 102 us, 0.75 158 -> 130, 1 161 -> 166; 14 of up to 2100, 37 rows, 20 slices: 0.6 45 -> 41, 0.75 46 -> 48, 0.8 46 -> 49), and
     // from four slices for three sequences on (9 sequences, 12 slices 158 -> 133, 10 158 -> 162; of up to 3000 keys, 40 rows, 20 slices for 13 sequences
     // 59 -> 44, 15 59.5 -> 59.5, 16 59.8 -> 63; 16/1 heads, 6000 keys, 64 rows, 32 slices for 24 109 -> 105, 26 109 -> 114). In two rounds of slices batches of one length lose (8 sequences of 5600 keys, 32 heads, 80

@@ -9,9 +9,10 @@
 //   e4m3: through registers, a tile ahead, converted with their row's scale (exact) on the way into LDS. K and V are converted
 //         once per 128 query rows: 32 of a wavefront's vector instructions per tile, next to some 230 of the softmax.
 //
-// 4 sequences of 1536 rows and keys, 32 heads of 128, e4m3 (155 GFLOP): 174-182 us by card, 850-890 TFLOP/s. Bound by power: with zeros
-// for data the same launch takes 160 us. Softmax, products and LDS reads hide behind each other: without its exponentials it takes
-// 5 % less, without the maximum 2 %, without the reads of V 4 %. Measured and not kept there: the maximum inside the stretch (193 us), 64 query rows
+// 4 sequences of 1536 rows and keys, 32 heads of 128 (155 GFLOP): e4m3 178-188 us by card, 820-870 TFLOP/s, bf16 191-193. A large product would take
+// 111 us. Power is part of the rest: with zeros for data the same launches take 160 and 143 us. What the other part is no counters show yet. Softmax, products
+// and LDS reads hide behind each other: without its exponentials the e4m3 launch took 5 % less, without the maximum 2 %, without the reads of V 4 %. Measured and
+// not kept there: the maximum inside the stretch (193 us), 64 query rows
 // per wavefront (227), e4m3 conversion spread over the stretch (no gain;
 // 64 dims 125 -> 150), two groups of wavefronts (187-209), blocks of 256 query rows with eight
 // wavefronts behind one barrier, which halves the fills (201 against 183: two workgroups to a compute unit drift apart and fill each other's
