@@ -233,3 +233,13 @@ def test_rows_of_any_bits_are_held_and_read_back(dtype):
         want = c.o["k"][page, :, :2].transpose(1, 0, 2)[::-1]
         want = O.round_bf16(want) if out == "bf16" else want
         assert np.array_equal(k.double().cpu().numpy(), want, equal_nan=True) and np.array_equal(v.double().cpu().numpy(), want, equal_nan=True)
+
+
+@every_call
+def test_a_table_that_is_much_wider_than_its_sequences(name, types):
+    """16384 positions, as a table for sequences that grow in a captured loop would have: the plan goes by them, the results by the lengths."""
+    act, dtype = types.split()
+    lens, counts, page, heads, group, dh, _ = CALLS[name]
+    c = Cache(lens, page, heads, dh, dtype, seed=41, wider=16384 // page - max(-(-n // page) for n in lens)).fill(act)
+    assert c.t.page_table.shape[1] == 16384 // page
+    check_attn(c, rows(np.random.default_rng(41), (sum(counts), heads * group, dh), act), counts)
