@@ -7,7 +7,7 @@
 // their places are found once per tile from page numbers that a lane each holds for the next 1024 keys.
 //   bf16: global memory to LDS without registers; keys that are not there (behind the end, no page) come from a row of zeros.
 //   e4m3: through registers, a tile ahead, converted with their row's scale (exact) on the way into LDS. K and V are converted
-//         once per 128 query rows: 32 of a wavefront's vector instructions per tile, next to some 230 of the softmax.
+//         once per 128 query rows: 32 of a wavefront's vector instructions per tile, next to some 200 of the softmax.
 //
 // 4 sequences of 1536 rows and keys, 32 heads of 128 (155 GFLOP): e4m3 178-188 us by card, 820-870 TFLOP/s, bf16 191-193. A large product would take
 // 111 us. Power is part of the rest: with zeros for data the same launches take 160 and 143 us. What the other part is no counters show yet. Softmax, products
