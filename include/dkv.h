@@ -33,6 +33,7 @@ extern "C" {
 #define DKV_BF16 0
 #define DKV_FP32 1
 #define DKV_E4M3 2        /* paged caches only (dkv_paged_cache): 8 bits per element, a scale per position and K/V head */
+#define DKV_E2M1 4        /* paged caches only: 4 bits per element, a scale for each 32 dims of a position and K/V head */
 
 /* cache variants (Sec. 3.3 "dKV-Cache-Decode", "dKV-Cache-Prefill and dKV-Cache-PD"; Sec. 3.4) */
 #define DKV_DECODE  0
@@ -278,14 +279,16 @@ int dkv_concat_reorder(const void *k_cached, const void *v_cached, const void *k
  * page_table[b][p / page_size] at slot p % page_size. An entry outside [0, n_pages) says that there is no page: rows are not
  * stored there, loads give zeros, attention leaves those positions out (a table can be wider than what is in use, and a
  * page can be given back before its sequence ends). Pages may be shared by sequences that only read them.
- *   k_pages, v_pages (dev) [n_pages][n_kv_heads][page_size][head_dim], elements of `dtype`, 16-byte aligned
+ *   k_pages, v_pages (dev) [n_pages][n_kv_heads][page_size][head_dim], elements of `dtype`, 16-byte aligned; DKV_E2M1: two to a byte
+ *                    ([head_dim / 2]), the lower dim in the lower 4 bits: a sign bit and 0, 0.5, 1, 1.5, 2, 3, 4 or 6
  *   k_scale, v_scale (dev) [n_pages][n_kv_heads][page_size], DKV_E4M3 only: scale of a row as the biased exponent of a
  *                    power of two (E8M0): element = code * 2^(scale - 127), of 17 to 247, which are those that a store writes; what
- *                    is read from a row with another one is not defined
+ *                    is read from a row with another one is not defined. DKV_E2M1: [n_pages][n_kv_heads][page_size][head_dim / 32], one for each 32
+                    dims, of 17 to 253, or 255, which makes the 32 dims NaN
  *   page_table (dev) [batch][max_pages]
  *   seq_len (dev) [batch] positions of each sequence (attention only; taken as 0 below 0, as max_pages * page_size above)
  * page_size: a power of two, 16 to 65536; max_pages * page_size at most 2^30, n_pages * n_kv_heads * page_size at most 2^32, n_kv_heads * head_dim
- * below 2^31; head_dim 32, 64 or 128; dtype DKV_BF16, DKV_FP32 or DKV_E4M3. Nothing in the structure is kept by a call; the structure itself is host memory. Table, lengths, positions
+ * below 2^31; head_dim 32, 64 or 128; dtype DKV_BF16, DKV_FP32, DKV_E4M3 or DKV_E2M1. Nothing in the structure is kept by a call; the structure itself is host memory. Table, lengths, positions
  * and row offsets are read on the device, so a captured call follows them. The current device is that of the cache and the stream. */
 typedef struct {
     void *k_pages, *v_pages;
@@ -303,7 +306,10 @@ typedef struct {
  * DKV_BF16 and DKV_FP32 caches hold the nearest value of their type. A DKV_E4M3 cache holds x * 2^-e rounded to the nearest e4m3
  * value, ties to even, with the smallest e >= -110 that brings the largest finite magnitude of the row to at most 448: an
  * error of at most 2^-4 of the element or 2^(e - 10), whichever is larger. Infinities and NaN become NaN, and count for nothing in e. (e is at
- * most 120, and then magnitudes end at 240 * 2^120, so that no finite element is read back as infinity.) */
+ * most 120, and then magnitudes end at 240 * 2^120, so that no finite element is read back as infinity.)
+ * A DKV_E2M1 cache holds x * 2^-e rounded to the nearest of its values, ties to the even code, with the smallest e >= -110 that brings the largest
+ * magnitude of the 32 dims to at most 6: an error of at most 2^-2 of the element or 2^(e - 2), whichever is larger. Where one of them is an infinity
+ * or a NaN all 32 become NaN. (e is at most 126, and then magnitudes end at 3 * 2^126.) */
 int dkv_paged_store(const dkv_paged_cache *cache, const void *k_new, const void *v_new, int64_t row_stride,
                     const int32_t *positions, const int32_t *row_off, int32_t rows, int32_t dtype, void *stream);
 
@@ -324,12 +330,12 @@ int dkv_paged_load(const dkv_paged_cache *cache, void *k_out, void *v_out, const
  *     batch * max_rows_per_seq, a larger one is refused
  *   workspace (dev), 16-byte aligned, of dkv_paged_attn_workspace_bytes for the same cache and heads and at least as many rows and as large a
  *     bound; calls that may overlap need one each
- * out overlaps none of the inputs. Results are finite where the sum of the magnitudes of V over a sequence's keys is below 2^128 (DKV_E4M3: 2^120; the
- * sums are divided last).
+ * out overlaps none of the inputs. Results are finite where the sum of the magnitudes of V over a sequence's keys is below 2^128 (DKV_E4M3 and
+ * DKV_E2M1: 2^120; the sums are divided last).
  * Rows from min(rows, row_off[batch]) on are left as they are. Kernels and slices are planned from the table's width, as if all of it were in
  * use: a call whose table is much wider than its lengths may take longer than with a narrow one, with the same results but for the order of sums.
- * dtype DKV_BF16 reads DKV_BF16 and DKV_E4M3 caches (products of bf16 operands, probabilities among them, sums in fp32; e4m3 elements with
- * their scales are exact in bf16); DKV_FP32 reads DKV_FP32 and DKV_E4M3 caches, in fp32 throughout. */
+ * dtype DKV_BF16 reads DKV_BF16, DKV_E4M3 and DKV_E2M1 caches (products of bf16 operands, probabilities among them, sums in fp32; e4m3 and e2m1
+ * elements with their scales are exact in bf16); DKV_FP32 reads DKV_FP32, DKV_E4M3 and DKV_E2M1 caches, in fp32 throughout. */
 size_t dkv_paged_attn_workspace_bytes(const dkv_paged_cache *cache, int32_t n_q_heads, int32_t rows, int32_t max_rows_per_seq,
                                       int32_t dtype);
 int dkv_paged_attn(const dkv_paged_cache *cache, const void *q, int64_t q_stride, const int32_t *row_off, void *out,

@@ -43,6 +43,35 @@ def quantise(x):
     return np.where(fine, round_e4m3(y) * scale, np.nan), e
 
 
+def e2m1_values():
+    """Value of each of the 16 codes: sign, 2 exponent bits (bias 1), 1 mantissa bit; neither infinities nor NaN."""
+    a = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+    return np.concatenate([a, -a])
+
+
+def round_e2m1(x):
+    """Nearest e2m1 value of magnitudes up to 6, ties to the even code."""
+    a, v = np.abs(x), e2m1_values()[:8]
+    hi = np.clip(np.searchsorted(v, a), 1, 7)
+    lo = hi - 1
+    below, above = a - v[lo], v[hi] - a
+    return np.copysign(v[np.where(below < above, lo, np.where(above < below, hi, np.where(lo % 2 == 0, lo, hi)))], x)
+
+
+def quantise_e2m1(x):
+    """Rows [..., n] -> (values held, exponents of their scales [..., n / 32]; 128: NaN)."""
+    x = np.asarray(x, dtype=np.float64)
+    y = x.reshape(x.shape[:-1] + (x.shape[-1] // 32, 32))
+    fine = np.isfinite(y).all(-1)
+    y = np.where(fine[..., None], y, 0.0)
+    # the smallest exponent that brings the 32 to at most 6
+    e = -110 + np.searchsorted(6.0 * 2.0 ** np.arange(-110, 126, dtype=np.float64), np.abs(y).max(-1))
+    scale = (2.0 ** e)[..., None]
+    most = np.where(e == 126, 3.0, 6.0)[..., None]
+    held = np.where(fine[..., None], round_e2m1(np.clip(y / scale, -most, most)) * scale, np.nan)
+    return held.reshape(x.shape), np.where(fine, e, 128)
+
+
 def round_bf16(x):
     import torch
     return torch.from_numpy(np.asarray(x, dtype=np.float32)).to(torch.bfloat16).double().numpy()
@@ -50,6 +79,8 @@ def round_bf16(x):
 
 def hold(x, dtype):
     """Rows as a cache of this type holds them."""
+    if dtype == "e2m1":
+        return quantise_e2m1(x)[0]
     return quantise(x)[0] if dtype == "e4m3" else round_bf16(x) if dtype == "bf16" else np.asarray(x, np.float32).astype(np.float64)
 
 

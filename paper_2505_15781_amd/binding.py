@@ -12,7 +12,7 @@ import torch
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libdkv.so")
-BF16, FP32, E4M3 = 0, 1, 2
+BF16, FP32, E4M3, E2M1 = 0, 1, 2, 4
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2505_15781_amd.build` "
@@ -351,18 +351,20 @@ class _Streams:
 
 _marshal.bind_paged(*(C.cast(f, c_vp).value for f in (lib.dkv_paged_store, lib.dkv_paged_load, lib.dkv_paged_attn_workspace_bytes,
                                                       lib.dkv_paged_attn)),
-                    torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.int32,
+                    torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.float8_e8m0fnu,
+                    getattr(torch, "float4_e2m1fn_x2", None), torch.int32,
                     torch._C if _raw_stream is not None and hasattr(torch._C, "_cuda_getDevice") else _Streams)
 
 
 class PagedCache(NamedTuple):
     """The tensors of a paged K/V cache, all of the caller's (see dkv_paged_cache in dkv.h).
 
-    k_pages, v_pages  [n_pages, n_kv_heads, page_size, head_dim], bfloat16, float32 or float8_e4m3fn
+    k_pages, v_pages  [n_pages, n_kv_heads, page_size, head_dim], bfloat16, float32 or float8_e4m3fn; or of head_dim / 2
+                      float4_e2m1fn_x2, the lower dim of a byte in its lower bits
     page_table        [batch, max_pages] int32; entries outside [0, n_pages): no page
     seq_len           [batch] int32, positions of each sequence (paged_attn only)
-    k_scale, v_scale  [n_pages, n_kv_heads, page_size] float8_e8m0fnu, with float8_e4m3fn pages only: 2^-110 to 2^120, as paged_store
-                      writes them
+    k_scale, v_scale  float8_e8m0fnu, as paged_store writes them; with float8_e4m3fn pages [n_pages, n_kv_heads, page_size], 2^-110 to
+                      2^120; with float4_e2m1fn_x2 pages [n_pages, n_kv_heads, page_size, head_dim / 32], 2^-110 to 2^126, or NaN
     """
     k_pages: torch.Tensor
     v_pages: torch.Tensor
@@ -373,7 +375,7 @@ class PagedCache(NamedTuple):
 
 
 def paged_store(cache, k_new, v_new, positions, row_off=None):
-    """Write rows of new K and V to their positions, quantised where the cache holds e4m3: row r of sequence b, i.e.
+    """Write rows of new K and V to their positions, quantised where the cache holds e4m3 or e2m1: row r of sequence b, i.e.
     row_off[b] <= r < row_off[b + 1], goes to position positions[r]; without row_off, row r belongs to sequence r.
     k_new, v_new [rows, n_kv_heads, head_dim], bfloat16 or float32; the rows may be parts of longer ones."""
     _check(_marshal.paged_store(cache, k_new, v_new, positions, row_off))

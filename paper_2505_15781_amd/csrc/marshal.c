@@ -165,7 +165,7 @@ static paged_store_fn f_paged_store;
 static paged_load_fn f_paged_load;
 static paged_bytes_fn f_paged_bytes;
 static paged_attn_fn f_paged_attn;
-enum { T_BF16 = DKV_BF16, T_FP32 = DKV_FP32, T_E4M3 = DKV_E4M3, T_E8M0, T_I32, T_COUNT };
+enum { T_BF16 = DKV_BF16, T_FP32 = DKV_FP32, T_E4M3 = DKV_E4M3, T_E8M0, T_E2M1 = DKV_E2M1, T_I32, T_COUNT };
 static PyObject *dtypes[T_COUNT];
 static PyObject *s_dtype, *s_is_contiguous, *s_get_device, *s_stride, *s_current, *s_stream;
 static PyObject *place_of;        /* has _cuda_getDevice() and _cuda_getCurrentRawStream(device) */
@@ -228,22 +228,25 @@ static int look_cache(PyObject *o, dkv_paged_cache *c, int *device) {
     tensor_info k, v, x;
     if (look(t[0], &k)) return -1;
     if (k.n_dims != 4) return refuse("k_pages", "pages have four dimensions: pages, kv heads, slots, head_dim");
-    if (k.dtype < 0 || k.dtype > T_E4M3) return refuse("k_pages", "pages of this type are not supported");
+    const int four_bits = k.dtype == T_E2M1;
+    if (k.dtype < 0 || (k.dtype > T_E4M3 && !four_bits)) return refuse("k_pages", "pages of this type are not supported");
     if (!k.whole) return refuse("k_pages", "a contiguous tensor is expected");
     if (look_whole(t[1], "v_pages", k.dtype, 4, k.dims, k.device, &v)) return -1;
     if (look_whole(t[2], "page_table", T_I32, -2, NULL, k.device, &x)) return -1;
-    *c = (dkv_paged_cache){k.ptr, v.ptr, NULL, NULL, x.ptr, NULL, x.dims[0], k.dims[0], x.dims[1], k.dims[2], k.dims[1], k.dims[3], k.dtype};
+    if (four_bits && k.dims[3] > INT32_MAX / 2) return refuse("k_pages", "sizes do not fit 32 bits");
+    *c = (dkv_paged_cache){k.ptr, v.ptr, NULL, NULL, x.ptr, NULL, x.dims[0], k.dims[0], x.dims[1], k.dims[2], k.dims[1], four_bits ? 2 * k.dims[3] : k.dims[3], k.dtype};
     if (t[3] != Py_None) {
         if (look_whole(t[3], "seq_len", T_I32, 1, &c->batch, k.device, &x)) return -1;
         c->seq_len = x.ptr;
     }
-    if (k.dtype != T_E4M3) {
-        if (t[4] != Py_None || t[5] != Py_None) return refuse("k_scale, v_scale", "scales go with pages of float8_e4m3fn only");
+    if (k.dtype != T_E4M3 && !four_bits) {
+        if (t[4] != Py_None || t[5] != Py_None) return refuse("k_scale, v_scale", "scales go with pages of float8_e4m3fn and float4_e2m1fn_x2 only");
     } else {
-        if (t[4] == Py_None || t[5] == Py_None) return refuse("k_scale, v_scale", "pages of float8_e4m3fn need k_scale and v_scale");
-        if (look_whole(t[4], "k_scale", T_E8M0, 3, k.dims, k.device, &x)) return -1;
+        if (t[4] == Py_None || t[5] == Py_None) return refuse("k_scale, v_scale", "pages of float8_e4m3fn and float4_e2m1fn_x2 need k_scale and v_scale");
+        const int32_t dims[4] = {k.dims[0], k.dims[1], k.dims[2], k.dims[3] / 16};      /* e2m1: one for each 32 dims */
+        if (look_whole(t[4], "k_scale", T_E8M0, four_bits ? 4 : 3, dims, k.device, &x)) return -1;
         c->k_scale = x.ptr;
-        if (look_whole(t[5], "v_scale", T_E8M0, 3, k.dims, k.device, &x)) return -1;
+        if (look_whole(t[5], "v_scale", T_E8M0, four_bits ? 4 : 3, dims, k.device, &x)) return -1;
         c->v_scale = x.ptr;
     }
     *device = k.device;
@@ -391,10 +394,10 @@ static PyObject *py_paged_attn(PyObject *self, PyObject *const *a, Py_ssize_t n)
 }
 
 /* bind_paged(addresses of dkv_paged_store, _load, _attn_workspace_bytes, _attn, then the types bfloat16, float32, float8_e4m3fn,
- * float8_e8m0fnu, int32, and what tells the current device and stream) */
+ * float8_e8m0fnu, float4_e2m1fn_x2, int32, and what tells the current device and stream) */
 static PyObject *py_bind_paged(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     if (n != 5 + T_COUNT) {
-        PyErr_SetString(PyExc_TypeError, "four addresses, five types and a source of streams are expected");
+        PyErr_SetString(PyExc_TypeError, "four addresses, six types and a source of streams are expected");
         return NULL;
     }
     void *f[4];

@@ -40,9 +40,20 @@ struct Divisor {
 };
 
 typedef uint8_t e4m3_t;      // a code; its row's scale is a biased exponent
+struct e2m1_t {              // codes of two neighbouring dims, the lower one in the lower bits; 32 dims of a row share a scale
+    uint8_t pair;
+};
+template <typename C, typename D> struct SameType { static constexpr bool value = false; };
+template <typename C> struct SameType<C, C> { static constexpr bool value = true; };
+template <typename C> constexpr bool kE2M1 = SameType<C, e2m1_t>::value;
+// Of a row (a position, a K/V head): bytes, scales.
+template <typename C, int DH> constexpr int kRowBytes = kE2M1<C> ? DH / 2 : DH * (int)sizeof(C);
+template <typename C, int DH> constexpr int kRowScales = kE2M1<C> ? DH / 32 : SameType<C, e4m3_t>::value ? 1 : 0;
 
-// Value of a scale: a normal number for the exponents that a store writes (-110 to 120).
+// Value of a scale: a normal number for the exponents that a store writes (-110 to 120, e2m1 126). As the operand of a conversion of e2m1 codes
+// 255 means NaN; a factor has to be one.
 __device__ __forceinline__ float scale_value(uint8_t biased) { return __uint_as_float((uint32_t)biased << 23); }
+__device__ __forceinline__ float scale_factor(uint8_t biased) { return biased == 255 ? __uint_as_float(0x7fc00000u) : scale_value(biased); }
 
 // Sequence of row r: the number of i with row_off[i + 1] <= r, `batch` for rows behind the last sequence. Called by whole
 // wavefronts with r uniform; a lane per sequence, so that batches of up to 64 cost one load instead of a search's chain.
@@ -92,6 +103,22 @@ __device__ __forceinline__ f32x8 load8(const e4m3_t *p) {
         x[4 * i + 3] = hi[1];
     }
     return x;
+}
+// 4 codes, in the lower two bytes, times 1
+__device__ __forceinline__ f32x4 from_e2m1(uint32_t a) {
+    const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(a, 1.f, 0), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(a, 1.f, 1);
+    return f32x4{lo[0], lo[1], hi[0], hi[1]};
+}
+// 8 codes times a scale (see scale_value): exact
+__device__ __forceinline__ u32x4 bf16_of_e2m1(uint32_t a, float scale) {
+    return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, scale, 0)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, scale, 1)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, scale, 2)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, scale, 3))};
+}
+__device__ __forceinline__ f32x8 load8(const e2m1_t *p) {
+    const uint32_t a = *reinterpret_cast<const uint32_t *>(p);
+    return __builtin_shufflevector(from_e2m1(a), from_e2m1(a >> 16), 0, 1, 2, 3, 4, 5, 6, 7);
 }
 __device__ __forceinline__ void store8(float *p, f32x8 x) {
     *reinterpret_cast<f32x4_el *>(p) = __builtin_shufflevector(x, x, 0, 1, 2, 3);

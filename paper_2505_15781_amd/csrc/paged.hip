@@ -1,12 +1,15 @@
-// Paged K/V cache: writing rows into its pages, quantised where the cache holds 8 bits, reading them back, and the boundary
+// Paged K/V cache: writing rows into its pages, quantised where the cache holds 8 bits or 4, reading them back, and the boundary
 // of these and of the attention over it (paged_attn.hip).
 //
-// Quantising. A row (one position, one K/V head) shares a power-of-two scale 2^e. e4m3 is a floating format, so a power of
+// Quantising. A row (one position, one K/V head) of an e4m3 cache shares a power-of-two scale 2^e. e4m3 is a floating format, so a power of
 // two costs no precision against a scale that brings the largest magnitude to exactly 448: each element is rounded
 // once, to 4 significant bits, and x * 2^-e, code * 2^e are exact. In return the scale is 8 bits, scaled elements are exact in bf16
 // (attention multiplies them as they are), and what is stored does not depend on how a division rounds. e is the smallest exponent with
 // max |x| <= 448 * 2^e, from the bits of the maximum: with max |x| = m 2^E, m in [1, 2), it is E - 8, or E - 7 where m > 1.75.
 // At least -110: the smallest code, 2^-9, is then 2^-119, so that every held element is a normal number of fp32 and bf16.
+// e2m1 has codes up to 6 and one bit behind the leading one: a whole row under one scale would lose its small elements, so 32 dims share
+// one (OCP's microscaling format). e is E - 2, or E - 1 where m > 1.5: nothing is cut off, and each element is rounded once, to 2 significant
+// bits, or by 2^(e - 2). There is no code for NaN; a block with an infinity or a NaN has the scale 255, which makes all of it NaN.
 #include "paged.h"
 
 namespace {
@@ -21,9 +24,14 @@ __device__ __forceinline__ int scale_exponent(float amax) {
     const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u);
     return min(max(e, kLowestExponent), kHighestExponent);
 }
+constexpr int kHighestExponentE2M1 = 126;
+__device__ __forceinline__ int scale_exponent_e2m1(uint32_t bits) {        // of the largest magnitude
+    const int e = (int)(bits >> 23) - 127 - 2 + ((bits & 0x7fffffu) > 0x400000u);
+    return min(max(e, kLowestExponent), kHighestExponentE2M1);
+}
 
-// Elements of a lane: 16 bytes of what is written.
-template <typename W> constexpr int kPiece = 16 / (int)sizeof(W);
+// Elements of a lane: 16 bytes of what is written, or for e2m1 (4 bytes) of the bf16 rows that are read.
+template <typename W> constexpr int kPiece = kE2M1<W> ? 8 : 16 / (int)sizeof(W);
 template <int N> using Piece = float __attribute__((ext_vector_type(N)));
 
 __device__ __forceinline__ Piece<4> load_piece(const float *p, Piece<4> *) { return *reinterpret_cast<const f32x4_el *>(p); }
@@ -36,6 +44,7 @@ __device__ __forceinline__ Piece<4> load_piece(const e4m3_t *p, Piece<4> *) {
     const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(a, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(a, true);
     return Piece<4>{lo[0], lo[1], hi[0], hi[1]};
 }
+__device__ __forceinline__ Piece<4> load_piece(const e2m1_t *p, Piece<4> *) { return from_e2m1(*reinterpret_cast<const uint16_t *>(p)); }
 template <typename T> __device__ __forceinline__ Piece<8> load_piece(const T *p, Piece<8> *) { return load8(p); }
 template <typename T> __device__ __forceinline__ Piece<16> load_piece(const T *p, Piece<16> *) {
     return __builtin_shufflevector(load8(p), load8(p + 8), 0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15);
@@ -54,7 +63,15 @@ template <int LANES> __device__ __forceinline__ float row_max(float x) {
     return x;
 }
 
-// Writes the elements of a lane into the cache (e4m3: with the rest of the row in the lanes beside it).
+// The lane's `piece` of a row of the cache, and its scale.
+template <typename C, int DH> __device__ __forceinline__ const C *piece_of(const unsigned char *base, uint32_t row, int piece, int elements) {
+    return reinterpret_cast<const C *>(base + (size_t)row * kRowBytes<C, DH> + piece * elements * kRowBytes<C, DH> / DH);
+}
+template <typename C, int DH> __device__ __forceinline__ uint8_t *scale_of(uint8_t *base, uint32_t row, int piece, int elements) {
+    return base + (size_t)row * kRowScales<C, DH> + (kE2M1<C> ? piece * elements / 32 : 0);
+}
+
+// Writes the elements of a lane into the cache (e4m3, e2m1: with the rest of what shares the scale in the lanes beside it).
 template <int DH> __device__ __forceinline__ void put(bf16_t *row, uint8_t *, int piece, Piece<8> x) { store_piece(row + 8 * piece, x); }
 template <int DH> __device__ __forceinline__ void put(float *row, uint8_t *, int piece, Piece<4> x) { store_piece(row + 4 * piece, x); }
 template <int DH> __device__ __forceinline__ void put(e4m3_t *row, uint8_t *scale, int piece, Piece<16> x) {
@@ -76,6 +93,25 @@ template <int DH> __device__ __forceinline__ void put(e4m3_t *row, uint8_t *scal
     }
     *reinterpret_cast<u32x4 *>(row + 16 * piece) = codes;
     if (piece == 0) *scale = (uint8_t)(e + 127);
+}
+template <int DH> __device__ __forceinline__ void put(e2m1_t *row, uint8_t *scale, int piece, Piece<8> x) {
+    uint32_t most = 0;                                       // as bits: a NaN is more than an infinity, and that more than all numbers
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
+    auto other = [&](auto control) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)most, decltype(control)::value, 0xf, 0xf, true); };
+    most = max(most, other(Size<0xB1>{}));                   // lane ^ 1
+    most = max(most, other(Size<0x4E>{}));                   // lane ^ 2
+    const int e = scale_exponent_e2m1(most);
+    const float inv = __uint_as_float((uint32_t)(127 - e) << 23), top = e == kHighestExponentE2M1 ? 3.f : 6.f;
+    uint32_t codes = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = fminf(fmaxf(x[i] * inv, -top), top);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0], x[1], 1.f, 0);      // rounds to nearest, ties to the even code
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2], x[3], 1.f, 1);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[4], x[5], 1.f, 2);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[6], x[7], 1.f, 3);
+    *reinterpret_cast<uint32_t *>(row + 4 * piece) = codes;
+    if (piece % 4 == 0) *scale = most < 0x7f800000u ? (uint8_t)(e + 127) : 255;
 }
 
 // Which row a wavefront works on, and where that row's place in the cache is: N pieces of a lane, 64 apart; piece i of a row is head
@@ -111,7 +147,7 @@ __global__ __launch_bounds__(256) void paged_store_kernel(PagedCache c, const T 
     int page, slot;
     if (!w.place(c, positions, row_off, rows, page, slot) || page < 0 || w.first >= pieces) return;
     const uint32_t at = c.row(page, head, slot);
-    put<DH>(reinterpret_cast<C *>(is_v ? c.v : c.k) + (size_t)at * DH, (is_v ? c.vs : c.ks) + at, piece, x);
+    put<DH>(const_cast<C *>(piece_of<C, DH>(is_v ? c.v : c.k, at, 0, E)), scale_of<C, DH>(is_v ? c.vs : c.ks, at, piece, E), piece, x);
 }
 
 // A lane writes N times 16 bytes. Its loads are short where the cache is e4m3 (8 bytes for bf16 rows, 4 for fp32), and wait for the
@@ -134,15 +170,15 @@ __global__ __launch_bounds__(256) void paged_load_kernel(PagedCache c, T *__rest
     for (int u = 0; u < N; ++u) {
         const int i = min(w.first + 64 * u, pieces - 1), is_v = i / P % 2;
         const uint32_t at = c.row(max(page, 0), i / (2 * P), slot);
-        x[u] = load_piece(reinterpret_cast<const C *>(is_v ? c.v : c.k) + (size_t)at * DH + E * (i % P), (Piece<E> *)nullptr);
+        x[u] = load_piece(piece_of<C, DH>(is_v ? c.v : c.k, at, i % P, E), (Piece<E> *)nullptr);
         scale[u] = 1.f;
-        if constexpr (sizeof(C) == 1) scale[u] = scale_value((is_v ? c.vs : c.ks)[at]);
+        if constexpr (kRowScales<C, DH> > 0) scale[u] = scale_factor(*scale_of<C, DH>(is_v ? c.vs : c.ks, at, i % P, E));
     }
 #pragma unroll
     for (int u = 0; u < N; ++u) {
         const int i = w.first + 64 * u;
         if (i >= pieces) return;
-        if constexpr (sizeof(C) == 1) x[u] *= scale[u];
+        if constexpr (kRowScales<C, DH> > 0) x[u] *= scale[u];
         if (page < 0) x[u] = 0.f;
         store_piece((i / P % 2 ? v_out : k_out) + ((size_t)w.r * c.n_kv_heads + i / (2 * P)) * DH + E * (i % P), x[u]);
     }
@@ -154,7 +190,10 @@ template <typename F> int with_types(int dtype, int cache_dtype, int head_dim, F
         return head_dim == 32 ? f(t, c, Size<32>{}) : head_dim == 64 ? f(t, c, Size<64>{}) : f(t, c, Size<128>{});
     };
     auto caches = [&](auto t) {
-        return cache_dtype == DKV_BF16 ? heads(t, Type<bf16_t>{}) : cache_dtype == DKV_FP32 ? heads(t, Type<float>{}) : heads(t, Type<e4m3_t>{});
+        return cache_dtype == DKV_BF16   ? heads(t, Type<bf16_t>{})
+               : cache_dtype == DKV_FP32 ? heads(t, Type<float>{})
+               : cache_dtype == DKV_E4M3 ? heads(t, Type<e4m3_t>{})
+                                         : heads(t, Type<e2m1_t>{});
     };
     return dtype == DKV_BF16 ? caches(Type<bf16_t>{}) : caches(Type<float>{});
 }
@@ -163,8 +202,9 @@ template <typename F> int with_types(int dtype, int cache_dtype, int head_dim, F
 
 int dkv_paged_view(const dkv_paged_cache *c, PagedCache &view) {
     if (!c || !c->k_pages || !c->v_pages || !c->page_table) { dkv_set_error("null argument"); return DKV_E_INVALID_ARG; }
-    if (c->dtype != DKV_BF16 && c->dtype != DKV_FP32 && c->dtype != DKV_E4M3) { dkv_set_error("unknown cache dtype %d", c->dtype); return DKV_E_INVALID_ARG; }
-    if (c->dtype == DKV_E4M3 && (!c->k_scale || !c->v_scale)) { dkv_set_error("an e4m3 cache needs k_scale and v_scale"); return DKV_E_INVALID_ARG; }
+    const bool scaled = c->dtype == DKV_E4M3 || c->dtype == DKV_E2M1;
+    if (c->dtype != DKV_BF16 && c->dtype != DKV_FP32 && !scaled) { dkv_set_error("unknown cache dtype %d", c->dtype); return DKV_E_INVALID_ARG; }
+    if (scaled && (!c->k_scale || !c->v_scale)) { dkv_set_error("an e4m3 or e2m1 cache needs k_scale and v_scale"); return DKV_E_INVALID_ARG; }
     if (c->batch < 1 || c->n_pages < 1 || c->max_pages < 1 || c->n_kv_heads < 1) { dkv_set_error("inconsistent sizes"); return DKV_E_INVALID_ARG; }
     if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128) { dkv_set_error("head_dim %d not supported (32, 64, 128)", c->head_dim); return DKV_E_UNSUPPORTED; }
     if (c->page_size < 16 || c->page_size > 65536 || (c->page_size & (c->page_size - 1))) {
@@ -196,7 +236,7 @@ int rows_call(const dkv_paged_cache *cache, PagedCache &view, const void *k, con
     return DKV_OK;
 }
 int64_t row_pieces(const dkv_paged_cache &c, int written) {
-    return 2 * (int64_t)(c.head_dim * (written == DKV_BF16 ? 2 : written == DKV_FP32 ? 4 : 1) / 16) * c.n_kv_heads;
+    return 2 * (int64_t)(written == DKV_E2M1 ? c.head_dim / 8 : c.head_dim * (written == DKV_BF16 ? 2 : written == DKV_FP32 ? 4 : 1) / 16) * c.n_kv_heads;
 }
 template <typename F> int rows_launch(const dkv_paged_cache &c, int written, int n, int rows, F f) {
     const int64_t waves = (row_pieces(c, written) + 64 * n - 1) / (64 * n), groups = (waves * rows + 3) / 4;
@@ -228,7 +268,7 @@ extern "C" int dkv_paged_load(const dkv_paged_cache *cache, void *k_out, void *v
     PagedCache c;
     const int rc = rows_call(cache, c, k_out, v_out, positions, row_off, rows, dtype);
     if (rc) return rc;
-    const int n = cache->dtype == DKV_E4M3 && rows * ((row_pieces(*cache, dtype) + 255) / 256) >= 4096 ? 4 : 1;
+    const int n = (cache->dtype == DKV_E4M3 || cache->dtype == DKV_E2M1) && rows * ((row_pieces(*cache, dtype) + 255) / 256) >= 4096 ? 4 : 1;
     return rows_launch(*cache, dtype, n, rows, [&](unsigned groups, Divisor waves) {
         return with_types(dtype, cache->dtype, cache->head_dim, [&](auto t, auto ct, auto dh) {
             typedef typename decltype(t)::type T;
@@ -239,7 +279,7 @@ extern "C" int dkv_paged_load(const dkv_paged_cache *cache, void *k_out, void *v
                 DKV_LAUNCH_CHECK();
                 return DKV_OK;
             };
-            if constexpr (sizeof(C) == 1) return n == 4 ? launch(Size<4>{}) : launch(Size<1>{});
+            if constexpr (kRowScales<C, decltype(dh)::value> > 0) return n == 4 ? launch(Size<4>{}) : launch(Size<1>{});
             else return launch(Size<1>{});
         });
     });

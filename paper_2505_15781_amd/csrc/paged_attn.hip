@@ -269,7 +269,7 @@ int dkv_paged_attn_plan(const dkv_paged_cache *cache, PagedCache &view, PagedAtt
         dkv_set_error("inconsistent sizes"); return DKV_E_INVALID_ARG;
     }
     if (dtype != DKV_BF16 && dtype != DKV_FP32) { dkv_set_error("unknown dtype"); return DKV_E_INVALID_ARG; }
-    if (cache->dtype != dtype && cache->dtype != DKV_E4M3) { dkv_set_error("rows of dtype %d do not read a cache of dtype %d", dtype, cache->dtype); return DKV_E_UNSUPPORTED; }
+    if (cache->dtype != dtype && cache->dtype != DKV_E4M3 && cache->dtype != DKV_E2M1) { dkv_set_error("rows of dtype %d do not read a cache of dtype %d", dtype, cache->dtype); return DKV_E_UNSUPPORTED; }
     if ((int64_t)rows * n_q_heads < 1 << 24 && (int64_t)cache->batch * cache->n_kv_heads < 1 << 22 &&
         (int64_t)cache->batch * cache->max_pages * cache->page_size <= 1ll << 35) {
         plan = make_plan(view, n_q_heads, rows, max_rows_per_seq, dtype, cache->head_dim);
@@ -308,8 +308,10 @@ extern "C" int dkv_paged_attn(const dkv_paged_cache *cache, const void *q, int64
     const int max_rows = max_rows_per_seq < rows ? max_rows_per_seq : rows;
     auto launch = [&](auto f) { return f(dh, c, p, q, q_stride, row_off, out, workspace, rows, max_rows, n_q_heads, s); };
     if (dtype == DKV_BF16)
-        return cache->dtype == DKV_BF16 ? launch([](auto... a) { return launch_attn<bf16_t, bf16_t>(a...); })
-                                        : launch([](auto... a) { return launch_attn<bf16_t, e4m3_t>(a...); });
-    return cache->dtype == DKV_FP32 ? launch([](auto... a) { return launch_attn<float, float>(a...); })
-                                    : launch([](auto... a) { return launch_attn<float, e4m3_t>(a...); });
+        return cache->dtype == DKV_BF16   ? launch([](auto... a) { return launch_attn<bf16_t, bf16_t>(a...); })
+               : cache->dtype == DKV_E4M3 ? launch([](auto... a) { return launch_attn<bf16_t, e4m3_t>(a...); })
+                                          : launch([](auto... a) { return launch_attn<bf16_t, e2m1_t>(a...); });
+    return cache->dtype == DKV_FP32   ? launch([](auto... a) { return launch_attn<float, float>(a...); })
+           : cache->dtype == DKV_E4M3 ? launch([](auto... a) { return launch_attn<float, e4m3_t>(a...); })
+                                      : launch([](auto... a) { return launch_attn<float, e2m1_t>(a...); });
 }

@@ -125,6 +125,8 @@ __device__ __forceinline__ bool find_slice(const PagedCache &c, const int *row_o
     return false;
 }
 
+template <int BYTES> struct PieceBits { typedef u32x4 type; };
+template <> struct PieceBits<8> { typedef u32x2 type; };
 template <typename T, int DH> struct SplitSmem {
     static constexpr int K_STRIDE = DH * (int)sizeof(T) + 16;                               // bytes per row; the rest spreads
     static constexpr int V_STRIDE = DH * (int)sizeof(T) + (sizeof(T) == 2 ? 32 : 16);       // the reads over the banks
@@ -132,7 +134,7 @@ template <typename T, int DH> struct SplitSmem {
     static constexpr int WAVE_BYTES = PKT * (K_STRIDE + V_STRIDE);
 };
 
-// A 16-byte piece of a row as it is stored -> elements of T in LDS.
+// A piece of a row as it is stored -> elements of T in LDS.
 __device__ __forceinline__ void stage(bf16_t *dst, const bf16_t *, u32x4 x, float) { *reinterpret_cast<u32x4 *>(dst) = x; }
 __device__ __forceinline__ void stage(float *dst, const float *, u32x4 x, float) { *reinterpret_cast<u32x4 *>(dst) = x; }
 __device__ __forceinline__ void stage(bf16_t *dst, const e4m3_t *, u32x4 x, float scale) {
@@ -153,6 +155,26 @@ __device__ __forceinline__ void stage(float *dst, const e4m3_t *, u32x4 x, float
         const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(x[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(x[i], true);
         *reinterpret_cast<f32x4 *>(dst + 4 * i) = f32x4{lo[0] * scale, lo[1] * scale, hi[0] * scale, hi[1] * scale};
     }
+}
+
+__device__ __forceinline__ void stage(bf16_t *dst, const e2m1_t *, u32x4 x, float scale) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4 *>(dst + 8 * i) = bf16_of_e2m1(x[i], scale);
+}
+__device__ __forceinline__ void stage(bf16_t *dst, const e2m1_t *, u32x2 x, float scale) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) *reinterpret_cast<u32x4 *>(dst + 8 * i) = bf16_of_e2m1(x[i], scale);
+}
+template <typename V> __device__ __forceinline__ void stage(float *dst, const e2m1_t *, V x, float scale) {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(V) / 4); ++i)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            // the instruction's choice of a byte is a constant
+            const auto lo = k ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[i], scale, 2) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[i], scale, 0);
+            const auto hi = k ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[i], scale, 3) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[i], scale, 1);
+            *reinterpret_cast<f32x4 *>(dst + 8 * i + 4 * k) = f32x4{lo[0], lo[1], hi[0], hi[1]};
+        }
 }
 
 // softmax_step with probabilities that stay in fp32 (in st), and their sum over this lane's keys in l_acc[0]
@@ -216,9 +238,13 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
 
     // the page of such an entry; -1: none, or behind the end
     auto page_of = [&](int entry, int j0) { return first_key(t_begin, j0) < len && (unsigned)entry < (unsigned)c.n_pages ? entry : -1; };
-    constexpr int ROW = DH * (int)sizeof(C), LPR = ROW / 16, RPI = 64 / LPR, N = PKT / RPI;    // lanes per row, rows per load, loads
-    u32x4 kreg[N], vreg[N];
+    // bytes of a row, of a lane's piece of it (16, or what spreads a tile over all lanes), lanes per row, rows per load, loads
+    constexpr int ROW = kRowBytes<C, DH>, PIECE = ROW * PKT < 1024 ? ROW * PKT / 64 : 16, LPR = ROW / PIECE, RPI = 64 / LPR, N = PKT / RPI;
+    constexpr int PER = PIECE * DH / ROW;     // elements of a piece
+    typedef typename PieceBits<PIECE>::type Bits;
+    Bits kreg[N], vreg[N];
     uint32_t scales = 0;                      // e4m3: lane i has the scale of K row i, or of V row i - 32, as a float
+    uint32_t k_scales[N], v_scales[N];        // e2m1: those of this lane's pieces
     int pages = -1, seen0 = 0, seen1 = 0;     // seen: keys of each half that are attended to
     auto load_tile = [&](int t, int j) {
         const int id0 = __builtin_amdgcn_readlane(pages, 2 * (j & 31)), id1 = __builtin_amdgcn_readlane(pages, 2 * (j & 31) + 1);
@@ -226,32 +252,46 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
         seen0 = id0 < 0 ? 0 : min(16, len - key);
         seen1 = id1 < 0 ? 0 : min(16, len - key - 16);
         const uint32_t row0 = c.row(max(id0, 0), kvh, slot), row1 = c.row(max(id1, 0), kvh, slot1);
-        auto fetch = [&](u32x4 (&reg)[N], const unsigned char *base) {
+        auto fetch = [&](Bits (&reg)[N], const unsigned char *base) {
             const unsigned char *p0 = base + (size_t)row0 * ROW, *p1 = base + (size_t)row1 * ROW;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const unsigned char *p;
-                if constexpr (RPI > 16) p = (lane < 32 ? p0 : p1) + (lane / LPR % 16) * ROW + lane % LPR * 16;
-                else p = (i * RPI < 16 ? p0 : p1) + i * RPI % 16 * ROW + (lane / LPR) * ROW + lane % LPR * 16;
-                reg[i] = ONCE ? __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)) : *reinterpret_cast<const u32x4 *>(p);
+                if constexpr (RPI > 16) p = (lane < 32 ? p0 : p1) + (lane / LPR % 16) * ROW + lane % LPR * PIECE;
+                else p = (i * RPI < 16 ? p0 : p1) + i * RPI % 16 * ROW + (lane / LPR) * ROW + lane % LPR * PIECE;
+                reg[i] = ONCE ? __builtin_nontemporal_load(reinterpret_cast<const Bits *>(p)) : *reinterpret_cast<const Bits *>(p);
             }
         };
         fetch(kreg, c.k);
         fetch(vreg, c.v);
-        if constexpr (sizeof(C) == 1) scales = (uint32_t)(lane < 32 ? c.ks : c.vs)[(lane & 16 ? row1 : row0) + (lane & 15)] << 23;
+        if constexpr (kE2M1<C>) {
+            constexpr int S = kRowScales<C, DH>;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int row = i * RPI + lane / LPR;
+                const size_t at = (size_t)(row < 16 ? row0 : row1) * S + (row & 15) * S + lane % LPR * PER / 32;
+                k_scales[i] = c.ks[at];
+                v_scales[i] = c.vs[at];
+            }
+        } else if constexpr (sizeof(C) == 1) {
+            scales = (uint32_t)(lane < 32 ? c.ks : c.vs)[(lane & 16 ? row1 : row0) + (lane & 15)] << 23;
+        }
     };
     auto store_tile = [&]() {
         const bool masked = seen0 < 16 || seen1 < 16;                 // uniform
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int row = i * RPI + lane / LPR, el = lane % LPR * (16 / (int)sizeof(C));
+            const int row = i * RPI + lane / LPR, el = lane % LPR * PER;
             float k_scale = 1.f, v_scale = 1.f;
-            if constexpr (sizeof(C) == 1) {
+            if constexpr (kE2M1<C>) {
+                k_scale = scale_value(k_scales[i]);
+                v_scale = scale_value(v_scales[i]);
+            } else if constexpr (sizeof(C) == 1) {
                 k_scale = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(row << 2, (int)scales));
                 v_scale = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute((32 + row) << 2, (int)scales));
             }
             if (masked && (row & 15) >= (row < 16 ? seen0 : seen1)) {
-                vreg[i] = u32x4{0, 0, 0, 0};
+                vreg[i] = Bits{};
                 v_scale = 1.f;
             }
             stage(reinterpret_cast<T *>(ksm + row * SM::K_STRIDE) + el, (const C *)nullptr, kreg[i], k_scale);

@@ -99,7 +99,7 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
     int2 *__restrict__ meta, float *__restrict__ partial, SlicePlan plan, int max_rows, GroupMap map, Divisor heads, Divisor G, int units,
     float scale_log2e) {
     constexpr int NW = 4, ROW = DH * 2, KT2 = 64, TILE = KT2 * ROW;     // bytes of an LDS row, of a K or V tile
-    constexpr bool E4M3 = sizeof(C) == 1;
+    constexpr bool CODES = sizeof(C) == 1;                              // e4m3 or e2m1
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_all[];
 
     // KS groups of four wavefronts, in LDS stages of their own
@@ -194,45 +194,55 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
             }
         }
     };
-    // e4m3. Load i of a wavefront has rows RPF (4 i + wave) + [0, RPF); lane -> row lane / LPF, elements 16 (lane % LPF) + [0, 16).
-    constexpr int LPF = DH / 16, RPF = 64 / LPF, FETCHES = KT2 / (RPF * NW);
+    // e4m3, e2m1. Load i of a wavefront has rows RPF (4 i + wave) + [0, RPF); lane -> row lane / LPF, elements PER (lane % LPF) + [0, PER).
+    constexpr int LPF = kE2M1<C> ? 4 : DH / 16, PER = DH / LPF, RPF = 64 / LPF, FETCHES = KT2 / (RPF * NW);
+    constexpr int SCALES = kE2M1<C> ? DH / 32 : 1, BYTES = kRowBytes<C, DH>;
+    typedef typename PieceBits<BYTES / LPF>::type Bits;
     const int f_row = (RPF * wave + lane / LPF) % 16;
     auto f_group = [&](const WideTile &x, int i) { return RPF == 16 ? (wave & 2 ? (wave & 1 ? x.row[3] : x.row[2]) : (wave & 1 ? x.row[1] : x.row[0]))
                                                                     : (wave >> 1 ? x.row[2 * i + 1] : x.row[2 * i]); };
-    u32x4 kreg[FETCHES], vreg[FETCHES];
+    Bits kreg[FETCHES], vreg[FETCHES];
     uint32_t k_scale[FETCHES], v_scale[FETCHES];
-    auto fetch = [&](u32x4 (&reg)[FETCHES], uint32_t (&scale)[FETCHES], const unsigned char *base, const uint8_t *scales, const WideTile &x) {
+    auto fetch = [&](Bits (&reg)[FETCHES], uint32_t (&scale)[FETCHES], const unsigned char *base, const uint8_t *scales, const WideTile &x) {
 #pragma unroll
         for (int i = 0; i < FETCHES; ++i) {
             const size_t row = f_group(x, i);                         // uniform
-            reg[i] = *reinterpret_cast<const u32x4 *>(base + row * DH + (uint32_t)(f_row * DH + 16 * (lane % LPF)));
-            scale[i] = (scales + row)[(uint32_t)f_row];
+            reg[i] = *reinterpret_cast<const Bits *>(base + row * BYTES + (uint32_t)(f_row * BYTES + BYTES / LPF * (lane % LPF)));
+            scale[i] = (scales + row * SCALES)[(uint32_t)(f_row * SCALES + (kE2M1<C> ? lane % LPF * PER / 32 : 0))];
         }
     };
-    auto convert = [&](const u32x4 (&reg)[FETCHES], const uint32_t (&scale)[FETCHES], int tile_pages, int t, uint32_t dst) {
+    auto convert = [&](const Bits (&reg)[FETCHES], const uint32_t (&scale)[FETCHES], int tile_pages, int t, uint32_t dst) {
         const bool all = whole(t, tile_pages);                        // uniform
 #pragma unroll
         for (int i = 0; i < FETCHES; ++i) {
             const int row = RPF * (NW * i + wave) + lane / LPF, sw = wide_swizzle<DH>(row);
             const float s = __uint_as_float(scale[i] << 23);
-            u32x4 y[2];
+            u32x4 y[PER / 8];
+            if constexpr (kE2M1<C>) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                y[e >> 1][2 * (e & 1)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(reg[i][e], s, false));
-                y[e >> 1][2 * (e & 1) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(reg[i][e], s, true));
+                for (int e = 0; e < PER / 8; ++e) y[e] = bf16_of_e2m1(reg[i][e], s);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    y[e >> 1][2 * (e & 1)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(reg[i][e], s, false));
+                    y[e >> 1][2 * (e & 1) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(reg[i][e], s, true));
+                }
             }
-            if (!all && f_row >= there(t, tile_pages, RPF == 16 ? wave : 2 * i + (wave >> 1))) y[0] = y[1] = u32x4{0, 0, 0, 0};
+            if (!all && f_row >= there(t, tile_pages, RPF == 16 ? wave : 2 * i + (wave >> 1))) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-                *reinterpret_cast<u32x4 *>(smem_raw + dst + row * ROW + (((2 * (lane % LPF) + e) ^ sw) << 4)) = y[e];
+                for (int e = 0; e < PER / 8; ++e) y[e] = u32x4{0, 0, 0, 0};
+            }
+#pragma unroll
+            for (int e = 0; e < PER / 8; ++e)
+                *reinterpret_cast<u32x4 *>(smem_raw + dst + row * ROW + (((PER / 8 * (lane % LPF) + e) ^ sw) << 4)) = y[e];
         }
     };
-    // pages of the tiles t, t + 1, t + 2 (of the last ones: of some tile), and where tile t + 1 (bf16) or t + 2 (e4m3) is
+    // pages of the tiles t, t + 1, t + 2 (of the last ones: of some tile), and where tile t + 1 (bf16) or t + 2 (codes) is
     int pages_0, pages_1, pages_2;
     WideTile x = find(0), ahead = x;
     pages_0 = pages_1 = pages_2 = x.pages;
-    if constexpr (E4M3) {                        // all loads at once: K0 V0 K1, and V1 K2 for the loop
-        u32x4 k0[FETCHES], v0[FETCHES], k1[FETCHES];
+    if constexpr (CODES) {                        // all loads at once: K0 V0 K1, and V1 K2 for the loop
+        Bits k0[FETCHES], v0[FETCHES], k1[FETCHES];
         uint32_t k0_scale[FETCHES], v0_scale[FETCHES], k1_scale[FETCHES];
         fetch(k0, k0_scale, c.k, c.ks, x);
         fetch(v0, v0_scale, c.v, c.vs, x);
@@ -344,7 +354,7 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
     // is as exact as what dkv_attn_update reads (the reference that lags: 8 sequences x 32 heads, 512 rows, 1024 keys 98 us instead of 105).
     // The probabilities of the half tile before still wait for their product: the output is rescaled to the new reference
     // only behind that product, at the next call.
-    constexpr float LAG = E4M3 ? 8.f : 0.f;
+    constexpr float LAG = CODES ? 8.f : 0.f;
     auto maximum = [&](f32x16 &st, int t, int half, int tile_pages) {
         rescale();
         if (!whole(t, tile_pages)) {                                   // uniform
@@ -390,7 +400,7 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
         }
         // behind the barrier K(t + 1) and V(t) have landed for everybody, and everybody is done with K(t) and V(t - 1)
         tile_barrier();
-        if constexpr (E4M3) {
+        if constexpr (CODES) {
             if (t + 2 < n_tiles) convert(kreg, k_scale, pages_2, t + 2, S * TILE);
             if (t + 1 < n_tiles) convert(vreg, v_scale, pages_1, t + 1, (2 + (S ^ 1)) * TILE);
             pages_0 = pages_1;
