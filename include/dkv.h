@@ -342,6 +342,65 @@ int dkv_paged_attn(const dkv_paged_cache *cache, const void *q, int64_t q_stride
                    int32_t rows, int32_t max_rows_per_seq, int32_t n_q_heads, int32_t dtype, void *workspace,
                    size_t workspace_bytes, void *stream);
 
+/* Page tables that follow the lengths of their sequences. One set of tables serves the caches of all layers.
+ *   page_table (dev) [batch][max_pages], seq_len (dev) [batch]: as in dkv_paged_cache
+ *   free_pages (dev) [n_pages]: a ring of the numbers of the free pages; free_at (dev) [2]: the place of the first of them, and how many
+ *                    there are. A cache without sequences has free_pages = 0 .. n_pages - 1, free_at = {0, n_pages} and seq_len = 0.
+ * page_size, max_pages as in dkv_paged_cache; at most 2^30 pages and 2^20 sequences. Nothing is kept by a call. */
+typedef struct {
+    int32_t *page_table, *seq_len, *free_pages, *free_at;
+    int32_t batch, n_pages, max_pages, page_size;
+} dkv_paged_tables;
+
+/* Give the sequences new lengths (dev) [batch]; a length below zero or beyond the table leaves its sequence as it is.
+ * A sequence that gets longer takes pages for the positions behind its last page from the front of the ring, the first sequence first. They are those that were free
+ * before the call: what it gives back can be taken by the next one. From the first sequence on for which they do not last, or the rows below do not, no sequence
+ * gets longer; seq_len (and row_off) say which have.
+ * A sequence that gets shorter gives the pages behind its new length back, to the end of the ring in the order of sequences and positions;
+ * their entries become -1. (Entries that name no page are passed over. No two sequences may share what one of them gives back.)
+ * Where row_off is not null the new positions are listed, as dkv_paged_store, dkv_rope and dkv_paged_attn take them:
+ *   row_off (dev) [batch + 1]; positions (dev, nullable) [rows]; slots (dev, nullable) [rows]: page * page_size + slot of the position, -1 where
+ *   the table names no page (a page given back before is not replaced while its sequence goes on)
+ * Entries of positions and slots from row_off[batch] on are left as they are. rows is at most 2^30.
+ * workspace (dev), 16-byte aligned, of dkv_paged_resize_workspace_bytes(batch) bytes; calls that may overlap need one each. Results do not depend
+ * on timing. Tables, lengths and ring are read and changed on the device, so a captured call follows them. */
+size_t dkv_paged_resize_workspace_bytes(int32_t batch);
+int dkv_paged_resize(const dkv_paged_tables *tables, const int32_t *lengths, int32_t *row_off, int32_t *positions, int64_t *slots,
+                     int32_t rows, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Rotary positions: each pair (a, b) of the first rot_dim dims of a head becomes scale * (a cos t - b sin t, b cos t + a sin t), t = position * freq[i],
+ * pair i being the dims i and i + rot_dim / 2, or where `interleaved` 2 i and 2 i + 1. head_dim 32, 64 or 128; rot_dim even, 2 to head_dim; freq in
+ * radians, rot_dim / 2 of them. Host memory, which dkv_rope_init fills and a caller may fill otherwise. */
+typedef struct {
+    int32_t head_dim, rot_dim, interleaved;
+    float scale;
+    double freq[64];
+} dkv_rope_desc;
+
+/* freq[i] = f = theta^(-2 i / rot_dim) and scale = 1, or, for longer contexts than a model was trained on:
+ *   DKV_ROPE_LINEAR  f / factor
+ *   DKV_ROPE_BASE    f of a larger base, theta * factor^(rot_dim / (rot_dim - 2)): the last pair is stretched by `factor`, the first not
+ *   DKV_ROPE_PARTS   f * y + f / factor * (1 - y) with y = (original f / 2 pi - slow) / (fast - slow) within [0, 1]: pairs that turn at least
+ *                    `fast` times over `original` positions stay, those that turn at most `slow` times are stretched; scale = 0.1 ln(factor) + 1
+ * original, slow and fast are read for DKV_ROPE_PARTS only (usual: slow 1, fast 32), factor not for DKV_ROPE_NONE. */
+#define DKV_ROPE_NONE   0
+#define DKV_ROPE_LINEAR 1
+#define DKV_ROPE_BASE   2
+#define DKV_ROPE_PARTS  3
+int dkv_rope_init(dkv_rope_desc *rope, int32_t head_dim, int32_t rot_dim, int32_t interleaved, double theta, int32_t scaling,
+                  double factor, double original, double slow, double fast);
+
+/* Rotate the rows of q and k by their positions:
+ *   q, k (dev) [rows] rows of [n_q_heads][head_dim] and [n_k_heads][head_dim], `q_stride` and `k_stride` elements apart (at least a row);
+ *     q_out, k_out the same with strides of their own: the inputs themselves (then with their stride), or memory that overlaps neither input.
+ *     n_q_heads or n_k_heads may be 0. Dims from rot_dim on are copied. Elements of `dtype` (DKV_BF16 or DKV_FP32), rounded once.
+ *   positions (dev) [rows]; row_off (dev, nullable) [batch + 1]: rows from row_off[batch] on are left as they are
+ * `inverse`: t = -position * freq[i], with the same scale: the gradient of q and k from that of q_out and k_out.
+ * Angles are formed in 64 bits, so that far positions lose nothing. */
+int dkv_rope(const dkv_rope_desc *rope, const void *q, int64_t q_stride, void *q_out, int64_t q_out_stride, int32_t n_q_heads,
+             const void *k, int64_t k_stride, void *k_out, int64_t k_out_stride, int32_t n_k_heads, const int32_t *positions,
+             const int32_t *row_off, int32_t batch, int32_t rows, int32_t dtype, int32_t inverse, void *stream);
+
 /* y[M, N] (fp32, dev) = x[M, K] * w[N, K]^T with x, w of `dtype` (dev): the projection kernel of
  * the path on its own, for parity tests and roofline measurements. workspace as returned by
  * dkv_gemm_workspace_bytes. */

@@ -5,7 +5,8 @@ The binding (and with it libdkv.so) is loaded on first use of one of the names b
 """
 _BINDING_NAMES = ("lib", "DkvError", "DkvRun", "attn_update", "attn_update_static", "attn_update_workspace_bytes",
                   "gemm", "GEMM_KINDS", "concat_reorder", "BF16", "FP32", "E4M3", "E2M1", "last_error", "PagedCache", "paged_store",
-                  "paged_load", "paged_attn", "paged_attn_workspace_bytes")
+                  "paged_load", "paged_attn", "paged_attn_workspace_bytes", "PagedTables", "paged_resize",
+                  "paged_resize_workspace_bytes", "Rope", "rope")
 
 
 def __getattr__(name):

@@ -95,6 +95,22 @@ lib.dkv_paged_load.argtypes = [C.POINTER(PagedCacheDesc), c_vp, c_vp, c_vp, c_vp
 lib.dkv_paged_attn_workspace_bytes.restype = c_sz
 lib.dkv_paged_attn_workspace_bytes.argtypes = [C.POINTER(PagedCacheDesc), c_i32, c_i32, c_i32, c_i32]
 lib.dkv_paged_attn.argtypes = [C.POINTER(PagedCacheDesc), c_vp, C.c_int64, c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_vp, c_sz, c_vp]
+
+
+class PagedTablesDesc(C.Structure):
+    _fields_ = [(n, c_vp) for n in ("page_table", "seq_len", "free_pages", "free_at")] + \
+               [(n, c_i32) for n in ("batch", "n_pages", "max_pages", "page_size")]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [(n, c_i32) for n in ("head_dim", "rot_dim", "interleaved")] + [("scale", c_f32), ("freq", C.c_double * 64)]
+
+
+lib.dkv_paged_resize_workspace_bytes.restype = c_sz
+lib.dkv_paged_resize_workspace_bytes.argtypes = [c_i32]
+lib.dkv_paged_resize.argtypes = [C.POINTER(PagedTablesDesc), c_vp, c_vp, c_vp, c_vp, c_i32, c_vp, c_sz, c_vp]
+lib.dkv_rope_init.argtypes = [C.POINTER(RopeDesc), c_i32, c_i32, c_i32, C.c_double, c_i32, C.c_double, C.c_double, C.c_double, C.c_double]
+lib.dkv_rope.argtypes = [C.POINTER(RopeDesc)] + ([c_vp, C.c_int64] * 2 + [c_i32]) * 2 + [c_vp, c_vp] + [c_i32] * 4 + [c_vp]
 lib.dkv_peak_copy.argtypes = [c_vp, c_vp, c_sz, c_vp]
 lib.dkv_peak_read.argtypes = [c_vp, c_vp, c_sz, c_vp]
 lib.dkv_peak_mfma.argtypes = [c_vp, c_i32, C.POINTER(C.c_double), c_vp]
@@ -350,9 +366,9 @@ class _Streams:
 
 
 _marshal.bind_paged(*(C.cast(f, c_vp).value for f in (lib.dkv_paged_store, lib.dkv_paged_load, lib.dkv_paged_attn_workspace_bytes,
-                                                      lib.dkv_paged_attn)),
+                                                      lib.dkv_paged_attn, lib.dkv_paged_resize, lib.dkv_rope)),
                     torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.float8_e8m0fnu,
-                    getattr(torch, "float4_e2m1fn_x2", None), torch.int32,
+                    getattr(torch, "float4_e2m1fn_x2", None), torch.int32, torch.int64,
                     torch._C if _raw_stream is not None and hasattr(torch._C, "_cuda_getDevice") else _Streams)
 
 
@@ -397,6 +413,74 @@ def paged_attn(cache, q, row_off, out, max_rows_per_seq, workspace):
     page) into `out`; row_off as in paged_store (None: one row per sequence). max_rows_per_seq bounds the rows of any one
     sequence, and q has at most that many for each; workspace: a tensor of paged_attn_workspace_bytes bytes, one for each call that may overlap."""
     _check(_marshal.paged_attn(cache, q, row_off, out, max_rows_per_seq, workspace))
+
+
+class PagedTables(NamedTuple):
+    """The page tables of a batch and its free pages, all of the caller's (see dkv_paged_tables in dkv.h).
+
+    page_table  [batch, max_pages] int32, seq_len [batch] int32: those of a PagedCache, or of the caches of all layers
+    free_pages  [n_pages] int32, a ring of the numbers of free pages
+    free_at     [2] int32: the place of the first free page in it, and how many there are (at first 0 and n_pages, with all numbers in the ring)
+    """
+    page_table: torch.Tensor
+    seq_len: torch.Tensor
+    free_pages: torch.Tensor
+    free_at: torch.Tensor
+    page_size: int
+
+
+def paged_resize_workspace_bytes(batch):
+    """Bytes of workspace that paged_resize needs for this many sequences (0 where it would refuse them)."""
+    return lib.dkv_paged_resize_workspace_bytes(batch)
+
+
+def paged_resize(tables, lengths, workspace, row_off=None, positions=None, slots=None):
+    """Give the sequences new lengths [batch] int32 (below zero: as they are): sequences that get longer take pages from the front of the ring of free
+    ones, the first sequence first, as long as these and the rows of the lists last; those that get shorter give theirs back to its end.
+    tables.seq_len says what each has got. The new positions are listed where row_off [batch + 1] int32 is given: positions [rows] int32, as
+    paged_store and rope take them, and slots [rows] int64, page * page_size + slot or -1. Entries from row_off[batch] on are left as they are.
+    workspace: a tensor of paged_resize_workspace_bytes bytes, one for each call that may overlap."""
+    _check(_marshal.paged_resize(tables, lengths, workspace, row_off, positions, slots))
+
+
+class Rope:
+    """The frequencies of rotary positions (see dkv_rope_init in dkv.h): pairs (i, i + rot_dim / 2), or where `interleaved` (2 i, 2 i + 1), of the first
+    rot_dim dims of a head. scaling: "none", "linear", "base" or "parts", by `factor`. `freq` (radians of each pair for one position) and
+    `scale` may be set otherwise."""
+    SCALINGS = ("none", "linear", "base", "parts")
+
+    def __init__(self, head_dim, rot_dim=None, theta=10000.0, interleaved=False, scaling="none", factor=1.0, original=4096, slow=1.0, fast=32.0):
+        if scaling not in self.SCALINGS:
+            raise ValueError(f"scaling: one of {self.SCALINGS} is expected")
+        self.desc = RopeDesc()
+        _check(lib.dkv_rope_init(C.byref(self.desc), head_dim, head_dim if rot_dim is None else rot_dim, bool(interleaved), theta,
+                                 self.SCALINGS.index(scaling), factor, original, slow, fast))
+        self.address = C.addressof(self.desc)
+
+    @property
+    def freq(self):
+        return list(self.desc.freq[:self.desc.rot_dim // 2])
+
+    @freq.setter
+    def freq(self, values):
+        if len(values) != self.desc.rot_dim // 2:
+            raise ValueError(f"{self.desc.rot_dim // 2} frequencies are expected")
+        self.desc.freq[:len(values)] = [float(x) for x in values]
+
+    @property
+    def scale(self):
+        return self.desc.scale
+
+    @scale.setter
+    def scale(self, value):
+        self.desc.scale = value
+
+
+def rope(rope, q, k, positions, row_off=None, q_out=None, k_out=None, inverse=False):
+    """Rotate the rows of q [rows, n_q_heads, head_dim] and k [rows, n_k_heads, head_dim] (bfloat16 or float32, either may be None, the rows may be parts
+    of longer ones) by their positions [rows] int32, in place or into q_out and k_out; rows from row_off[-1] on are left as they are.
+    inverse: back, which takes the gradient of the results to that of q and k."""
+    _check(_marshal.rope(rope.address, q, k, positions, row_off, q_out, k_out, inverse))
 
 
 GEMM_OPT_STAGGER, GEMM_OPT_XCD_GROUP, GEMM_OPT_SWIGLU, GEMM_OPT_STREAM_W = 1, 2, 4, 8

@@ -165,7 +165,12 @@ static paged_store_fn f_paged_store;
 static paged_load_fn f_paged_load;
 static paged_bytes_fn f_paged_bytes;
 static paged_attn_fn f_paged_attn;
-enum { T_BF16 = DKV_BF16, T_FP32 = DKV_FP32, T_E4M3 = DKV_E4M3, T_E8M0, T_E2M1 = DKV_E2M1, T_I32, T_COUNT };
+typedef int (*paged_resize_fn)(const dkv_paged_tables *, const int32_t *, int32_t *, int32_t *, int64_t *, int32_t, void *, size_t, void *);
+typedef int (*rope_fn)(const dkv_rope_desc *, const void *, int64_t, void *, int64_t, int32_t, const void *, int64_t, void *, int64_t, int32_t,
+                       const int32_t *, const int32_t *, int32_t, int32_t, int32_t, int32_t, void *);
+static paged_resize_fn f_paged_resize;
+static rope_fn f_rope;
+enum { T_BF16 = DKV_BF16, T_FP32 = DKV_FP32, T_E4M3 = DKV_E4M3, T_E8M0, T_E2M1 = DKV_E2M1, T_I32, T_I64, T_COUNT };
 static PyObject *dtypes[T_COUNT];
 static PyObject *s_dtype, *s_is_contiguous, *s_get_device, *s_stride, *s_current, *s_stream;
 static PyObject *place_of;        /* has _cuda_getDevice() and _cuda_getCurrentRawStream(device) */
@@ -284,9 +289,9 @@ static int look_offsets(PyObject *t, int32_t batch, int32_t rows, int device, co
     return 0;
 }
 
-/* the current stream of the cache's device, which has to be the current one: asked of torch only where there is a GPU */
-static int look_place(int device, void **s) {
-    if (device < 0) return refuse("k_pages", "the cache is not on a GPU");
+/* the current stream of the tensors' device, which has to be the current one: asked of torch only where there is a GPU */
+static int look_place(const char *name, int device, void **s) {
+    if (device < 0) return refuse(name, "not on a GPU");
     PyObject *at = PyObject_CallMethodObjArgs(place_of, s_current, NULL);
     if (!at) return -1;
     const long current = PyLong_AsLong(at);
@@ -297,7 +302,7 @@ static int look_place(int device, void **s) {
     }
     Py_DECREF(at);
     if (PyErr_Occurred()) return -1;
-    return current == device ? 0 : refuse("k_pages", "the cache is not on the current device");
+    return current == device ? 0 : refuse(name, "not on the current device");
 }
 
 static int ready(Py_ssize_t n, Py_ssize_t want) {
@@ -329,7 +334,7 @@ static PyObject *rows_call(PyObject *const *a, Py_ssize_t n, int storing) {
         return NULL;
     }
     if (look_whole(a[3], "positions", T_I32, 1, &k.dims[0], device, &pos) || look_offsets(a[4], c.batch, k.dims[0], device, &off) ||
-        look_place(device, &stream))
+        look_place("k_pages", device, &stream))
         return NULL;
     int rc;
     Py_BEGIN_ALLOW_THREADS
@@ -354,6 +359,18 @@ static PyObject *py_paged_attn_workspace_bytes(PyObject *self, PyObject *const *
     return PyLong_FromLong((long)f_paged_bytes(&c, x[0], x[1], x[2], x[3]));
 }
 
+/* None, or memory of any type and shape: its sizes may pass 32 bits */
+static int look_workspace(PyObject *t, int device, tensor_info *ws, size_t *bytes) {
+    if (t == Py_None) return 0;
+    if (look_memory(t, ws)) return -1;
+    if (!ws->whole || ws->device != device) return refuse("workspace", "a contiguous tensor on the device of the cache is expected");
+    PyObject *b = PyObject_GetAttr(t, s_nbytes);
+    if (!b) return -1;
+    *bytes = PyLong_AsSize_t(b);
+    Py_DECREF(b);
+    return PyErr_Occurred() ? -1 : 0;
+}
+
 /* (cache, q, row_off, out, max_rows_per_seq, workspace): the status code of the library call */
 static PyObject *py_paged_attn(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     if (!ready(n, 6)) return NULL;
@@ -373,19 +390,8 @@ static PyObject *py_paged_attn(PyObject *self, PyObject *const *a, Py_ssize_t n)
     if (look_rows(a[1], "q", -1, c.head_dim, device, &q, &stride) || look_offsets(a[2], c.batch, q.dims[0], device, &off) ||
         look_whole(a[3], "out", q.dtype, 3, q.dims, device, &out) || get_i32(a[4], &most))
         return NULL;
-    if (a[5] != Py_None) {
-        if (look_memory(a[5], &ws)) return NULL;      /* of any type and shape: its sizes may pass 32 bits */
-        if (!ws.whole || ws.device != device) {
-            refuse("workspace", "a contiguous tensor on the device of the cache is expected");
-            return NULL;
-        }
-        PyObject *b = PyObject_GetAttr(a[5], s_nbytes);
-        if (!b) return NULL;
-        bytes = PyLong_AsSize_t(b);
-        Py_DECREF(b);
-        if (PyErr_Occurred()) return NULL;
-    }
-    if (look_place(device, &stream)) return NULL;
+    if (look_workspace(a[5], device, &ws, &bytes)) return NULL;
+    if (look_place("k_pages", device, &stream)) return NULL;
     int rc;
     Py_BEGIN_ALLOW_THREADS
     rc = f_paged_attn(&c, q.ptr, stride, off, out.ptr, q.dims[0], most, q.dims[1], q.dtype, ws.ptr, bytes, stream);
@@ -393,30 +399,141 @@ static PyObject *py_paged_attn(PyObject *self, PyObject *const *a, Py_ssize_t n)
     return PyLong_FromLong(rc);
 }
 
-/* bind_paged(addresses of dkv_paged_store, _load, _attn_workspace_bytes, _attn, then the types bfloat16, float32, float8_e4m3fn,
- * float8_e8m0fnu, float4_e2m1fn_x2, int32, and what tells the current device and stream) */
-static PyObject *py_bind_paged(PyObject *self, PyObject *const *a, Py_ssize_t n) {
-    if (n != 5 + T_COUNT) {
-        PyErr_SetString(PyExc_TypeError, "four addresses, six types and a source of streams are expected");
+/* ((page_table, seq_len, free_pages, free_at, page_size), lengths, workspace, row_off, positions, slots): the status code of the library call */
+static PyObject *py_paged_resize(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    if (!ready(n, 6)) return NULL;
+    if (!PyTuple_Check(a[0]) || PyTuple_Size(a[0]) != 5) {
+        PyErr_SetString(PyExc_TypeError, "PagedTables are expected");
         return NULL;
     }
-    void *f[4];
-    for (int i = 0; i < 4; ++i) f[i] = PyLong_AsVoidPtr(a[i]);
+    PyObject *t[5];
+    for (int i = 0; i < 5; ++i) t[i] = PyTuple_GetItem(a[0], i);
+    tensor_info table, len, ring, at, x, off = {0}, pos = {0}, slots = {0}, ws = {0};
+    int32_t page_size;
+    size_t bytes = 0;
+    void *stream;
+    if (look(t[0], &table)) return NULL;
+    if (table.dtype != T_I32 || table.n_dims != 2 || !table.whole) {
+        refuse("page_table", "a contiguous int32 tensor [batch, max_pages] is expected");
+        return NULL;
+    }
+    const int device = table.device;
+    const int32_t batch = table.dims[0], two = 2, many = batch < INT32_MAX ? batch + 1 : batch;
+    if (look_whole(t[1], "seq_len", T_I32, 1, &batch, device, &len) || look_whole(t[2], "free_pages", T_I32, -1, NULL, device, &ring) ||
+        look_whole(t[3], "free_at", T_I32, 1, &two, device, &at) || get_i32(t[4], &page_size) ||
+        look_whole(a[1], "lengths", T_I32, 1, &batch, device, &x) || look_workspace(a[2], device, &ws, &bytes))
+        return NULL;
+    int32_t rows = 0;
+    if (a[3] != Py_None && look_whole(a[3], "row_off", T_I32, 1, &many, device, &off)) return NULL;
+    if (a[4] != Py_None) {
+        if (look_whole(a[4], "positions", T_I32, -1, NULL, device, &pos)) return NULL;
+        rows = pos.dims[0];
+    }
+    if (a[5] != Py_None) {
+        if (look_whole(a[5], "slots", T_I64, -1, NULL, device, &slots)) return NULL;
+        if (a[4] != Py_None && slots.dims[0] != rows) {
+            refuse("slots", "as many as positions are expected");
+            return NULL;
+        }
+        rows = slots.dims[0];
+    }
+    if (a[3] != Py_None && a[4] == Py_None && a[5] == Py_None) {
+        refuse("row_off", "positions or slots say how many rows there may be");
+        return NULL;
+    }
+    if (look_place("page_table", device, &stream)) return NULL;
+    const dkv_paged_tables c = {table.ptr, len.ptr, ring.ptr, at.ptr, batch, ring.dims[0], table.dims[1], page_size};
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = f_paged_resize(&c, x.ptr, off.ptr, pos.ptr, slots.ptr, rows, ws.ptr, bytes, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* rows of one of the two tensors that are rotated, None for none, and where they go (None: where they are) */
+static int look_rotated(PyObject *t, PyObject *to, const char *name, const char *to_name, int32_t head_dim, int device, tensor_info *in,
+                        int64_t *in_stride, tensor_info *out, int64_t *out_stride) {
+    if (look_rows(t, name, -1, head_dim, device, in, in_stride)) return -1;
+    *out = *in;
+    *out_stride = *in_stride;
+    if (to == Py_None) return 0;
+    if (look_rows(to, to_name, in->dims[1], head_dim, device, out, out_stride)) return -1;
+    return out->dtype == in->dtype && out->dims[0] == in->dims[0] ? 0 : refuse(to_name, "the input's type and rows are expected");
+}
+
+/* (address of a dkv_rope_desc, q, k, positions, row_off, q_out, k_out, inverse): the status code of the library call */
+static PyObject *py_rope(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    if (!ready(n, 8)) return NULL;
+    const dkv_rope_desc *rope = PyLong_AsVoidPtr(a[0]);
+    if (PyErr_Occurred()) return NULL;
+    tensor_info pos, off = {0}, q = {0}, k = {0}, q_out = {0}, k_out = {0};
+    int64_t strides[4] = {0};
+    int32_t inverse;
+    void *stream;
+    if (look(a[3], &pos)) return NULL;
+    if (pos.dtype != T_I32 || pos.n_dims != 1 || !pos.whole) {
+        refuse("positions", "a contiguous int32 tensor [rows] is expected");
+        return NULL;
+    }
+    const int device = pos.device, has_q = a[1] != Py_None, has_k = a[2] != Py_None;
+    if ((!has_q && a[5] != Py_None) || (!has_k && a[6] != Py_None)) {
+        refuse(has_q ? "k_out" : "q_out", "there is nothing that goes there");
+        return NULL;
+    }
+    if ((has_q && look_rotated(a[1], a[5], "q", "q_out", rope->head_dim, device, &q, &strides[0], &q_out, &strides[1])) ||
+        (has_k && look_rotated(a[2], a[6], "k", "k_out", rope->head_dim, device, &k, &strides[2], &k_out, &strides[3])) || get_i32(a[7], &inverse))
+        return NULL;
+    if ((has_q && q.dims[0] != pos.dims[0]) || (has_k && k.dims[0] != pos.dims[0])) {
+        refuse("positions", "one for each row is expected");
+        return NULL;
+    }
+    if (has_q && has_k && q.dtype != k.dtype) {
+        refuse("k", "the type of q is expected");
+        return NULL;
+    }
+    if (a[4] != Py_None) {
+        if (look_whole(a[4], "row_off", T_I32, -1, NULL, device, &off)) return NULL;
+        if (off.dims[0] < 2) {
+            refuse("row_off", "a number more than there are sequences is expected");
+            return NULL;
+        }
+    }
+    if (look_place("positions", device, &stream)) return NULL;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = f_rope(rope, q.ptr, strides[0], q_out.ptr, strides[1], has_q ? q.dims[1] : 0, k.ptr, strides[2], k_out.ptr, strides[3], has_k ? k.dims[1] : 0,
+                pos.ptr, off.ptr, off.ptr ? off.dims[0] - 1 : 0, pos.dims[0], has_q ? q.dtype : has_k ? k.dtype : DKV_FP32, inverse, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* bind_paged(addresses of dkv_paged_store, _load, _attn_workspace_bytes, _attn, _resize and dkv_rope, then the types bfloat16, float32, float8_e4m3fn,
+ * float8_e8m0fnu, float4_e2m1fn_x2, int32, int64, and what tells the current device and stream) */
+static PyObject *py_bind_paged(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    enum { FUNCTIONS = 6 };
+    if (n != FUNCTIONS + T_COUNT + 1) {
+        PyErr_SetString(PyExc_TypeError, "six addresses, seven types and a source of streams are expected");
+        return NULL;
+    }
+    void *f[FUNCTIONS];
+    for (int i = 0; i < FUNCTIONS; ++i) f[i] = PyLong_AsVoidPtr(a[i]);
     if (PyErr_Occurred()) return NULL;
     for (int i = 0; i < T_COUNT; ++i) {
         PyObject *old = dtypes[i];
-        Py_INCREF(a[4 + i]);
-        dtypes[i] = a[4 + i];
+        Py_INCREF(a[FUNCTIONS + i]);
+        dtypes[i] = a[FUNCTIONS + i];
         Py_XDECREF(old);
     }
     PyObject *before = place_of;
-    Py_INCREF(a[4 + T_COUNT]);
-    place_of = a[4 + T_COUNT];
+    Py_INCREF(a[FUNCTIONS + T_COUNT]);
+    place_of = a[FUNCTIONS + T_COUNT];
     Py_XDECREF(before);
     f_paged_store = (paged_store_fn)f[0];
     f_paged_load = (paged_load_fn)f[1];
     f_paged_bytes = (paged_bytes_fn)f[2];
     f_paged_attn = (paged_attn_fn)f[3];
+    f_paged_resize = (paged_resize_fn)f[4];
+    f_rope = (rope_fn)f[5];
     Py_RETURN_NONE;
 }
 
@@ -427,6 +544,8 @@ static PyMethodDef methods[] = {
     {"paged_load", (PyCFunction)(void (*)(void))py_paged_load, METH_FASTCALL, NULL},
     {"paged_attn_workspace_bytes", (PyCFunction)(void (*)(void))py_paged_attn_workspace_bytes, METH_FASTCALL, NULL},
     {"paged_attn", (PyCFunction)(void (*)(void))py_paged_attn, METH_FASTCALL, NULL},
+    {"paged_resize", (PyCFunction)(void (*)(void))py_paged_resize, METH_FASTCALL, NULL},
+    {"rope", (PyCFunction)(void (*)(void))py_rope, METH_FASTCALL, NULL},
     {"bind_paged", (PyCFunction)(void (*)(void))py_bind_paged, METH_FASTCALL, NULL},
     {"bind", (PyCFunction)(void (*)(void))py_bind, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};
