@@ -104,12 +104,12 @@ __device__ __forceinline__ f32x8 load8(const e4m3_t *p) {
     }
     return x;
 }
-// 4 codes, in the lower two bytes, times 1
-__device__ __forceinline__ f32x4 from_e2m1(uint32_t a) {
-    const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(a, 1.f, 0), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(a, 1.f, 1);
-    return f32x4{lo[0], lo[1], hi[0], hi[1]};
-}
 // 8 codes times a scale (see scale_value): exact
+__device__ __forceinline__ f32x8 f32_of_e2m1(uint32_t a, float scale) {
+    const auto x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(a, scale, 0), y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(a, scale, 1),
+               z = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(a, scale, 2), w = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(a, scale, 3);
+    return f32x8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
+}
 __device__ __forceinline__ u32x4 bf16_of_e2m1(uint32_t a, float scale) {
     return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, scale, 0)),
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, scale, 1)),
@@ -117,8 +117,7 @@ __device__ __forceinline__ u32x4 bf16_of_e2m1(uint32_t a, float scale) {
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, scale, 3))};
 }
 __device__ __forceinline__ f32x8 load8(const e2m1_t *p) {
-    const uint32_t a = *reinterpret_cast<const uint32_t *>(p);
-    return __builtin_shufflevector(from_e2m1(a), from_e2m1(a >> 16), 0, 1, 2, 3, 4, 5, 6, 7);
+    return f32_of_e2m1(*reinterpret_cast<const uint32_t *>(p), 1.f);
 }
 __device__ __forceinline__ void store8(float *p, f32x8 x) {
     *reinterpret_cast<f32x4_el *>(p) = __builtin_shufflevector(x, x, 0, 1, 2, 3);

@@ -44,7 +44,10 @@ __device__ __forceinline__ Piece<4> load_piece(const e4m3_t *p, Piece<4> *) {
     const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(a, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(a, true);
     return Piece<4>{lo[0], lo[1], hi[0], hi[1]};
 }
-__device__ __forceinline__ Piece<4> load_piece(const e2m1_t *p, Piece<4> *) { return from_e2m1(*reinterpret_cast<const uint16_t *>(p)); }
+__device__ __forceinline__ Piece<4> load_piece(const e2m1_t *p, Piece<4> *) {
+    const f32x8 x = f32_of_e2m1(*reinterpret_cast<const uint16_t *>(p), 1.f);
+    return __builtin_shufflevector(x, x, 0, 1, 2, 3);
+}
 template <typename T> __device__ __forceinline__ Piece<8> load_piece(const T *p, Piece<8> *) { return load8(p); }
 template <typename T> __device__ __forceinline__ Piece<16> load_piece(const T *p, Piece<16> *) {
     return __builtin_shufflevector(load8(p), load8(p + 8), 0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15);

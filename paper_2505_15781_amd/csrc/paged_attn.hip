@@ -207,7 +207,7 @@ int launch_merge(const PagedCache &c, const Plan &p, const int *row_off, void *o
 template <typename T, typename C, int DH, int NQ, int NW>
 int launch_split(const PagedCache &c, const Plan &p, const void *q, int64_t q_stride, const int *row_off, void *out, void *part, int rows,
                  int max_rows, int Hq, hipStream_t s) {
-    constexpr int smem = NW * SplitSmem<T, DH>::WAVE_BYTES;
+    constexpr int smem = NW * SplitSmem<T, C, DH, NQ>::WAVE_BYTES;
     const float scale_log2e = 1.4426950408889634f / sqrtf((float)DH);
 #define SPLIT(ONCE)                                                                                                              \
     do {                                                                                                                         \

@@ -127,11 +127,16 @@ __device__ __forceinline__ bool find_slice(const PagedCache &c, const int *row_o
 
 template <int BYTES> struct PieceBits { typedef u32x4 type; };
 template <> struct PieceBits<8> { typedef u32x2 type; };
-template <typename T, int DH> struct SplitSmem {
+template <> struct PieceBits<4> { typedef uint32_t type; };
+// e2m1: a lane's part of a row of K is what the matrix instruction takes of it (see score_operand), so K does not go through LDS.
+template <typename C> constexpr bool kDirectK = kE2M1<C>;
+template <typename T, typename C, int DH, int NQ> struct SplitSmem {
     static constexpr int K_STRIDE = DH * (int)sizeof(T) + 16;                               // bytes per row; the rest spreads
     static constexpr int V_STRIDE = DH * (int)sizeof(T) + (sizeof(T) == 2 ? 32 : 16);       // the reads over the banks
-    static constexpr int K_BYTES = PKT * K_STRIDE;
-    static constexpr int WAVE_BYTES = PKT * (K_STRIDE + V_STRIDE);
+    static constexpr int K_BYTES = kDirectK<C> ? 0 : PKT * K_STRIDE;
+    static constexpr int RECORDS = NQ * 16 * (DH + 4) * 4;                                  // what a wavefront leaves at the end
+    static constexpr int TILES = K_BYTES + PKT * V_STRIDE;
+    static constexpr int WAVE_BYTES = TILES > RECORDS ? TILES : RECORDS;
 };
 
 // A piece of a row as it is stored -> elements of T in LDS.
@@ -167,14 +172,11 @@ __device__ __forceinline__ void stage(bf16_t *dst, const e2m1_t *, u32x2 x, floa
 }
 template <typename V> __device__ __forceinline__ void stage(float *dst, const e2m1_t *, V x, float scale) {
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(V) / 4); ++i)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            // the instruction's choice of a byte is a constant
-            const auto lo = k ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[i], scale, 2) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[i], scale, 0);
-            const auto hi = k ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[i], scale, 3) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[i], scale, 1);
-            *reinterpret_cast<f32x4 *>(dst + 8 * i + 4 * k) = f32x4{lo[0], lo[1], hi[0], hi[1]};
-        }
+    for (int i = 0; i < (int)(sizeof(V) / 4); ++i) {
+        const f32x8 y = f32_of_e2m1(x[i], scale);
+        *reinterpret_cast<f32x4 *>(dst + 8 * i) = __builtin_shufflevector(y, y, 0, 1, 2, 3);
+        *reinterpret_cast<f32x4 *>(dst + 8 * i + 4) = __builtin_shufflevector(y, y, 4, 5, 6, 7);
+    }
 }
 
 // softmax_step with probabilities that stay in fp32 (in st), and their sum over this lane's keys in l_acc[0]
@@ -208,10 +210,9 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
                                                                     const int *__restrict__ row_off, T *__restrict__ out, int2 *__restrict__ meta,
                                                                     float *__restrict__ part, int rows, int max_rows, GroupMap map, Divisor heads,
                                                                     Divisor G, float scale_log2e) {
-    using SM = SplitSmem<T, DH>;
+    using SM = SplitSmem<T, C, DH, NQ>;
     constexpr bool BF = sizeof(T) == 2;
     constexpr int REC = DH + 4;                       // floats per record: m, l, pad, pad, o[DH]
-    static_assert(NQ * 16 * REC * 4 <= SM::WAVE_BYTES, "records fit the wavefront's LDS region");
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     unsigned char *ksm = smem_raw + wave * SM::WAVE_BYTES, *vsm = ksm + SM::K_BYTES;
@@ -244,7 +245,9 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
     typedef typename PieceBits<PIECE>::type Bits;
     Bits kreg[N], vreg[N];
     uint32_t scales = 0;                      // e4m3: lane i has the scale of K row i, or of V row i - 32, as a float
-    uint32_t k_scales[N], v_scales[N];        // e2m1: those of this lane's pieces
+    // e2m1: of half h of the tile lane (qi, g) holds dims g DH / 4 + [0, DH / 4) of key qi; the scales of these and of its pieces of V
+    constexpr int WORDS = DH / 32;
+    uint32_t kd[2][WORDS], kd_scale[2], v_scales[N];
     int pages = -1, seen0 = 0, seen1 = 0;     // seen: keys of each half that are attended to
     auto load_tile = [&](int t, int j) {
         const int id0 = __builtin_amdgcn_readlane(pages, 2 * (j & 31)), id1 = __builtin_amdgcn_readlane(pages, 2 * (j & 31) + 1);
@@ -262,16 +265,23 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
                 reg[i] = ONCE ? __builtin_nontemporal_load(reinterpret_cast<const Bits *>(p)) : *reinterpret_cast<const Bits *>(p);
             }
         };
-        fetch(kreg, c.k);
+        if constexpr (!kDirectK<C>) fetch(kreg, c.k);
         fetch(vreg, c.v);
         if constexpr (kE2M1<C>) {
             constexpr int S = kRowScales<C, DH>;
+            typedef typename PieceBits<4 * WORDS>::type Part;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const size_t row = (size_t)(h ? row1 : row0) + (lane & 15);
+                const Part *p = reinterpret_cast<const Part *>(c.k + row * ROW + (lane >> 4) * 4 * WORDS);
+                const Part x = ONCE ? __builtin_nontemporal_load(p) : *p;
+                __builtin_memcpy(kd[h], &x, sizeof x);
+                kd_scale[h] = c.ks[row * S + (lane >> 4) * (DH / 4) / 32];
+            }
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int row = i * RPI + lane / LPR;
-                const size_t at = (size_t)(row < 16 ? row0 : row1) * S + (row & 15) * S + lane % LPR * PER / 32;
-                k_scales[i] = c.ks[at];
-                v_scales[i] = c.vs[at];
+                v_scales[i] = c.vs[(size_t)(row < 16 ? row0 : row1) * S + (row & 15) * S + lane % LPR * PER / 32];
             }
         } else if constexpr (sizeof(C) == 1) {
             scales = (uint32_t)(lane < 32 ? c.ks : c.vs)[(lane & 16 ? row1 : row0) + (lane & 15)] << 23;
@@ -284,7 +294,6 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
             const int row = i * RPI + lane / LPR, el = lane % LPR * PER;
             float k_scale = 1.f, v_scale = 1.f;
             if constexpr (kE2M1<C>) {
-                k_scale = scale_value(k_scales[i]);
                 v_scale = scale_value(v_scales[i]);
             } else if constexpr (sizeof(C) == 1) {
                 k_scale = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(row << 2, (int)scales));
@@ -294,7 +303,7 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
                 vreg[i] = Bits{};
                 v_scale = 1.f;
             }
-            stage(reinterpret_cast<T *>(ksm + row * SM::K_STRIDE) + el, (const C *)nullptr, kreg[i], k_scale);
+            if constexpr (!kDirectK<C>) stage(reinterpret_cast<T *>(ksm + row * SM::K_STRIDE) + el, (const C *)nullptr, kreg[i], k_scale);
             stage(reinterpret_cast<T *>(vsm + row * SM::V_STRIDE) + el, (const C *)nullptr, vreg[i], v_scale);
         }
     };
@@ -312,18 +321,19 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
     int t = t_begin + wave, j = 0;
     if (plan.split) entry = load_entry(b, first_key(t_begin, 0));
     entry_ahead = load_entry(b, first_key(t_begin, 32));
-    // Query operands. bf16: dims 32 ks + 8 g + [0, 8); fp32: dims 16 ks + 4 g + [0, 4), one of the four for each product
-    constexpr int QS = BF ? DH / 32 : DH / 16;
+    // Query operands. bf16: dims 32 ks + 8 g + [0, 8); fp32: dims 16 ks + 4 g + [0, 4), one of the four for each product. The order of the dims is
+    // free as long as K has the same: where K is taken from registers, g DH / 4 + 8 ks + [0, 8) and g DH / 4 + 4 ks + [0, 4)
+    constexpr int QS = BF ? DH / 32 : DH / 16, Q_STEP = kDirectK<C> ? (BF ? 8 : 4) : (BF ? 32 : 16), Q_LANE = kDirectK<C> ? DH / 4 : (BF ? 8 : 4);
     u32x4 qf[NQ][QS];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         const int mq = m0 + 16 * n + qi;
         const int r = r0 + G.div(mq);
         const bool ok = mq < nq && (unsigned)r < (unsigned)rows;
-        const T *qp = Q + (ok ? r * q_stride + (kvh * G.d + G.mod(mq)) * DH : 0) + (BF ? 8 : 4) * g;
+        const T *qp = Q + (ok ? r * q_stride + (kvh * G.d + G.mod(mq)) * DH : 0) + Q_LANE * g;
 #pragma unroll
         for (int ks = 0; ks < QS; ++ks) {
-            const u32x4 x = *reinterpret_cast<const bf16x8_el *>(qp + (BF ? 32 : 16) * ks);
+            const u32x4 x = *reinterpret_cast<const bf16x8_el *>(qp + Q_STEP * ks);
             qf[n][ks] = ok ? x : u32x4{0, 0, 0, 0};
         }
     }
@@ -343,9 +353,34 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
             pages = page_of(entry_ahead, j + 1);
             entry_ahead = load_entry(b, first_key(t_begin, j + 33));
         }
+        f32x4 st[NQ][2];
+        if constexpr (kDirectK<C>) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) st[n][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+                const float scale = scale_value(kd_scale[h]);
+#pragma unroll
+                for (int w = 0; w < WORDS; ++w) {
+                    if constexpr (BF) {
+                        const bf16x8 kf = __builtin_bit_cast(bf16x8, bf16_of_e2m1(kd[h][w], scale));
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n)
+                            st[n][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, __builtin_bit_cast(bf16x8, qf[n][w]), st[n][h], 0, 0, 0);
+                    } else {
+                        const f32x8 kf = f32_of_e2m1(kd[h][w], scale);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+#pragma unroll
+                            for (int n = 0; n < NQ; ++n)
+                                st[n][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], __uint_as_float(qf[n][2 * w + (e >> 2)][e & 3]), st[n][h], 0, 0, 0);
+                    }
+                }
+            }
+        }
         if (t + NW < t_end) load_tile(t + NW, j + 1);
 
-        f32x4 st[NQ][2];
+        if constexpr (!kDirectK<C>)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const unsigned char *krow = ksm + (16 * h + qi) * SM::K_STRIDE + g * 16;
