@@ -87,6 +87,12 @@ __device__ __forceinline__ bool wide_item(const PagedCache &c, const int *row_of
     return false;
 }
 
+// Words e and e ^ turn change places.
+__device__ __forceinline__ void turn_words(u32x4 &a, int turn) {
+    const u32x4 b = turn & 1 ? u32x4{a[1], a[0], a[3], a[2]} : a;
+    a = turn & 2 ? u32x4{b[2], b[3], b[0], b[1]} : b;
+}
+
 // Where a tile of 64 keys is: the rows (see PagedCache::row) of its four groups of 16 keys, and which of them have a page.
 struct WideTile {
     uint32_t row[4];
@@ -199,8 +205,14 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
     constexpr int SCALES = kE2M1<C> ? DH / 32 : 1, BYTES = kRowBytes<C, DH>;
     typedef typename PieceBits<BYTES / LPF>::type Bits;
     const int f_row = (RPF * wave + lane / LPF) % 16;
-    auto f_group = [&](const WideTile &x, int i) { return RPF == 16 ? (wave & 2 ? (wave & 1 ? x.row[3] : x.row[2]) : (wave & 1 ? x.row[1] : x.row[0]))
-                                                                    : (wave >> 1 ? x.row[2 * i + 1] : x.row[2 * i]); };
+    auto f_group = [&](const WideTile &x, int i) {
+        if constexpr (RPF == 16) {                   // numbers, not places, to choose from: those would put the tile into memory
+            const uint32_t r0 = x.row[0], r1 = x.row[1], r2 = x.row[2], r3 = x.row[3], lo = wave & 1 ? r1 : r0, hi = wave & 1 ? r3 : r2;
+            return wave & 2 ? hi : lo;
+        } else {
+            return wave >> 1 ? x.row[2 * i + 1] : x.row[2 * i];
+        }
+    };
     Bits kreg[FETCHES], vreg[FETCHES];
     uint32_t k_scale[FETCHES], v_scale[FETCHES];
     auto fetch = [&](Bits (&reg)[FETCHES], uint32_t (&scale)[FETCHES], const unsigned char *base, const uint8_t *scales, const WideTile &x) {
@@ -211,6 +223,9 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
             scale[i] = (scales + row * SCALES)[(uint32_t)(f_row * SCALES + (kE2M1<C> ? lane % LPF * PER / 32 : 0))];
         }
     };
+    // e2m1, 128 dims: a lane writes four chunks in a row, and four neighbouring rows would have theirs on the same banks at a time: each begins
+    // with another one
+    const int turn = kE2M1<C> && DH == 128 ? lane / LPF & 3 : 0;
     auto convert = [&](const Bits (&reg)[FETCHES], const uint32_t (&scale)[FETCHES], int tile_pages, int t, uint32_t dst) {
         const bool all = whole(t, tile_pages);                        // uniform
 #pragma unroll
@@ -219,8 +234,10 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
             const float s = __uint_as_float(scale[i] << 23);
             u32x4 y[PER / 8];
             if constexpr (kE2M1<C>) {
+                Bits a = reg[i];
+                if constexpr (DH == 128) turn_words(a, turn);
 #pragma unroll
-                for (int e = 0; e < PER / 8; ++e) y[e] = bf16_of_e2m1(reg[i][e], s);
+                for (int e = 0; e < PER / 8; ++e) y[e] = bf16_of_e2m1(a[e], s);
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -234,7 +251,7 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
             }
 #pragma unroll
             for (int e = 0; e < PER / 8; ++e)
-                *reinterpret_cast<u32x4 *>(smem_raw + dst + row * ROW + (((PER / 8 * (lane % LPF) + e) ^ sw) << 4)) = y[e];
+                *reinterpret_cast<u32x4 *>(smem_raw + dst + row * ROW + (((PER / 8 * (lane % LPF) + (e ^ turn)) ^ sw) << 4)) = y[e];
         }
     };
     // pages of the tiles t, t + 1, t + 2 (of the last ones: of some tile), and where tile t + 1 (bf16) or t + 2 (codes) is
