@@ -23,15 +23,17 @@ struct Lists {
     int64_t *slots;
     int rows;
 };
-// In the workspace: `head`, then arrays of one number for each sequence.
+// In the workspace (one launch: in LDS): totals, then arrays of one number for each sequence.
 struct Totals {
     uint32_t head, count;        // the free pages of the ring before the call
     int taken, rows;
+    uint32_t left;               // see Work::give, all sequences
 };
 struct Work {
     Totals *totals;
     int *before, *after;         // lengths
-    int *take, *give, *row;      // pages taken, pages given back, new rows of the sequences before
+    int *take, *row;             // pages taken, new rows of the sequences before
+    int *give;                   // pages given back by them (one launch: entries that are cleared, whether they name a page or not)
 };
 
 constexpr uint32_t kMost = 0x7fffffff;      // sums end here
@@ -68,17 +70,24 @@ template <typename F> __device__ __forceinline__ void each_entry(const int *row,
     }
 }
 
-// The sequence of item x: the last one with first[b] <= x. Whole wavefronts, x uniform; 64 of them are asked at once.
-__device__ __forceinline__ int find(const int *first, int n, int x) {
+// The sequences of the items x and y: the last ones with first[b] <= x, and y. Whole wavefronts, x and y uniform; 64 sequences are asked at once, for both.
+__device__ __forceinline__ void find(const int *first, int batch, int x, int y, int &bx, int &by) {
     const int lane = threadIdx.x & 63;
-    int lo = 0;
-    while (n > 1) {
-        const int step = (n + 63) >> 6;
-        const int k = __popcll(__ballot(lane * step < n && first[lo + min(lane * step, n - 1)] <= x)) - 1;
-        lo += k * step;
-        n = min(step, n - k * step);
+    int lo[2] = {0, 0}, n[2] = {batch, batch};
+    const int item[2] = {x, y};
+    while (n[0] > 1 || n[1] > 1) {
+        int at[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) at[i] = first[lo[i] + min(lane * ((n[i] + 63) >> 6), n[i] - 1)];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int step = (n[i] + 63) >> 6, k = __popcll(__ballot(lane * step < n[i] && at[i] <= item[i])) - 1;
+            lo[i] += k * step;
+            n[i] = min(step, n[i] - k * step);
+        }
     }
-    return __builtin_amdgcn_readfirstlane(lo);
+    bx = __builtin_amdgcn_readfirstlane(lo[0]);
+    by = __builtin_amdgcn_readfirstlane(lo[1]);
 }
 __device__ __forceinline__ int find_between(const int *first, int lo, int hi, int x) {
     while (lo < hi) {
@@ -89,8 +98,25 @@ __device__ __forceinline__ int find_between(const int *first, int lo, int hi, in
     return lo;
 }
 
-__device__ void plan(const Tables &t, const int *lengths, const Lists &l, const Work &w) {
-    __shared__ int from[kThreads], to[kThreads], given[kThreads];
+// Lengths of sequence b before the call and wanted.
+__device__ __forceinline__ void lengths_of(const Tables &t, const int *lengths, int b, int &old, int &now) {
+    old = min(max(t.len[b], 0), t.max_pages << t.shift);
+    now = lengths[b];
+    if (now < 0 || now > t.max_pages << t.shift) now = old;
+}
+__device__ __forceinline__ void move_ring(const Tables &t, const Totals &all, uint32_t given) {
+    t.ring_at[0] = (int)t.place(all.head + all.taken);
+    t.ring_at[1] = (int)(min(given, t.n_pages - all.count) + (all.count - all.taken));
+}
+// Pages that a sequence gives back, of its entries [from, to).
+__device__ __forceinline__ int count_pages(const Tables &t, int b, int from, int to) {
+    int n = 0;
+    each_entry(t.table + (size_t)b * t.max_pages, from, to, [&](int id, bool is, int) { n += __popcll(__ballot(is && t.is_page(id))); });
+    return n;
+}
+
+// COUNTED: w.give has the pages that each sequence gives back (paged_resize_count), otherwise the ring's new place is left to give_back.
+template <bool COUNTED> __device__ __forceinline__ void plan(const Tables &t, const int *lengths, const Lists &l, const Work &w) {
     __shared__ uint32_t sums[3][kWaves];
     __shared__ int most[2];                      // pages and rows of the sequences that fit
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -103,33 +129,11 @@ __device__ void plan(const Tables &t, const int *lengths, const Lists &l, const 
         const int b = base + tid;
         const bool here = b < t.batch;
         int old = 0, now = 0;
-        if (here) {
-            old = min(max(t.len[b], 0), t.max_pages << t.shift);
-            now = lengths[b];
-            if (now < 0 || now > t.max_pages << t.shift) now = old;
-        }
+        if (here) lengths_of(t, lengths, b, old, now);
         const int have = t.pages(old);
         const uint32_t pages = max(t.pages(now) - have, 0), rows = l.row_off ? max(now - old, 0) : 0;
-        from[tid] = t.pages(now);
-        to[tid] = have;
-        given[tid] = 0;
-        __syncthreads();
-        // pages given back, where entries may be missing: the wavefronts take the sequences in turn
-        {
-            const int mine = lane * kWaves + wave;
-            unsigned long long left = __ballot(from[mine] < to[mine]);
-            while (left) {
-                const int i = __builtin_ctzll(left) * kWaves + wave;
-                left &= left - 1;
-                int n = 0;
-                each_entry(t.table + (size_t)(base + i) * t.max_pages, from[i], to[i], [&](int id, bool is, int) { n += __popcll(__ballot(is && t.is_page(id))); });
-                if (lane == 0) given[i] = n;
-            }
-        }
-        uint32_t pages_upto = wave_sums(pages), rows_upto = wave_sums(rows);
-        __syncthreads();
-        const uint32_t gives = given[tid];
-        uint32_t given_upto = wave_sums(gives);
+        const uint32_t gives = COUNTED ? (here ? (uint32_t)w.give[b] : 0) : max(have - t.pages(now), 0);
+        const uint32_t pages_upto = wave_sums(pages), rows_upto = wave_sums(rows), given_upto = wave_sums(gives);
         if (lane == 63) {
             sums[0][wave] = pages_upto;
             sums[1][wave] = rows_upto;
@@ -168,28 +172,33 @@ __device__ void plan(const Tables &t, const int *lengths, const Lists &l, const 
     }
     if (tid == 0) {
         const int taken = most[0] < 0 ? (int)pages_before : most[0], rows = most[0] < 0 ? (int)rows_before : most[1];
-        *w.totals = Totals{head, count, taken, rows};
+        *w.totals = Totals{head, count, taken, rows, given_before};
         if (l.row_off) l.row_off[0] = 0;
-        t.ring_at[0] = (int)t.place(head + taken);
-        t.ring_at[1] = (int)(min(given_before, t.n_pages - count) + (count - taken));
+        if constexpr (COUNTED) move_ring(t, *w.totals, given_before);
     }
 }
 
-// Wavefront `wave` of `waves`.
-__device__ void fill(const Tables &t, const Lists &l, const Work &w, int wave, int waves) {
+// The three parts of the work are independent of each other; each for wavefront `wave` of `waves`.
+__device__ __forceinline__ void take_pages(const Tables &t, const Work &w, int wave, int waves) {
     const int lane = threadIdx.x & 63;
     const Totals all = *w.totals;
-    // pages taken
     for (int x = wave * 64; x < all.taken; x += waves * 64) {
-        const int b0 = find(w.take, t.batch, x), b1 = find(w.take, t.batch, min(x + 63, all.taken - 1)), mine = x + lane;
+        const int mine = x + lane;
+        int b0, b1;
+        find(w.take, t.batch, x, min(x + 63, all.taken - 1), b0, b1);
         if (mine < all.taken) {
             const int b = find_between(w.take, b0, b1, mine);
             t.table[(size_t)b * t.max_pages + t.pages(w.before[b]) + mine - w.take[b]] = t.ring[t.place(all.head + mine)];
         }
     }
-    // new rows, four to a lane
+}
+// Four rows to a lane.
+__device__ __forceinline__ void list_rows(const Tables &t, const Lists &l, const Work &w, int wave, int waves) {
+    const int lane = threadIdx.x & 63;
+    const Totals all = *w.totals;
     for (int x = wave * 256; x < all.rows; x += waves * 256) {
-        const int b0 = find(w.row, t.batch, x), b1 = find(w.row, t.batch, min(x + 255, all.rows - 1));
+        int b0, b1;
+        find(w.row, t.batch, x, min(x + 255, all.rows - 1), b0, b1);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const int r = x + 64 * u + lane;
@@ -203,7 +212,11 @@ __device__ void fill(const Tables &t, const Lists &l, const Work &w, int wave, i
             }
         }
     }
-    // pages given back: behind the end of the ring
+}
+// To the end of the ring, a sequence at a time.
+__device__ __forceinline__ void give_pages(const Tables &t, const Work &w, int wave, int waves) {
+    const int lane = threadIdx.x & 63;
+    const Totals all = *w.totals;
     for (int base = 0; base < t.batch; base += 64 * waves) {
         const int b = base + lane * waves + wave;
         const int need = b < t.batch ? t.pages(w.after[b]) : 0, have = b < t.batch ? t.pages(w.before[b]) : 0;
@@ -225,18 +238,80 @@ __device__ void fill(const Tables &t, const Lists &l, const Work &w, int wave, i
     }
 }
 
-__global__ __launch_bounds__(kThreads) void paged_resize_plan(Tables t, const int *lengths, Lists l, Work w) { plan(t, lengths, l, w); }
-__global__ __launch_bounds__(256) void paged_resize_fill(Tables t, Lists l, Work w) {
-    fill(t, l, w, (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), (int)gridDim.x * 4);
+// The same by a whole workgroup for all entries in a row, where nobody has counted the pages among them: 4 kThreads at a time.
+__device__ __forceinline__ void give_entries(const Tables &t, const Work &w) {
+    static_assert(4 * kWaves == 64, "a count for each lane");
+    __shared__ int counts[4 * kWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Totals all = *w.totals;
+    uint32_t given = 0;
+    for (uint32_t x = 0; x < all.left; x += 4 * kThreads) {
+        int *entry[4], id[4];
+        unsigned long long pages[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const uint32_t begin = x + u * kThreads + wave * 64, mine = begin + lane;
+            entry[u] = nullptr;
+            if (begin < all.left) {                       // uniform
+                int b0, b1;
+                find(w.give, t.batch, (int)begin, (int)min(begin + 63, all.left - 1), b0, b1);
+                const int b = find_between(w.give, b0, b1, (int)min(mine, all.left - 1));
+                if (mine < all.left) entry[u] = t.table + (size_t)b * t.max_pages + t.pages(w.after[b]) + ((int)mine - w.give[b]);
+            }
+            id[u] = entry[u] ? *entry[u] : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            pages[u] = __ballot(t.is_page(id[u]));
+            if (lane == 0) counts[u * kWaves + wave] = __popcll(pages[u]);
+        }
+        __syncthreads();
+        const uint32_t upto = wave_sums((uint32_t)counts[lane]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const uint32_t before = u * kWaves + wave ? (uint32_t)__builtin_amdgcn_readlane((int)upto, max(u * kWaves + wave - 1, 0)) : 0;
+            const uint32_t n = given + before + __popcll(pages[u] & ((1ull << lane) - 1));
+            if (t.is_page(id[u]) && n < t.n_pages - all.count) t.ring[t.place(t.place(all.head + all.count) + n)] = id[u];
+            if (entry[u]) *entry[u] = -1;
+        }
+        given += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+        __syncthreads();
+    }
+    if (tid == 0) move_ring(t, all, given);
 }
-__global__ __launch_bounds__(kThreads) void paged_resize_small(Tables t, const int *lengths, Lists l, Work w) {
-    plan(t, lengths, l, w);
+
+__global__ __launch_bounds__(256) void paged_resize_count(Tables t, const int *lengths, Work w) {
+    const int b = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    if (b >= t.batch) return;
+    int old, now;
+    lengths_of(t, lengths, b, old, now);
+    const int n = count_pages(t, b, t.pages(now), t.pages(old));
+    if ((threadIdx.x & 63) == 0) w.give[b] = n;
+}
+__global__ __launch_bounds__(kThreads) void paged_resize_plan(Tables t, const int *lengths, Lists l, Work w) { plan<true>(t, lengths, l, w); }
+__global__ __launch_bounds__(256) void paged_resize_fill(Tables t, Lists l, Work w) {
+    const int wave = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = (int)gridDim.x * 4;
+    if (blockIdx.y == 0) list_rows(t, l, w, wave, waves);
+    else if (blockIdx.y == 1) take_pages(t, w, wave, waves);
+    else give_pages(t, w, wave, waves);
+}
+// Up to kThreads sequences, all in one workgroup.
+__global__ __launch_bounds__(kThreads) void paged_resize_small(Tables t, const int *lengths, Lists l) {
+    __shared__ int arrays[5][kThreads];
+    __shared__ Totals totals;
+    const Work w = {&totals, arrays[0], arrays[1], arrays[2], arrays[3], arrays[4]};
+    plan<false>(t, lengths, l, w);
     __syncthreads();
-    fill(t, l, w, __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), kWaves);
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    take_pages(t, w, wave, kWaves);
+    list_rows(t, l, w, wave, kWaves);
+    give_entries(t, w);
 }
 
 constexpr int kMostSequences = 1 << 20;
-size_t work_bytes(int batch) { return 16 + 5 * sizeof(int) * (size_t)batch; }
+constexpr size_t kTotalsBytes = 32;
+static_assert(sizeof(Totals) <= kTotalsBytes, "totals lie in front of the arrays");
+size_t work_bytes(int batch) { return kTotalsBytes + 5 * sizeof(int) * (size_t)batch; }
 
 }  // namespace
 
@@ -263,17 +338,23 @@ extern "C" int dkv_paged_resize(const dkv_paged_tables *tables, const int32_t *l
     if (reinterpret_cast<uintptr_t>(workspace) % 16) { dkv_set_error("workspace must be 16-byte aligned"); return DKV_E_INVALID_ARG; }
     const Tables t = {c.page_table, c.seq_len, c.free_pages, c.free_at, c.batch, c.max_pages, __builtin_ctz((unsigned)c.page_size), (uint32_t)c.n_pages};
     const Lists l = {row_off, positions, slots, rows};      // no rows are counted without row_off
-    int *arrays = reinterpret_cast<int *>(static_cast<char *>(workspace) + 16);
+    int *arrays = reinterpret_cast<int *>(static_cast<char *>(workspace) + kTotalsBytes);
     const Work w = {static_cast<Totals *>(workspace), arrays, arrays + c.batch, arrays + 2 * (size_t)c.batch, arrays + 3 * (size_t)c.batch, arrays + 4 * (size_t)c.batch};
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (c.batch <= kThreads && (!row_off || rows <= 8192)) {
-        hipLaunchKernelGGL(paged_resize_small, dim3(1), dim3(kThreads), 0, s, t, lengths, l, w);
+        hipLaunchKernelGGL(paged_resize_small, dim3(1), dim3(kThreads), 0, s, t, lengths, l);
         DKV_LAUNCH_CHECK();
         return DKV_OK;
     }
+    hipLaunchKernelGGL(paged_resize_count, dim3((unsigned)((c.batch + 3) / 4)), dim3(256), 0, s, t, lengths, w);
+    DKV_LAUNCH_CHECK();
     hipLaunchKernelGGL(paged_resize_plan, dim3(1), dim3(kThreads), 0, s, t, lengths, l, w);
     DKV_LAUNCH_CHECK();
-    hipLaunchKernelGGL(paged_resize_fill, dim3(512), dim3(256), 0, s, t, l, w);
+    // a wavefront for 256 rows, 64 pages or a sequence at a time, up to what runs at once
+    const int64_t pages = (int64_t)c.batch * c.max_pages < c.n_pages ? (int64_t)c.batch * c.max_pages : c.n_pages;
+    int64_t waves = row_off ? (rows + 255) / 256 : (pages + 63) / 64;
+    waves = waves > c.batch ? waves : c.batch;
+    hipLaunchKernelGGL(paged_resize_fill, dim3((unsigned)(waves < 8192 ? (waves + 3) / 4 : 2048), 3), dim3(256), 0, s, t, l, w);
     DKV_LAUNCH_CHECK();
     return DKV_OK;
 }
