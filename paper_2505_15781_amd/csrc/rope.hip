@@ -19,7 +19,7 @@ template <typename T> struct RopeArgs {
     int64_t q_stride, k_stride, q_out_stride, k_out_stride;
     const int *positions, *row_off;
     int batch, rows, n_q, heads;           // heads: of q and k
-    int head_dim, half, pieces, lanes;     // half: pairs of a head; pieces of V pairs, and lanes (log2) of a head
+    int head_dim, half, lanes;             // half: pairs of a head; lanes (log2) that have a head
     Divisor parts{1};                      // wavefronts of a row
     float scale, way;                      // way: -1 turns back
     double quarters[64];                   // quarter turns of a pair for one position
@@ -72,16 +72,20 @@ __device__ __forceinline__ void cos_sin(double quarters, float &c, float &s) {
     if (n & 2) s = -s;
 }
 
-// A wavefront has H times 64 >> lanes heads of a row. PAIRS: (2 i, 2 i + 1), else (i, i + half).
+// A wavefront has H times 64 >> lanes heads of a row, a lane two pieces of V elements of each: pieces that hold V pairs (i, i + half), or with PAIRS
+// the pieces `piece` and 1 << lanes further on, of V / 2 pairs (2 i, 2 i + 1) each (V = 1: the two elements of a pair). The dims behind the pairs are copied.
 template <typename T, int V, bool PAIRS, int H>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs<T> a) {
     typedef Bits<T, V> B;
+    constexpr bool WITHIN = PAIRS && V > 1;            // pairs within a piece
     const int id = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int r = a.parts.div(id), piece = lane & ((1 << a.lanes) - 1), at_once = 64 >> a.lanes;
     const int first = a.parts.mod(id) * H * at_once + (lane >> a.lanes);
     if (r >= a.rows || (a.row_off && r >= a.row_off[a.batch])) return;
-    const bool turns = piece < a.pieces;               // the dims behind the pairs are copied
-    const int lo = PAIRS || !turns ? 2 * V * piece : V * piece, hi = PAIRS || !turns ? lo + V : lo + a.half;
+    const int ahead = V << a.lanes, behind = 2 * V * piece - 2 * a.half;          // behind: of a piece of pairs (i, i + half) after all of them
+    const int lo = WITHIN ? V * piece : PAIRS || behind >= 0 ? 2 * V * piece : V * piece;
+    const int hi = WITHIN ? lo + ahead : PAIRS || behind >= 0 ? lo + V : lo + a.half;
+    const bool turn_lo = WITHIN ? lo < 2 * a.half : behind < 0, turn_hi = WITHIN ? hi < 2 * a.half : behind < 0;
     typename B::type x[H], y[H];
 #pragma unroll
     for (int i = 0; i < H; ++i) {
@@ -91,10 +95,11 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs<T> a) {
         y[i] = *reinterpret_cast<const typename B::at *>(p + hi);
     }
     const double position = a.positions[r];
-    float c[V], s[V];
+    float c[V], s[V];                                  // WITHIN: of lo's pairs, then of hi's
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-        cos_sin(position * a.quarters[turns ? V * piece + e : 0], c[e], s[e]);
+        const int pair = WITHIN ? ((2 * e < V ? lo : hi) >> 1) + e % ((V + 1) / 2) : V * piece + e;
+        cos_sin(position * a.quarters[min(pair, a.half - 1)], c[e], s[e]);
         c[e] *= a.scale;
         s[e] *= a.scale * a.way;
     }
@@ -102,39 +107,26 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs<T> a) {
     for (int i = 0; i < H; ++i) {
         const int h = first + i * at_once;
         if (h >= a.heads) return;
-        const bool is_q = h < a.n_q;
-        const T *from = is_q ? a.q : a.k;
-        T *to = is_q ? a.q_out : a.k_out;
-        T *p = to + (is_q ? r * a.q_out_stride + h * a.head_dim : r * a.k_out_stride + (h - a.n_q) * a.head_dim);
-        if (turns) {
-            const Floats<V> u = widen(x[i]), w = widen(y[i]);
-            Floats<V> m, n;                            // the halves as they lie, or pairs side by side
+        const bool is_q = h < a.n_q, moves = (is_q ? a.q : a.k) != (is_q ? a.q_out : a.k_out);
+        T *p = is_q ? a.q_out + r * a.q_out_stride + h * a.head_dim : a.k_out + r * a.k_out_stride + (h - a.n_q) * a.head_dim;
+        const Floats<V> u = widen(x[i]), w = widen(y[i]);
+        Floats<V> m, n;
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                // pair e: elements e of both halves, or 2 e and 2 e + 1 of the two pieces
-                const float p0 = !PAIRS || V == 1 ? u.x[e] : 2 * e < V ? u.x[2 * e % V] : w.x[2 * e % V];
-                const float p1 = !PAIRS || V == 1 ? w.x[e] : 2 * e < V ? u.x[(2 * e + 1) % V] : w.x[(2 * e + 1) % V];
-                const float r0 = p0 * c[e] - p1 * s[e], r1 = p1 * c[e] + p0 * s[e];
-                if (!PAIRS || V == 1) {
-                    m.x[e] = r0;
-                    n.x[e] = r1;
-                } else {
-                    (2 * e < V ? m : n).x[2 * e % V] = r0;
-                    (2 * e < V ? m : n).x[(2 * e + 1) % V] = r1;
-                }
-            }
-            narrow(m, x[i]);
-            narrow(n, y[i]);
-        } else if (from == to) {
-            continue;
+        for (int e = 0; e < V; ++e) {
+            const int k = 2 * e % V;                   // WITHIN: pair e is elements k and k + 1 of a piece
+            const float p0 = !WITHIN ? u.x[e] : 2 * e < V ? u.x[k] : w.x[k], p1 = !WITHIN ? w.x[e] : 2 * e < V ? u.x[(k + 1) % V] : w.x[(k + 1) % V];
+            const float r0 = p0 * c[e] - p1 * s[e], r1 = p1 * c[e] + p0 * s[e];
+            (WITHIN && 2 * e >= V ? n : m).x[WITHIN ? k : e] = r0;
+            (WITHIN && 2 * e < V ? m : n).x[WITHIN ? (k + 1) % V : e] = r1;
         }
-        *reinterpret_cast<typename B::at *>(p + lo) = x[i];
-        *reinterpret_cast<typename B::at *>(p + hi) = y[i];
+        if (turn_lo) narrow(m, x[i]);
+        if (turn_hi) narrow(n, y[i]);
+        if (turn_lo || moves) *reinterpret_cast<typename B::at *>(p + lo) = x[i];
+        if (turn_hi || moves) *reinterpret_cast<typename B::at *>(p + hi) = y[i];
     }
 }
 
 template <typename T, int V> int launch(RopeArgs<T> &a, bool pairs, hipStream_t s) {
-    a.pieces = a.half / V;
     a.lanes = __builtin_ctz((unsigned)(a.head_dim / (2 * V)));
     const int at_once = 64 >> a.lanes;
     const bool many = (int64_t)a.rows * ((a.heads + 4 * at_once - 1) / (4 * at_once)) >= 2048;
@@ -219,10 +211,10 @@ extern "C" int dkv_rope(const dkv_rope_desc *rope, const void *q, int64_t q_stri
         a.scale = rope->scale, a.way = inverse ? -1.f : 1.f;
         for (int i = 0; i < a.half; ++i) a.quarters[i] = rope->freq[i] * 0.6366197723675814;      // 2 / pi
         const bool pairs = rope->interleaved != 0;
-        // pieces of 16 bytes where they fit the pairs of a head
+        const int piece = pairs ? 2 * a.half : a.half;             // what pieces have to fit
         if constexpr (sizeof(T) == 2)
-            return a.half % 8 == 0 ? launch<T, 8>(a, pairs, s) : a.half % 4 == 0 ? launch<T, 4>(a, pairs, s) : launch<T, 1>(a, pairs, s);
-        else return a.half % 4 == 0 ? launch<T, 4>(a, pairs, s) : launch<T, 1>(a, pairs, s);
+            return piece % 8 == 0 ? launch<T, 8>(a, pairs, s) : piece % 4 == 0 ? launch<T, 4>(a, pairs, s) : launch<T, 1>(a, pairs, s);
+        else return piece % 4 == 0 ? launch<T, 4>(a, pairs, s) : launch<T, 1>(a, pairs, s);
     };
     return dtype == DKV_BF16 ? call((bf16_t *)nullptr) : call((float *)nullptr);
 }
