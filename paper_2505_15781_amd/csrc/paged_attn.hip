@@ -72,13 +72,23 @@ int64_t row_groups(const PagedCache &c, int rows, int max_rows, int G, int n) {
 // Blocks of 128 query rows, see make_plan: whether there are rows enough, whether groups of 32 are so many or the keys that are cut so long, and
 // whether keys are cut. None of them turns back with more rows.
 bool rows_for_blocks(int dtype, int head_dim, int query_rows) { return dtype == DKV_BF16 && head_dim >= 64 && query_rows > (head_dim == 128 ? 32 : 64); }
-bool blocks_for_rounds(int head_dim, int64_t groups) { return groups > (head_dim == 128 ? kWorkgroups : 3 * kWorkgroups); }
-bool blocks_for_keys(int head_dim, int64_t groups, int64_t keys) { return keys * head_dim >= 4096 * 128 && groups * keys >= kWorkgroups * 1536; }
+// e2m1, 128 dims: groups of 32 read K without LDS, and are worth more of it: up to two rounds of workgroups (16 ragged sequences of 28/4 heads, 2000 keys, 40
+// rows 41.6 us in blocks and 30.5; 4100 keys 76 and 51; 8 of 1900 keys, 64 rows 39.5 and 34.6, 2100 keys 44.6 and 37.2; 32/32 heads, 3 of 2600 keys, 150 rows 51 and 43;
+// the other way 8 of 300 keys, 64 rows 13.7 and 15.4, one of 2700 keys, 300 rows of 32/8 heads 39.4 and 44.5; more than two rounds lose: 32 of 512 keys,
+// 28/4 heads, 32 rows 20 and 33), and slices of 6144 keys each (2 of 4000 keys, 130 rows of 28/4 heads 37.3 and 31.8, 8192 keys, 40 rows of 32/32 44.7 and 36.3; one of
+// 8192 keys, 128 rows of 28/4 heads 34.1 and 37.1, 32768 keys 83 and 104). With 64 dims neither gains.
+bool four_bits(int cache_dtype, int head_dim) { return cache_dtype == DKV_E2M1 && head_dim == 128; }
+bool blocks_for_rounds(int cache_dtype, int head_dim, int64_t groups) {
+    return groups > (four_bits(cache_dtype, head_dim) ? 2 * kWorkgroups : head_dim == 128 ? kWorkgroups : 3 * kWorkgroups);
+}
+bool blocks_for_keys(int cache_dtype, int head_dim, int64_t groups, int64_t keys) {
+    return keys * head_dim >= 4096 * 128 && groups * keys >= kWorkgroups * (four_bits(cache_dtype, head_dim) ? 6144 : 1536);
+}
 bool keys_to_cut(int head_dim, int64_t keys) { return keys >= (head_dim == 64 ? 4096 : 2048); }
 int block_workgroups_per_cu(int head_dim) { return head_dim == 64 ? 3 : 1; }
 int split_tiles(int dtype, int tiles) { return dtype == DKV_BF16 && tiles > 1 ? 2 : 1; }
 
-Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int dtype, int head_dim) {
+Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int dtype, int cache_dtype, int head_dim) {
     Plan p;
     max_rows = max_rows < rows ? max_rows : rows;
     const int G = n_q_heads / c.n_kv_heads, heads = c.n_kv_heads;
@@ -127,7 +137,7 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
         const bool cut = (wide == 2 || head_dim == 64) && keys_to_cut(head_dim, keys) &&
                          (slices >= 2 * c.batch || (ragged && 3 * slices >= 4 * c.batch));
         if (cut && head_dim == 64) wide = 1;
-        if (blocks_for_rounds(head_dim, groups) || (cut && blocks_for_keys(head_dim, groups, keys))) {
+        if (blocks_for_rounds(cache_dtype, head_dim, groups) || (cut && blocks_for_keys(cache_dtype, head_dim, groups, keys))) {
             p.wide = wide;
             p.blocks = (int)blocks;
             p.nq = 8;
@@ -169,7 +179,7 @@ size_t partial_bytes(const Plan &p, const PagedCache &c, int head_dim) {
 // What no plan of this many rows and fewer exceeds, so that one workspace serves an active set that shrinks (fewer rows can have more slices: 28/4
 // heads, 8 sequences of 4096 keys, none with 128 rows each, 17 MB with 64, 4 with 8). The slices of a plan times its K/V heads and query groups are
 // one round of workgroups at most (slices_at_once), and no sequence has slices of less than `least` tiles.
-size_t most_partial_bytes(const PagedCache &c, int n_q_heads, int rows, int max_rows, int dtype, int head_dim) {
+size_t most_partial_bytes(const PagedCache &c, int n_q_heads, int rows, int max_rows, int dtype, int cache_dtype, int head_dim) {
     max_rows = max_rows < rows ? max_rows : rows;
     const int G = n_q_heads / c.n_kv_heads, tiles = ceil_div(max_rows > 0 ? max_rows * G : 1, 16), key_tiles = ceil_div(c.max_pages << c.page_shift, PKT);
     if (key_tiles <= whole_tiles(dtype, head_dim)) return 0;
@@ -184,7 +194,7 @@ size_t most_partial_bytes(const PagedCache &c, int n_q_heads, int rows, int max_
     const size_t split = bytes(split_tiles(dtype, tiles), kLeast, 1);
     const int64_t groups = row_groups(c, rows, max_rows, G, 32), keys = (int64_t)key_tiles * PKT;
     if (!rows_for_blocks(dtype, head_dim, max_rows * G) || !keys_to_cut(head_dim, keys) ||
-        !(blocks_for_rounds(head_dim, groups) || blocks_for_keys(head_dim, groups, keys)))
+        !(blocks_for_rounds(cache_dtype, head_dim, groups) || blocks_for_keys(cache_dtype, head_dim, groups, keys)))
         return split;
     const size_t blocks = bytes(8, kLeastWide, block_workgroups_per_cu(head_dim));
     return blocks > split ? blocks : split;
@@ -272,7 +282,7 @@ int dkv_paged_attn_plan(const dkv_paged_cache *cache, PagedCache &view, PagedAtt
     if (cache->dtype != dtype && cache->dtype != DKV_E4M3 && cache->dtype != DKV_E2M1) { dkv_set_error("rows of dtype %d do not read a cache of dtype %d", dtype, cache->dtype); return DKV_E_UNSUPPORTED; }
     if ((int64_t)rows * n_q_heads < 1 << 24 && (int64_t)cache->batch * cache->n_kv_heads < 1 << 22 &&
         (int64_t)cache->batch * cache->max_pages * cache->page_size <= 1ll << 35) {
-        plan = make_plan(view, n_q_heads, rows, max_rows_per_seq, dtype, cache->head_dim);
+        plan = make_plan(view, n_q_heads, rows, max_rows_per_seq, dtype, cache->dtype, cache->head_dim);
         if (plan.wide && !plan.split ? plan.blocks < 1 << 23 : split_grid(plan, view) < 1 << 22) return DKV_OK;
     }
     dkv_set_error("%d rows of %d heads in %d sequences are too many for one call", rows, n_q_heads, cache->batch);
@@ -284,7 +294,7 @@ extern "C" size_t dkv_paged_attn_workspace_bytes(const dkv_paged_cache *cache, i
     PagedCache c;
     Plan p;
     if (dkv_paged_attn_plan(cache, c, p, n_q_heads, rows, max_rows_per_seq, dtype)) return 0;
-    return align_up(most_partial_bytes(c, n_q_heads, rows, max_rows_per_seq, dtype, cache->head_dim) + 256, 256);
+    return align_up(most_partial_bytes(c, n_q_heads, rows, max_rows_per_seq, dtype, cache->dtype, cache->head_dim) + 256, 256);
 }
 
 extern "C" int dkv_paged_attn(const dkv_paged_cache *cache, const void *q, int64_t q_stride, const int32_t *row_off, void *out,

@@ -327,6 +327,7 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
                        bf16x8 (&pn)[2]) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) sn[v] = 0.f;
+        if constexpr (DH == 64) __builtin_amdgcn_s_setprio(1);
         f32x8 p[2];
         constexpr int MT = DH / 32, N = DH / 16, PER = 16 / N;        // products of the scores, and of the output; exponentials next to each two
 #pragma unroll
@@ -341,6 +342,7 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) pn[ks] = __builtin_convertvector(p[ks], bf16x8);
         asm volatile("" : "+v"(pn[0]), "+v"(pn[1]));        // here, not behind the branches of maximum()
+        if constexpr (DH == 64) __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
         __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
 #pragma unroll

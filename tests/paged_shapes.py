@@ -21,9 +21,16 @@ CALLS = {
     "halves_cut_ragged": ([6500, 40, 2100], [100, 70, 129], 32, 2, 4, 128, "wide2+"),
 }
 BLOCKS = [name for name in CALLS if CALLS[name][6].startswith("wide")]
+# Over an e2m1 cache, whose blocks of 128 query rows begin later with 128 dims, the same kernels.
+E2M1_CALLS = CALLS | {
+    "blocks": ([200, 90], [300, 40], 16, 16, 4, 128, "wide1"),
+    "halves": ([700, 333], [300, 40], 16, 12, 4, 128, "wide2"),
+    "halves_cut": ([11000], [300], 16, 4, 4, 128, "wide2+"),
+    "halves_cut_ragged": ([6500, 40, 2100], [400, 70, 129], 32, 2, 8, 128, "wide2+"),
+}
 
 
-def plan_of(name, cache_dtype, dtype=0):
+def plan_of(name, cache_dtype, dtype=0, calls=CALLS):
     """The plan of a call with a table one page wider than the longest sequence."""
-    lens, counts, page, heads, group, dh, _ = CALLS[name]
+    lens, counts, page, heads, group, dh, _ = calls[name]
     return paged_plan(heads * group, sum(counts), max(counts), dtype, len(lens), max(-(-n // page) for n in lens) + 1, page, heads, dh, cache_dtype)

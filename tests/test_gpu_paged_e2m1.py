@@ -12,7 +12,7 @@ import paper_2505_15781_amd as P
 import test_gpu_paged as paged
 import test_gpu_paged_calls as calls
 from oracle import paged as O
-from paged_shapes import BLOCKS, CALLS, plan_of
+from paged_shapes import BLOCKS, E2M1_CALLS, plan_of
 from test_gpu_paged import ATTN, TORCH, Cache, check_attn, dev, rows, workspace
 
 pytestmark = pytest.mark.gpu
@@ -159,16 +159,16 @@ def test_attention(act, case, holes):
 
 
 def make(name, types, seed, size=1.0):
-    lens, counts, page, heads, group, dh, kernel = CALLS[name]
+    lens, counts, page, heads, group, dh, kernel = E2M1_CALLS[name]
     act, dtype = types.split()
     if act == "bf16":
-        assert plan_of(name, P.E2M1).kernel == kernel
+        assert plan_of(name, P.E2M1, calls=E2M1_CALLS).kernel == kernel
     c = FourBits(lens, page, heads, dh, seed=seed).fill(act, size=size)
     extra = min(2, len(counts) * max(counts) - sum(counts))
     return c, rows(np.random.default_rng(seed), (sum(counts) + extra, heads * group, dh), act), counts
 
 
-EVERY = [(name, act + " e2m1") for name in CALLS for act in (("bf16",) if name in BLOCKS else ("bf16", "fp32"))]
+EVERY = [(name, act + " e2m1") for name in E2M1_CALLS for act in (("bf16",) if name in BLOCKS else ("bf16", "fp32"))]
 
 
 @pytest.mark.parametrize("name,types", EVERY, ids=[n + "-" + t.replace(" ", "-") for n, t in EVERY])
@@ -180,6 +180,7 @@ def test_every_kernel(name, types, check, monkeypatch):
     """What test_gpu_paged_calls.py asks of the other caches (an infinity or a NaN is one of 32 dims here)."""
     monkeypatch.setattr(calls, "Cache", FourBits)
     monkeypatch.setattr(calls, "make", make)
+    monkeypatch.setattr(calls, "CALLS", E2M1_CALLS)
     getattr(calls, "test_" + check)(name, types)
 
 

@@ -7,9 +7,11 @@ import torch
 
 import paper_2505_15781_amd as P
 from oracle import paged as O
-from paged_shapes import CALLS, plan_of
+from paged_shapes import CALLS, E2M1_CALLS, plan_of
 from paper_2505_15781_amd import binding as B
+from plans import paged_plan
 from test_paged_cpu import ALL, CACHE_FAULTS, attn, calls, desc, load, store
+from test_paged_plan_cpu import need
 
 
 def test_codes_and_rounding_of_the_oracle():
@@ -70,12 +72,42 @@ def test_what_is_refused_and_what_is_not():
     assert store(cache_dtype=5) == -1 and "dtype" in B.last_error()
 
 
-@pytest.mark.parametrize("dtype", [P.BF16, P.FP32])
-@pytest.mark.parametrize("name", CALLS)
-def test_plans_are_those_of_the_other_caches(name, dtype):
-    """A cache of any type takes the kernel that the calls of the GPU tests are there for."""
-    a, b = plan_of(name, P.E2M1, dtype), plan_of(name, P.E4M3, dtype)
-    assert [getattr(a, f) for f, _ in a._fields_] == [getattr(b, f) for f, _ in b._fields_]
+@pytest.mark.parametrize("name", E2M1_CALLS)
+def test_the_calls_of_the_gpu_tests_take_the_kernels_they_are_there_for(name):
+    """A threshold that moves must not take a kernel out of the tests: then these shapes move with it."""
+    assert plan_of(name, P.E2M1, calls=E2M1_CALLS).kernel == E2M1_CALLS[name][6]
+    assert plan_of(name, P.E2M1, P.FP32, E2M1_CALLS).kernel in ("split", "split+")
+
+
+def test_the_calls_take_every_kernel():
+    kinds = lambda calls: {(c[6], c[5] if c[6].startswith("wide") else 0) for c in calls.values()}
+    assert kinds(E2M1_CALLS) == kinds(CALLS)
+
+
+@pytest.mark.parametrize("group,heads,dh,batch,keys,dtype", [
+    (7, 4, 128, 8, 4096, P.BF16), (7, 4, 128, 1, 32768, P.BF16), (1, 32, 128, 4, 2100, P.BF16), (16, 1, 64, 6, 9000, P.BF16), (4, 8, 64, 2, 100000, P.BF16),
+    (3, 8, 32, 3, 5000, P.BF16), (4, 2, 128, 5, 1000, P.FP32), (8, 24, 128, 2, 700, P.BF16), (1, 1, 128, 100, 2000, P.BF16), (16, 1, 128, 2, 50000, P.BF16)])
+def test_a_workspace_for_many_rows_is_enough_for_fewer(group, heads, dh, batch, keys, dtype):
+    sizes = dict(batch=batch, max_pages=-(-keys // 16), page_size=16, n_kv_heads=heads, head_dim=dh, cache_dtype=P.E2M1)
+    d = B.PagedCacheDesc(16, 16, 16, 16, 16, 16, batch, batch * sizes["max_pages"], sizes["max_pages"], 16, heads, dh, P.E2M1)
+    largest = 0
+    for m in (1, 2, 3, 5, 8, 12, 16, 20, 33, 40, 64, 80, 96, 128, 130, 200, 300, 513, 1000):
+        for rows in sorted({m, m + 1, batch * m // 3, batch * m * 3 // 4, batch * m - 1, batch * m}):
+            if 1 <= rows <= batch * m:
+                largest = max(largest, need(paged_plan(group * heads, rows, m, dtype, **sizes), batch, heads, dh))
+        assert B.lib.dkv_paged_attn_workspace_bytes(C.byref(d), group * heads, batch * m, m, dtype) >= largest, m
+    assert largest > 0
+
+
+@pytest.mark.parametrize("heads,rows,keys,kernel", [
+    (32, 64, 1000, "wide2"), (31, 64, 1000, "split"),      # up to two rounds of 256 groups of 32 query rows: 8 sequences of 64 (31 heads: 496)
+    (4, 1024, 12320, "wide2+"), (4, 1024, 12256, "split+")])
+def test_where_blocks_of_128_rows_begin(heads, rows, keys, kernel):
+    """128 dims: from 513 groups on, or from 6144 keys a slice of 256 on (4 heads, 128 groups: 12288 keys)."""
+    batch = 8 if rows == 64 else 1
+    extra = 1 if rows == 64 and kernel == "wide2" else 0
+    p = paged_plan(heads, batch * rows + extra * batch, rows + extra, P.BF16, batch, -(-keys // 32), 32, heads, 128, P.E2M1)
+    assert p.kernel == kernel
 
 
 def tensors():
