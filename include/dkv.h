@@ -346,7 +346,7 @@ int dkv_paged_attn(const dkv_paged_cache *cache, const void *q, int64_t q_stride
  *   page_table (dev) [batch][max_pages], seq_len (dev) [batch]: as in dkv_paged_cache
  *   free_pages (dev) [n_pages]: a ring of the numbers of the free pages; free_at (dev) [2]: the place of the first of them, and how many
  *                    there are. A cache without sequences has free_pages = 0 .. n_pages - 1, free_at = {0, n_pages} and seq_len = 0.
- * page_size, max_pages as in dkv_paged_cache; at most 2^30 pages and 2^20 sequences. Nothing is kept by a call. */
+ * page_size, max_pages as in dkv_paged_cache; at most 2^30 pages, 2^20 sequences, and fewer than 2^31 entries of a table. Nothing is kept by a call. */
 typedef struct {
     int32_t *page_table, *seq_len, *free_pages, *free_at;
     int32_t batch, n_pages, max_pages, page_size;

@@ -329,6 +329,7 @@ extern "C" int dkv_paged_resize(const dkv_paged_tables *tables, const int32_t *l
         dkv_set_error("page_size %d not supported (a power of two, 16 to 65536)", c.page_size); return DKV_E_UNSUPPORTED;
     }
     if ((int64_t)c.max_pages * c.page_size > 1 << 30) { dkv_set_error("the table covers more than 2^30 positions"); return DKV_E_UNSUPPORTED; }
+    if ((int64_t)c.batch * c.max_pages >= 1ll << 31) { dkv_set_error("tables of 2^31 entries and more are not supported"); return DKV_E_UNSUPPORTED; }
     if (c.n_pages > 1 << 30 || c.batch > kMostSequences || rows > 1 << 30) { dkv_set_error("%d pages, %d sequences or %d rows are too many for one call", c.n_pages, c.batch, rows); return DKV_E_UNSUPPORTED; }
     if ((positions || slots) && !row_off) { dkv_set_error("positions and slots go with row_off"); return DKV_E_INVALID_ARG; }
     if (!workspace || workspace_bytes < work_bytes(c.batch)) {

@@ -52,6 +52,7 @@ def test_refused_arguments():
     for size in (8, 0, 48, 131072, -16):
         assert resize(page_size=size) == -3
     assert resize(max_pages=(1 << 26) + 1) == -3 == resize(n_pages=(1 << 30) + 1) == resize(batch=(1 << 20) + 1) == resize(rows=(1 << 30) + 1)
+    assert resize(batch=32, max_pages=1 << 26) == -3 and "2^31" in B.last_error()
     assert resize(ws=None) == -4 == resize(nbytes=16) == resize(nbytes=P.paged_resize_workspace_bytes(3) - 1)
     assert resize(ws=24) == -1
     assert B.lib.dkv_paged_resize(None, 16, 16, 16, 16, 9, 16, 1 << 20, None) == -1
