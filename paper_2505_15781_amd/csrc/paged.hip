@@ -54,6 +54,13 @@ template <typename T> __device__ __forceinline__ Piece<16> load_piece(const T *p
 }
 __device__ __forceinline__ void store_piece(float *p, Piece<4> x) { *reinterpret_cast<f32x4_el *>(p) = x; }
 __device__ __forceinline__ void store_piece(bf16_t *p, Piece<8> x) { store8(p, x); }
+// with the non-temporal hint
+__device__ __forceinline__ void store_piece_nt(float *p, Piece<4> x) { __builtin_nontemporal_store((f32x4)x, reinterpret_cast<f32x4_el *>(p)); }
+__device__ __forceinline__ void store_piece_nt(bf16_t *p, Piece<8> x) {
+    u32x4 y;
+    store8(reinterpret_cast<bf16_t *>(&y), x);
+    __builtin_nontemporal_store(y, reinterpret_cast<bf16x8_el *>(p));
+}
 
 // Maximum over the 2, 4 or 8 neighbouring lanes that hold a row.
 template <int LANES> __device__ __forceinline__ float row_max(float x) {
@@ -183,7 +190,9 @@ __global__ __launch_bounds__(256) void paged_load_kernel(PagedCache c, T *__rest
         if (i >= pieces) return;
         if constexpr (kRowScales<C, DH> > 0) x[u] *= scale[u];
         if (page < 0) x[u] = 0.f;
-        store_piece((i / P % 2 ? v_out : k_out) + ((size_t)w.r * c.n_kv_heads + i / (2 * P)) * DH + E * (i % P), x[u]);
+        T *to = (i / P % 2 ? v_out : k_out) + ((size_t)w.r * c.n_kv_heads + i / (2 * P)) * DH + E * (i % P);
+        if constexpr (N > 1) store_piece_nt(to, x[u]);
+        else store_piece(to, x[u]);
     }
 }
 

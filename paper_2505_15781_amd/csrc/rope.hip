@@ -121,8 +121,12 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs<T> a) {
         }
         if (turn_lo) narrow(m, x[i]);
         if (turn_hi) narrow(n, y[i]);
-        if (turn_lo || moves) *reinterpret_cast<typename B::at *>(p + lo) = x[i];
-        if (turn_hi || moves) *reinterpret_cast<typename B::at *>(p + hi) = y[i];
+        auto put = [&](typename B::type v, T *to) {
+            if constexpr (H > 1) __builtin_nontemporal_store(v, reinterpret_cast<typename B::at *>(to));
+            else *reinterpret_cast<typename B::at *>(to) = v;
+        };
+        if (turn_lo || moves) put(x[i], p + lo);
+        if (turn_hi || moves) put(y[i], p + hi);
     }
 }
 
