@@ -10,6 +10,8 @@
 // e2m1 has codes up to 6 and one bit behind the leading one: a whole row under one scale would lose its small elements, so 32 dims share
 // one (OCP's microscaling format). e is E - 2, or E - 1 where m > 1.5: nothing is cut off, and each element is rounded once, to 2 significant
 // bits, or by 2^(e - 2). There is no code for NaN; a block with an infinity or a NaN has the scale 255, which makes all of it NaN.
+#include <type_traits>
+
 #include "paged.h"
 
 namespace {
@@ -30,8 +32,8 @@ __device__ __forceinline__ int scale_exponent_e2m1(uint32_t bits) {        // of
     return min(max(e, kLowestExponent), kHighestExponentE2M1);
 }
 
-// Elements of a lane: 16 bytes of what is written, or for e2m1 (4 bytes) of the bf16 rows that are read.
-template <typename W> constexpr int kPiece = kE2M1<W> ? 8 : 16 / (int)sizeof(W);
+// Elements of a lane: 16 bytes of what is written.
+template <typename W> constexpr int kPiece = 16 / (int)sizeof(W);
 template <int N> using Piece = float __attribute__((ext_vector_type(N)));
 
 __device__ __forceinline__ Piece<4> load_piece(const float *p, Piece<4> *) { return *reinterpret_cast<const f32x4_el *>(p); }
@@ -160,6 +162,50 @@ __global__ __launch_bounds__(256) void paged_store_kernel(PagedCache c, const T 
     put<DH>(const_cast<C *>(piece_of<C, DH>(is_v ? c.v : c.k, at, 0, E)), scale_of<C, DH>(is_v ? c.vs : c.ks, at, piece, E), piece, x);
 }
 
+// e2m1: rows of a head lie one behind the other in a page, in 64 bytes and 4 of scales for 128 dims, parts of a line of memory. So a wavefront has
+// several rows of one head, and a workgroup 8 wavefronts of them: positions that follow on each other fill whole lines from one workgroup, and thus
+// from one XCD's L2. N heads (of K, then V) to a wavefront.
+template <typename T, int DH, int N>
+__global__ __launch_bounds__(512) void paged_store_e2m1(PagedCache c, const T *__restrict__ k_new, const T *__restrict__ v_new, int64_t row_stride,
+                                                        const int *__restrict__ positions, const int *__restrict__ row_off, int rows, Divisor parts) {
+    constexpr int P = DH / 8, R = 64 / P;             // lanes that hold a row of a head, rows of a wavefront
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), piece = lane % P;
+    const int first = (parts.div((int)blockIdx.x) * 8 + wave) * R, unit = parts.mod((int)blockIdx.x) * N, r = first + lane / P;
+    if (first >= rows) return;
+    const int from = min(r, rows - 1);
+    Piece<8> x[N];
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        const int i = min(unit + u, 2 * c.n_kv_heads - 1), is_v = i >= c.n_kv_heads;
+        x[u] = load_piece((is_v ? v_new : k_new) + from * row_stride + (is_v ? i - c.n_kv_heads : i) * DH + 8 * piece, (Piece<8> *)nullptr);
+    }
+    const int p = positions[from];
+    int b = from;                                     // the row's sequence: see sequence_of_row
+    if (row_off) {
+        b = 0;
+        for (int i = 0; i < c.batch; i += 64) {
+            const int upto = row_off[min(i + lane, c.batch - 1) + 1];
+            int last = 0;
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                last = __popcll(__ballot(i + lane < c.batch && upto <= first + k));
+                if (lane / P == k) b += last;
+            }
+            if (last < 64) break;
+        }
+    }
+    if (r >= rows || b >= c.batch) return;
+    const int page = c.page(b, p), slot = p & (c.page_size() - 1);
+    if (page < 0) return;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        const int i = unit + u, is_v = i >= c.n_kv_heads;
+        if (i >= 2 * c.n_kv_heads) return;
+        const uint32_t at = c.row(page, is_v ? i - c.n_kv_heads : i, slot);
+        put<DH>(const_cast<e2m1_t *>(piece_of<e2m1_t, DH>(is_v ? c.v : c.k, at, 0, 8)), scale_of<e2m1_t, DH>(is_v ? c.vs : c.ks, at, piece, 8), piece, x[u]);
+    }
+}
+
 // A lane writes N times 16 bytes. Its loads are short where the cache is e4m3 (8 bytes for bf16 rows, 4 for fp32), and wait for the
 // row's place: with many rows four at once are ahead, 16384 rows of 32 heads 87 us against 105, 64 rows 3.2 against 2.5. They meet at
 // 4096 wavefronts of four pieces a lane (32 heads of 128 to bf16: 512 rows 5.6 against 4.9, 1024 rows 7.3 and 7.5, 2048 rows 14.2 and 16.4; 8 heads of 64 to fp32,
@@ -196,18 +242,10 @@ __global__ __launch_bounds__(256) void paged_load_kernel(PagedCache c, T *__rest
     }
 }
 
-// Calls f(element type of the rows, of the cache, head_dim) for the combination at hand.
-template <typename F> int with_types(int dtype, int cache_dtype, int head_dim, F f) {
-    auto heads = [&](auto t, auto c) {
-        return head_dim == 32 ? f(t, c, Size<32>{}) : head_dim == 64 ? f(t, c, Size<64>{}) : f(t, c, Size<128>{});
-    };
-    auto caches = [&](auto t) {
-        return cache_dtype == DKV_BF16   ? heads(t, Type<bf16_t>{})
-               : cache_dtype == DKV_FP32 ? heads(t, Type<float>{})
-               : cache_dtype == DKV_E4M3 ? heads(t, Type<e4m3_t>{})
-                                         : heads(t, Type<e2m1_t>{});
-    };
-    return dtype == DKV_BF16 ? caches(Type<bf16_t>{}) : caches(Type<float>{});
+// Calls f(element type of the rows, head_dim) for the combination at hand.
+template <typename F> int with_heads(int dtype, int head_dim, F f) {
+    auto heads = [&](auto t) { return head_dim == 32 ? f(t, Size<32>{}) : head_dim == 64 ? f(t, Size<64>{}) : f(t, Size<128>{}); };
+    return dtype == DKV_BF16 ? heads(Type<bf16_t>{}) : heads(Type<float>{});
 }
 
 }  // namespace
@@ -248,11 +286,12 @@ int rows_call(const dkv_paged_cache *cache, PagedCache &view, const void *k, con
     return DKV_OK;
 }
 int64_t row_pieces(const dkv_paged_cache &c, int written) {
-    return 2 * (int64_t)(written == DKV_E2M1 ? c.head_dim / 8 : c.head_dim * (written == DKV_BF16 ? 2 : written == DKV_FP32 ? 4 : 1) / 16) * c.n_kv_heads;
+    return 2 * (int64_t)(c.head_dim * (written == DKV_BF16 ? 2 : written == DKV_FP32 ? 4 : 1) / 16) * c.n_kv_heads;
 }
+int too_many(int rows, int heads) { dkv_set_error("%d rows of %d heads are too many for one call", rows, heads); return DKV_E_UNSUPPORTED; }
 template <typename F> int rows_launch(const dkv_paged_cache &c, int written, int n, int rows, F f) {
     const int64_t waves = (row_pieces(c, written) + 64 * n - 1) / (64 * n), groups = (waves * rows + 3) / 4;
-    if (rows >= 1 << 24 || groups >= 1 << 23) { dkv_set_error("%d rows of %d heads are too many for one call", rows, c.n_kv_heads); return DKV_E_UNSUPPORTED; }
+    if (rows >= 1 << 24 || groups >= 1 << 23) return too_many(rows, c.n_kv_heads);
     return rows == 0 ? DKV_OK : f((unsigned)groups, Divisor((int)waves));
 }
 }  // namespace
@@ -263,14 +302,37 @@ extern "C" int dkv_paged_store(const dkv_paged_cache *cache, const void *k_new, 
     const int rc = rows_call(cache, c, k_new, v_new, positions, row_off, rows, dtype);
     if (rc) return rc;
     if (row_stride < (int64_t)cache->n_kv_heads * cache->head_dim) { dkv_set_error("row stride %lld is less than a row", (long long)row_stride); return DKV_E_INVALID_ARG; }
-    return rows_launch(*cache, cache->dtype, 1, rows, [&](unsigned groups, Divisor waves) {
-        return with_types(dtype, cache->dtype, cache->head_dim, [&](auto t, auto ct, auto dh) {
+    if (cache->dtype == DKV_E2M1) {
+        const int at_once = 8 * 64 / (cache->head_dim / 8);             // rows of a workgroup
+        const int64_t blocks = ((int64_t)rows + at_once - 1) / at_once, units = 2 * (int64_t)cache->n_kv_heads;
+        const int n = blocks * units >= 2048 ? 4 : 1;
+        const int64_t parts = (units + n - 1) / n;
+        if (rows >= 1 << 24 || blocks * parts >= 1 << 23) return too_many(rows, cache->n_kv_heads);
+        if (rows == 0) return DKV_OK;
+        return with_heads(dtype, cache->head_dim, [&](auto t, auto dh) {
             typedef typename decltype(t)::type T;
-            typedef typename decltype(ct)::type C;
-            hipLaunchKernelGGL((paged_store_kernel<T, C, decltype(dh)::value>), dim3(groups), dim3(256), 0,
-                               static_cast<hipStream_t>(stream), c, (const T *)k_new, (const T *)v_new, row_stride, positions, row_off, rows, waves);
-            DKV_LAUNCH_CHECK();
-            return DKV_OK;
+            auto launch = [&](auto kernel) {
+                hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks * parts)), dim3(512), 0, static_cast<hipStream_t>(stream), c, (const T *)k_new,
+                                   (const T *)v_new, row_stride, positions, row_off, rows, Divisor((int)parts));
+                DKV_LAUNCH_CHECK();
+                return DKV_OK;
+            };
+            return n == 4 ? launch(paged_store_e2m1<T, decltype(dh)::value, 4>) : launch(paged_store_e2m1<T, decltype(dh)::value, 1>);
+        });
+    }
+    return rows_launch(*cache, cache->dtype, 1, rows, [&](unsigned groups, Divisor waves) {
+        return with_heads(dtype, cache->head_dim, [&](auto t, auto dh) {
+            typedef typename decltype(t)::type T;
+            auto launch = [&](auto kernel) {
+                hipLaunchKernelGGL(kernel, dim3(groups), dim3(256), 0, static_cast<hipStream_t>(stream), c, (const T *)k_new, (const T *)v_new,
+                                   row_stride, positions, row_off, rows, waves);
+                DKV_LAUNCH_CHECK();
+                return DKV_OK;
+            };
+            constexpr int DH = decltype(dh)::value;
+            return cache->dtype == DKV_BF16   ? launch(paged_store_kernel<T, bf16_t, DH>)
+                   : cache->dtype == DKV_FP32 ? launch(paged_store_kernel<T, float, DH>)
+                                              : launch(paged_store_kernel<T, e4m3_t, DH>);
         });
     });
 }
@@ -282,17 +344,19 @@ extern "C" int dkv_paged_load(const dkv_paged_cache *cache, void *k_out, void *v
     if (rc) return rc;
     const int n = (cache->dtype == DKV_E4M3 || cache->dtype == DKV_E2M1) && rows * ((row_pieces(*cache, dtype) + 255) / 256) >= 4096 ? 4 : 1;
     return rows_launch(*cache, dtype, n, rows, [&](unsigned groups, Divisor waves) {
-        return with_types(dtype, cache->dtype, cache->head_dim, [&](auto t, auto ct, auto dh) {
+        return with_heads(dtype, cache->head_dim, [&](auto t, auto dh) {
             typedef typename decltype(t)::type T;
-            typedef typename decltype(ct)::type C;
-            auto launch = [&](auto pieces) {
-                hipLaunchKernelGGL((paged_load_kernel<T, C, decltype(dh)::value, decltype(pieces)::value>), dim3(groups), dim3(256), 0,
-                                   static_cast<hipStream_t>(stream), c, (T *)k_out, (T *)v_out, positions, row_off, rows, waves);
+            auto launch = [&](auto kernel) {
+                hipLaunchKernelGGL(kernel, dim3(groups), dim3(256), 0, static_cast<hipStream_t>(stream), c, (T *)k_out, (T *)v_out, positions, row_off,
+                                   rows, waves);
                 DKV_LAUNCH_CHECK();
                 return DKV_OK;
             };
-            if constexpr (kRowScales<C, decltype(dh)::value> > 0) return n == 4 ? launch(Size<4>{}) : launch(Size<1>{});
-            else return launch(Size<1>{});
+            constexpr int DH = decltype(dh)::value;
+            if (cache->dtype == DKV_BF16) return launch(paged_load_kernel<T, bf16_t, DH, 1>);
+            if (cache->dtype == DKV_FP32) return launch(paged_load_kernel<T, float, DH, 1>);
+            if (cache->dtype == DKV_E4M3) return n == 4 ? launch(paged_load_kernel<T, e4m3_t, DH, 4>) : launch(paged_load_kernel<T, e4m3_t, DH, 1>);
+            return n == 4 ? launch(paged_load_kernel<T, e2m1_t, DH, 4>) : launch(paged_load_kernel<T, e2m1_t, DH, 1>);
         });
     });
 }

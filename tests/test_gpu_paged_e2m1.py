@@ -93,6 +93,26 @@ def test_many_rows_are_read_back(out, heads, dh):
     assert np.array_equal(ko.double().cpu().numpy(), wk) and np.array_equal(vo.double().cpu().numpy(), wv)
 
 
+@pytest.mark.parametrize("act,heads,dh", [("bf16", 33, 128), ("fp32", 33, 128), ("fp32", 45, 64), ("bf16", 45, 64), ("bf16", 97, 32), ("fp32", 97, 32)])
+def test_many_rows_are_stored(act, heads, dh):
+    """Calls large enough that a wavefront has several heads, the last ones not all there: more sequences than it has lanes, some without rows, positions in any
+    order, some without a page; rows of no sequence, which are parts of longer ones."""
+    g = np.random.default_rng(dh)
+    lens = g.integers(0, 45, 71)
+    c = FourBits([int(n) for n in lens], 16, heads, dh, seed=heads, holes=0.1)
+    counts = np.where(g.random(71) < 0.2, 0, lens)
+    counts[70] = 0
+    off = np.concatenate([[0], np.cumsum(counts)])
+    n = int(off[-1]) + 3
+    assert -(-n // (4096 // dh)) * 2 * heads >= 2048
+    pos = np.concatenate([g.permutation(int(lens[b]))[:counts[b]] for b in range(71)] + [[0, 1, 2]]).astype(int)
+    wide = rows(g, (n, 2 * heads + 1, dh), act)
+    k, v = wide[:, :heads], wide[:, heads + 1:]
+    P.paged_store(c.t, k, v, dev(pos), dev(off))
+    O.store(c.o, k.double().cpu().numpy(), v.double().cpu().numpy(), pos, off, "e2m1")
+    assert c.same()
+
+
 def test_every_bf16_value_is_quantised_as_the_oracle_does():
     """All 65536 bit patterns, 32 to a block: blocks of one magnitude (all exponents, zeros, infinities, NaN) and shuffled ones."""
     bits = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
