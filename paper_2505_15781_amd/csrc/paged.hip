@@ -164,7 +164,9 @@ __global__ __launch_bounds__(256) void paged_store_kernel(PagedCache c, const T 
 
 // e2m1: rows of a head lie one behind the other in a page, in 64 bytes and 4 of scales for 128 dims, parts of a line of memory. So a wavefront has
 // several rows of one head, and a workgroup 8 wavefronts of them: positions that follow on each other fill whole lines from one workgroup, and thus
-// from one XCD's L2. N heads (of K, then V) to a wavefront.
+// from one XCD's L2. N heads (of K, then V) to a wavefront, four where that leaves 512 workgroups. 6144 rows of 32 heads of 128 29.4 us (127 MB, 4.3 TB/s;
+// N = 1 35.3; a wavefront to a part of one row, as above, 32.5), fp32 43.7 (5.2 TB/s), 64 rows 2.8 us (N = 4: 3.8). Written with the non-temporal hint the
+// same store takes 1 us less, and a load of these rows behind it 10 more.
 template <typename T, int DH, int N>
 __global__ __launch_bounds__(512) void paged_store_e2m1(PagedCache c, const T *__restrict__ k_new, const T *__restrict__ v_new, int64_t row_stride,
                                                         const int *__restrict__ positions, const int *__restrict__ row_off, int rows, Divisor parts) {
@@ -206,11 +208,11 @@ __global__ __launch_bounds__(512) void paged_store_e2m1(PagedCache c, const T *_
     }
 }
 
-// A lane writes N times 16 bytes. Its loads are short where the cache is e4m3 (8 bytes for bf16 rows, 4 for fp32), and wait for the
-// row's place: with many rows four at once are ahead, 16384 rows of 32 heads 87 us against 105, 64 rows 3.2 against 2.5. They meet at
-// 4096 wavefronts of four pieces a lane (32 heads of 128 to bf16: 512 rows 5.6 against 4.9, 1024 rows 7.3 and 7.5, 2048 rows 14.2 and 16.4; 8 heads of 64 to fp32,
-// 4096 rows 6.6 and 7.3). From bf16 and fp32 caches one is. 6144 rows from e4m3 to bf16 35 us (4.3 TB/s), from bf16 to bf16 42 (4.8), to fp32 75 (4.0), from fp32
-// to fp32 72 (5.6).
+// A lane writes N times 16 bytes. Its loads are short where the cache is e4m3 (8 bytes for bf16 rows, 4 for fp32) or e2m1 (half of that), and wait for the
+// row's place: with many rows four at once are ahead. They meet at 4096 wavefronts of four pieces a lane (32 heads of 128 from e4m3 to bf16: 512 rows 5.6
+// against 4.9, 1024 rows 7.3 and 7.5, 2048 rows 14.2 and 16.4). From bf16 and fp32 caches one is. So many rows are more than the caches hold until somebody reads
+// them: four pieces are written with the non-temporal hint (6144 rows of 32 heads from e2m1 to bf16 38.4 -> 26.5 us, 4.8 TB/s, to fp32 62.6 -> 39.0, 5.8; from e4m3 to bf16
+// 35 -> 25.2, 6.0; 2048 rows 14.2 -> 11.3). From bf16 to bf16 42 (4.8 TB/s), to fp32 75 (4.0), from fp32 to fp32 72 (5.6).
 template <typename T, typename C, int DH, int N>
 __global__ __launch_bounds__(256) void paged_load_kernel(PagedCache c, T *__restrict__ k_out, T *__restrict__ v_out,
                                                          const int *__restrict__ positions, const int *__restrict__ row_off, int rows,

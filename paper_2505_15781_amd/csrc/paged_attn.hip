@@ -104,7 +104,7 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     // Blocks of 128 query rows (paged_wide.h) where tiles of 32 would make more than one round of workgroups (128 dims; 28/4 heads, 1024 keys: 1
     // sequence of 300 rows, 264 workgroups, 29 -> 26 us, 4 of 128 rows, 448, 30 -> 27, but 4 of 64 rows, 224, 17 -> 26) or more than three (64
     // dims, 32 heads, 8 ragged sequences of up to 5600 keys: bf16, 80 rows 61 -> 61, 128 rows 81 -> 70, 250 rows, 119 -> 104; e4m3 65 ->
-    // 68, 94 -> 77, 144 -> 125; of 700 keys each 24.1 -> 21, 32 -> 22, 59 -> 32). Also where the
+    // 68, 94 -> 77, 144 -> 125, since then 63 and 103 in blocks; of 700 keys each 24.1 -> 21, 32 -> 22, 59 -> 32). Also where the
     // keys are so many that slices of them keep the compute units busy without those workgroups: 1536 keys each for tiles of 32 (28/4
     // heads, 1 sequence of 128 rows, 4096 keys 30.3 -> 28.9 us, 32768 keys 131 -> 98, but 32 rows, 4096 keys 15.9 -> 21.4, 8192 keys 21.0 -> 23.3),
     // of more than 4096 keys of 128 dims (64 dims, 28/4 heads, 2 sequences of 128 rows: 4096 keys 27.6 -> 34.4 over e4m3, 8192 keys 48.3 -> 46.9, bf16 42.8 -> 44.6).
@@ -119,8 +119,8 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     // 32.9 us whole and 33.8 in slices, 2700 keys 55.9 and 43.0; 28/4 heads, 4 ragged sequences of 130 rows and 2000 keys at most 43.8 and 35.4),
     // from 4096 of 64 dims (4 sequences of 300 rows, 2700 keys: 32/32 heads 69 and 86, 28/4 heads 69 and 79, 3500 keys 85 and 89).
     // Slices of heads of 64 have one group of wavefronts, and three workgroups a compute unit, which hold more loads on their way than one of
-    // two groups (28/4 heads, 130 rows, 100000 keys: e4m3 214 -> 167 us, bf16 155 -> 151; 32/32 heads, 80 rows, 2 sequences of 31000
-    // 152 -> 123 and 116 -> 113; the other way 28/4 heads, 17 rows of 2 sequences of 31000 31.1 -> 32.8 and 28.4 -> 28.8).
+    // two groups (28/4 heads, 130 rows, 100000 keys: e4m3 214 -> 167 us, since then 139, bf16 155 -> 151; 32/32 heads, 80 rows, 2 sequences of 31000
+    // 152 -> 123, since then 96, and 116 -> 113; the other way 28/4 heads, 17 rows of 2 sequences of 31000 31.1 -> 32.8 and 28.4 -> 28.8).
     // With fewer slices the long sequences of a ragged batch are cut all the same. The host knows the rows, and takes it that keys go with
     // them (a batch of equal rows over ragged lengths is not seen): ragged is a batch with at most 3/4 of the rows that the longest sequence's would make (28/4 heads, 8 sequences of up to 9000 keys and 80 rows, 12
     // slices: 0.6 of them 159 -> 102 us, 0.75 158 -> 130, 1 161 -> 166; 14 of up to 2100, 37 rows, 20 slices: 0.6 45 -> 41, 0.75 46 -> 48, 0.8 46 -> 49), and

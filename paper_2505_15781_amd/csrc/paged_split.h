@@ -12,12 +12,14 @@
 // sum over the sequences. So a captured call follows the lengths, and a ragged batch is cut where its keys are.
 //
 // e4m3 elements are converted on their way into LDS with their row's scale (exact in bf16 and fp32), everything behind is the same
-// for all caches. A tile is two halves of 16 keys, each on one page: no load needs a bounds check, a half without a page reads page 0
+// for all caches, but for K of an e2m1 cache: 32 dims are 16 bytes, so that the lanes that hold a key's operand of the matrix instruction load
+// just that, and convert it where it is used. It needs no LDS, which leaves room for a second workgroup on a compute unit. (The order of the dims in a
+// product is free; the queries are read in the same one.) A tile is two halves of 16 keys, each on one page: no load needs a bounds check, a half without a page reads page 0
 // and is masked. Masked scores become -infinity and masked V rows zero, whatever they hold.
 //
 // Bound by the K/V stream where there is much of it: one token of 32 sequences of up to 4096 keys, 32 heads of 128 in e4m3 (558 MB), 95 us, 5.9
 // TB/s (a cold read of that size reaches 6.0); two sequences of 131072 keys, 28/4 heads, e4m3 (271 MB), 45 us and 4.5 us
-// of paged_merge. 32 query rows of 8 sequences of 1024 keys, 32 heads, bf16 (138 MB) 25 us, 5.5 TB/s. Few keys are a chain of latencies
+// of paged_merge. In e2m1 (295 MB) 53-56 us, 5.3-5.5 TB/s (K through LDS: 74), and (143 MB) 27 us and 4.5. 32 query rows of 8 sequences of 1024 keys, 32 heads, bf16 (138 MB) 25 us, 5.5 TB/s. Few keys are a chain of latencies
 // (length, page number, first tile, join): 512 keys of 32 heads 7.6 us.
 #pragma once
 
@@ -128,7 +130,7 @@ __device__ __forceinline__ bool find_slice(const PagedCache &c, const int *row_o
 template <int BYTES> struct PieceBits { typedef u32x4 type; };
 template <> struct PieceBits<8> { typedef u32x2 type; };
 template <> struct PieceBits<4> { typedef uint32_t type; };
-// e2m1: a lane's part of a row of K is what the matrix instruction takes of it (see score_operand), so K does not go through LDS.
+// Whether K goes from memory to the matrix instruction's operands.
 template <typename C> constexpr bool kDirectK = kE2M1<C>;
 template <typename T, typename C, int DH, int NQ> struct SplitSmem {
     static constexpr int K_STRIDE = DH * (int)sizeof(T) + 16;                               // bytes per row; the rest spreads

@@ -6,7 +6,7 @@
 // j - 1 and the exponentials of half tile j. What differs is where a tile comes from. It is four groups of 16 keys, each on one page;
 // their places are found once per tile from page numbers that a lane each holds for the next 1024 keys.
 //   bf16: global memory to LDS without registers; keys that are not there (behind the end, no page) come from a row of zeros.
-//   e4m3: through registers, a tile ahead, converted with their row's scale (exact) on the way into LDS. K and V are converted
+//   e4m3, e2m1: through registers, a tile ahead, converted with their scale (exact) on the way into LDS. K and V are converted
 //         once per 128 query rows: 32 of a wavefront's vector instructions per tile, next to some 200 of the softmax.
 //
 // 4 sequences of 1536 rows and keys, 32 heads of 128 (155 GFLOP): e4m3 178-188 us by card, 820-870 TFLOP/s, bf16 191-193. A large product would take
@@ -17,6 +17,10 @@
 // 64 dims 125 -> 150), two groups of wavefronts (187-209), blocks of 256 query rows with eight
 // wavefronts behind one barrier, which halves the fills (201 against 183: two workgroups to a compute unit drift apart and fill each other's
 // gaps), LDS reads 9 and 12 ahead instead of 6 (no change).
+// Over e2m1 171-188 us by card. Not kept there: the conversion between the products of a stretch, from two sets of registers (171 -> 179 us), or of K
+// where it is used, each wavefront for itself and without LDS (172 -> 177); keys that are not there made zero when they are fetched (178 -> 181). Two
+// wavefronts of a SIMD take 1.25 us for a tile each, one alone 1.5. Products of K in 4 bits with the queries in two parts of 8 (the same matrix time, no
+// conversion) add up to less than fp32: up to 2^-12 of the sum of magnitudes is lost.
 #pragma once
 
 typedef __attribute__((address_space(3))) void *lds_ptr_t;
@@ -327,6 +331,7 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
                        bf16x8 (&pn)[2]) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) sn[v] = 0.f;
+        // heads of 64, whose exponentials weigh as much as the products: the wavefront in here goes first (e2m1, 4 sequences of 1536 102 -> 98 us; 128 dims: no change)
         if constexpr (DH == 64) __builtin_amdgcn_s_setprio(1);
         f32x8 p[2];
         constexpr int MT = DH / 32, N = DH / 16, PER = 16 / N;        // products of the scores, and of the output; exponentials next to each two

@@ -5,6 +5,10 @@
 // works through its heads, so their cosines are computed once for all of them. Angles of far positions need more than 32 bits (2^20
 // positions at one radian each: an fp32 product is off by 2^-4): position times frequency, in quarter turns, and what is left of it in the
 // quarter are formed in 64 bits, sine and cosine of that from their Taylor series in 32.
+//
+// 6144 rows of 64 heads of 128 in bf16 (201 MB) 33.6 us, 6.0 TB/s (a large copy 4.46); 4099 rows of 32 heads in fp32, neighbouring pairs of 64 dims, into other memory (134 MB)
+// 20.2 us. With stores that stay in the caches 39.3 and 27.0: so many rows are more than the caches hold until somebody reads them. Neighbouring pairs in one piece of
+// 32 bytes a lane, every other 16 to a load, took 30.1 instead of 27.0. 64 rows 3.4 us; the call is 5.5 us of the host.
 #include <math.h>
 
 #include <type_traits>
@@ -121,6 +125,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs<T> a) {
         }
         if (turn_lo) narrow(m, x[i]);
         if (turn_hi) narrow(n, y[i]);
+        // many rows: with the non-temporal hint
         auto put = [&](typename B::type v, T *to) {
             if constexpr (H > 1) __builtin_nontemporal_store(v, reinterpret_cast<typename B::at *>(to));
             else *reinterpret_cast<typename B::at *>(to) = v;
@@ -133,7 +138,9 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs<T> a) {
 template <typename T, int V> int launch(RopeArgs<T> &a, bool pairs, hipStream_t s) {
     a.lanes = __builtin_ctz((unsigned)(a.head_dim / (2 * V)));
     const int at_once = 64 >> a.lanes;
-    const bool many = (int64_t)a.rows * ((a.heads + 4 * at_once - 1) / (4 * at_once)) >= 2048;
+    // four heads of a lane at once where that leaves 512 wavefronts (32 and 32 heads of 128, one head and four: 128 rows 3.6 and 4.2 us, 256 rows 5.0 and 4.4, 2048 rows 15.3
+    // and 12.5; 28 and 4: 256 rows 3.6 and 4.2, 512 rows 4.9 and 4.4; 8 and 2 of 64 in fp32: 512 rows 3.0 and 3.2, 1024 rows 3.5 and 3.4)
+    const bool many = (int64_t)a.rows * ((a.heads + 4 * at_once - 1) / (4 * at_once)) >= 512;
     const int64_t parts = (a.heads + (many ? 4 : 1) * at_once - 1) / ((many ? 4 : 1) * at_once), groups = (parts * a.rows + 3) / 4;
     if (groups >= 1 << 23) { dkv_set_error("%d rows of %d heads are too many for one call", a.rows, a.heads); return DKV_E_UNSUPPORTED; }
     a.parts = Divisor((int)parts);
