@@ -455,7 +455,10 @@ class Rope:
         self.desc = RopeDesc()
         _check(lib.dkv_rope_init(C.byref(self.desc), head_dim, head_dim if rot_dim is None else rot_dim, bool(interleaved), theta,
                                  self.SCALINGS.index(scaling), factor, original, slow, fast))
-        self.address = C.addressof(self.desc)
+
+    @property
+    def address(self):        # asked each time: a copy of this object has another
+        return C.addressof(self.desc)
 
     @property
     def freq(self):

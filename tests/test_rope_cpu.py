@@ -1,6 +1,8 @@
 """Rotary positions without a GPU: frequencies and refusals."""
+import copy
 import ctypes as C
 import math
+import pickle
 
 import numpy as np
 import pytest
@@ -61,6 +63,14 @@ def test_what_the_frequencies_refuse():
         P.Rope(64, scaling="cubic")
     with pytest.raises(P.DkvError):
         P.Rope(48)
+
+
+def test_a_copy_has_frequencies_of_its_own():
+    r = P.Rope(64, 32, interleaved=True)
+    for other in (copy.copy(r), copy.deepcopy(r), pickle.loads(pickle.dumps(r))):
+        assert other.address == C.addressof(other.desc) and other.freq == r.freq and other.scale == r.scale
+    other.freq = [0.5] * 16
+    assert r.freq[0] == 1.0 and other.freq[0] == B.RopeDesc.from_address(other.address).freq[0] == 0.5
 
 
 def call(rope=None, q=16, qs=512, qo=16, qos=512, nq=4, k=16, ks=256, ko=16, kos=256, nk=2, pos=16, off=16, batch=3, rows=5, dtype=0, inverse=0):
