@@ -283,8 +283,8 @@ int dkv_concat_reorder(const void *k_cached, const void *v_cached, const void *k
  *                    ([head_dim / 2]), the lower dim in the lower 4 bits: a sign bit and 0, 0.5, 1, 1.5, 2, 3, 4 or 6
  *   k_scale, v_scale (dev) [n_pages][n_kv_heads][page_size], DKV_E4M3 only: scale of a row as the biased exponent of a
  *                    power of two (E8M0): element = code * 2^(scale - 127), of 17 to 247, which are those that a store writes; what
- *                    is read from a row with another one is not defined. DKV_E2M1: [n_pages][n_kv_heads][page_size][head_dim / 32], one for each 32
-                    dims, of 17 to 253, or 255, which makes the 32 dims NaN
+ *                    is read from a row with another one is not defined. DKV_E2M1: [n_pages][n_kv_heads][page_size][head_dim / 32], one for
+ *                    each 32 dims, of 17 to 253, or 255, which makes the 32 dims NaN
  *   page_table (dev) [batch][max_pages]
  *   seq_len (dev) [batch] positions of each sequence (attention only; taken as 0 below 0, as max_pages * page_size above)
  * page_size: a power of two, 16 to 65536; max_pages * page_size at most 2^30, n_pages * n_kv_heads * page_size at most 2^32, n_kv_heads * head_dim

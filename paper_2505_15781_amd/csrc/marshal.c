@@ -219,7 +219,7 @@ static int look_whole(PyObject *t, const char *name, int dtype, int n, const int
     if (i->n_dims != (n < 0 ? -n : n)) return refuse(name, "wrong number of dimensions");
     for (int k = 0; k < n; ++k)
         if (i->dims[k] != dims[k]) return refuse(name, "sizes do not fit those of the cache and the rows");
-    return i->device == device ? 0 : refuse(name, "not on the device of the cache");
+    return i->device == device ? 0 : refuse(name, "not on the device of the other tensors");
 }
 
 /* (k_pages, v_pages, page_table, seq_len, k_scale, v_scale) */
@@ -262,8 +262,8 @@ static int look_cache(PyObject *o, dkv_paged_cache *c, int *device) {
 static int look_rows(PyObject *t, const char *name, int32_t heads, int32_t head_dim, int device, tensor_info *i, int64_t *stride) {
     if (look(t, i)) return -1;
     if (i->n_dims != 3 || (heads >= 0 && i->dims[1] != heads) || i->dims[2] != head_dim || (i->dtype != T_BF16 && i->dtype != T_FP32))
-        return refuse(name, "[rows, heads, head_dim] of bfloat16 or float32 with the cache's head_dim is expected");
-    if (i->device != device) return refuse(name, "not on the device of the cache");
+        return refuse(name, "[rows, heads, head_dim] of bfloat16 or float32 with the head_dim at hand is expected");
+    if (i->device != device) return refuse(name, "not on the device of the other tensors");
     *stride = (int64_t)i->dims[1] * head_dim;
     if (i->whole) return 0;
     PyObject *s = PyObject_CallMethodObjArgs(t, s_stride, NULL);
@@ -363,7 +363,7 @@ static PyObject *py_paged_attn_workspace_bytes(PyObject *self, PyObject *const *
 static int look_workspace(PyObject *t, int device, tensor_info *ws, size_t *bytes) {
     if (t == Py_None) return 0;
     if (look_memory(t, ws)) return -1;
-    if (!ws->whole || ws->device != device) return refuse("workspace", "a contiguous tensor on the device of the cache is expected");
+    if (!ws->whole || ws->device != device) return refuse("workspace", "a contiguous tensor on the device of the others is expected");
     PyObject *b = PyObject_GetAttr(t, s_nbytes);
     if (!b) return -1;
     *bytes = PyLong_AsSize_t(b);
