@@ -57,7 +57,7 @@ class Both:
         assert np.array_equal(self.t.free_pages.cpu().numpy(), np.array(self.ring))
 
 
-# batch, pages of a table, pages, page size: one launch, and (many sequences, or rows) two
+# batch, pages of a table, pages, page size: one launch, and (many sequences, or rows) three
 SIZES = [(1, 1, 1, 16), (1, 700, 600, 16), (3, 9, 20, 16), (64, 40, 1500, 32), (65, 7, 200, 256), (1000, 3, 2000, 16), (1024, 5, 3000, 64), (1025, 4, 3000, 16),
          (2500, 6, 9000, 16), (130, 300, 30000, 16)]
 
@@ -125,25 +125,26 @@ def test_sums_beyond_32_bits_do_not_fit():
     assert torch.equal(table[:2].flatten(), torch.arange(n, dtype=torch.int32, device="cuda")) and (table[2:] == -1).all()
 
 
-def test_captured_calls_follow_the_lengths():
+@pytest.mark.parametrize("batch,rows", [(20, 700), (20, 9000), (1030, 40000)])
+def test_captured_calls_follow_the_lengths(batch, rows):
     """Two graphs that share tables and workspace, replayed in turn, with eager calls between them."""
-    b = Both(20, 30, 400, 16, seed=4)
-    grow, leave = dev(np.zeros(20)), dev(np.zeros(20))
-    off, pos, slots = dev(np.zeros(21)), dev(np.full(700, -3)), torch.full((700,), -3, dtype=torch.int64, device="cuda")
-    b.resize(np.full(20, 7))
+    b = Both(batch, 30, 20 * batch, 16, seed=4)
+    grow, leave = dev(np.zeros(batch)), dev(np.zeros(batch))
+    off, pos, slots = dev(np.zeros(batch + 1)), dev(np.full(rows, -3)), torch.full((rows,), -3, dtype=torch.int64, device="cuda")
+    b.resize(np.full(batch, 7))
     first, second = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
     with torch.cuda.graph(first):
         P.paged_resize(b.t, grow, b.ws, off, pos, slots)
     with torch.cuda.graph(second):
         P.paged_resize(b.t, leave, b.ws)
     for i in range(5):
-        want = np.array(b.len) + b.g.integers(0, 33, 20)
+        want = np.array(b.len) + b.g.integers(0, 33, batch)
         grow.copy_(dev(want))
         first.replay()
-        o, p, s = O.resize(b.table, b.len, b.ring, b.at, 16, want.tolist(), 700)
+        o, p, s = O.resize(b.table, b.len, b.ring, b.at, 16, want.tolist(), rows)
         b.same()
         assert off.tolist() == o and pos[:o[-1]].tolist() == p and slots[:o[-1]].tolist() == s
-        want = np.where(b.g.random(20) < 0.3, b.g.integers(0, 5, 20), -1)
+        want = np.where(b.g.random(batch) < 0.3, b.g.integers(0, 5, batch), -1)
         leave.copy_(dev(want))
         second.replay()
         O.resize(b.table, b.len, b.ring, b.at, 16, want.tolist())
@@ -151,9 +152,10 @@ def test_captured_calls_follow_the_lengths():
         b.resize(np.array(b.len) + 1)
 
 
-def test_two_tables_on_two_streams():
-    both = [Both(300, 40, 9000, 16, seed=i) for i in range(2)]
-    wants = [[b.g.integers(0, 640, 300) for _ in range(8)] for b in both]
+@pytest.mark.parametrize("batch", [300, 1300])
+def test_two_tables_on_two_streams(batch):
+    both = [Both(batch, 40, 30 * batch, 16, seed=i) for i in range(2)]
+    wants = [[b.g.integers(0, 640, batch) for _ in range(8)] for b in both]
     streams = [torch.cuda.Stream() for _ in both]
     dev_wants = [[dev(w) for w in ws] for ws in wants]
     torch.cuda.synchronize()

@@ -73,6 +73,26 @@ def test_rows_behind_the_last_sequence_and_odd_addresses(act):
         assert torch.equal(x[n - 2:], was[n - 2:]) and torch.equal(room[:3], before[:3]) and torch.equal(room[3 + x.numel():], before[3 + x.numel():])
 
 
+@pytest.mark.parametrize("n,rot", [(3, 128), (520, 96)])
+def test_rows_that_are_far_apart(n, rot):
+    """Rows behind the first four gigabytes, in place and into others."""
+    g = np.random.default_rng(5)
+    step = (5 << 30) // (2 * (n - 1)) // 128 * 128
+    x = rows(g, (n, 12, 128), "bf16")
+    room = torch.empty((n - 1) * step + 12 * 128, dtype=torch.bfloat16, device="cuda")
+    far = torch.as_strided(room, (n, 12, 128), (step, 128, 1))
+    far.copy_(x)
+    pos, r = g.integers(0, 1 << 17, n), P.Rope(128, rot)
+    out = torch.empty_like(x)
+    P.rope(r, far[:, :9], far[:, 9:], dev(pos), q_out=out[:, :9], k_out=out[:, 9:])
+    check(out, x, pos, r, False)
+    P.rope(r, far[:, :9], far[:, 9:], dev(pos))
+    assert torch.equal(far, out)
+    far.fill_(0.0)
+    P.rope(r, x[:, :9], x[:, 9:], dev(pos), q_out=far[:, :9], k_out=far[:, 9:])
+    assert torch.equal(far, out)
+
+
 def test_every_angle_of_a_wide_range_of_positions():
     """Positions of all magnitudes up to the largest, both signs, frequencies from radians to almost none: the pair (1, 0) becomes (cos, sin)."""
     pos = np.unique(np.concatenate([np.arange(-300, 300), (2.0 ** np.linspace(0, 31, 3000)).astype(np.int64) - 1, -(2.0 ** np.linspace(0, 31, 500)).astype(np.int64)]))
