@@ -9,8 +9,8 @@
 // sequence (by the one workgroup, a sequence after the other to a wavefront, 512 sequences of 256 pages took 28 us instead of 3 + 3), or in the one-launch form by
 // going through all such entries in a row, 4096 at a time.
 //
-// One launch: 64 sequences, 1000 rows, 4 of them leave 5.8-7.2 us in a trace, the least 4.1: the chain of lengths, barriers, ring or table, stores. Three: 512 sequences, 1.9 million
-// rows 18 us (3 + 3 + 11.5; 23 MB written at 2 TB/s in the last).
+// One launch: 64 sequences, 1000 rows, 4 of them leave 5.8-6.5 us in a trace, the least 4.1: the chain of lengths, barriers, ring or table, stores. Three: 512 sequences, 1.9 million
+// rows 16 us (3 + 3 + 9.7; 23 MB written at 2.4 TB/s in the last). There each row of a lane that looked its sequence up in memory by itself, with the row before stored between, took 12.4 instead of 9.7.
 #include <type_traits>
 
 #include "paged.h"
@@ -185,7 +185,8 @@ template <bool COUNTED> __device__ __forceinline__ void plan(const Tables &t, co
     }
 }
 
-// The three parts of the work are independent of each other; each for wavefront `wave` of `waves`.
+// The parts of the work are independent of each other; each for wavefront `wave` of `waves`.
+// Without lists of the new positions.
 __device__ __forceinline__ void take_pages(const Tables &t, const Work &w, int wave, int waves) {
     const int lane = threadIdx.x & 63;
     const Totals all = *w.totals;
@@ -199,24 +200,54 @@ __device__ __forceinline__ void take_pages(const Tables &t, const Work &w, int w
         }
     }
 }
-// Four rows to a lane.
+// Four rows to a lane (eight: 1.9 million rows 15.2 us instead of 13.6). The first position of a new page is one of them: it writes the table's entry.
 __device__ __forceinline__ void list_rows(const Tables &t, const Lists &l, const Work &w, int wave, int waves) {
+    constexpr int N = 4;
     const int lane = threadIdx.x & 63;
     const Totals all = *w.totals;
-    for (int x = wave * 256; x < all.rows; x += waves * 256) {
-        int b0, b1;
-        find(w.row, t.batch, x, min(x + 255, all.rows - 1), b0, b1);
+    for (int x = wave * 64 * N; x < all.rows; x += waves * 64 * N) {
+        int b0, b1, b[N], old[N], row[N], take[N], p[N], id[N], entry[N];      // entry: of the table, -1 where it is there already
+        find(w.row, t.batch, x, min(x + 64 * N - 1, all.rows - 1), b0, b1);
+        if (b1 - b0 < 64) {                                // a lane reads what there is of one sequence, for all rows of the wavefront
+            const int mine = min(b0 + lane, b1), olds = w.before[mine], rows = w.row[mine], takes = w.take[mine];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+            for (int u = 0; u < N; ++u) b[u] = 0;
+            for (int step = 32; step > 0; step >>= 1) {
+                if (step > b1 - b0) continue;              // uniform
+#pragma unroll
+                for (int u = 0; u < N; ++u) {
+                    const int i = b[u] + step, first = __builtin_amdgcn_ds_bpermute(min(i, b1 - b0) << 2, rows);       // by all lanes
+                    if (i <= b1 - b0 && first <= x + 64 * u + lane) b[u] = i;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                old[u] = __builtin_amdgcn_ds_bpermute(b[u] << 2, olds);
+                row[u] = __builtin_amdgcn_ds_bpermute(b[u] << 2, rows);
+                take[u] = __builtin_amdgcn_ds_bpermute(b[u] << 2, takes);
+                b[u] += b0;
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                b[u] = find_between(w.row, b0, b1, min(x + 64 * u + lane, all.rows - 1));
+                old[u] = w.before[b[u]], row[u] = w.row[b[u]], take[u] = w.take[b[u]];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            p[u] = old[u] + min(x + 64 * u + lane, all.rows - 1) - row[u];
+            const int j = p[u] >> t.shift, have = t.pages(old[u]), at = b[u] * t.max_pages + j;
+            id[u] = *(j < have ? t.table + at : t.ring + t.place(all.head + take[u] + j - have));
+            entry[u] = j >= have && !(p[u] & ((1 << t.shift) - 1)) ? at : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
             const int r = x + 64 * u + lane;
             if (r >= all.rows) continue;
-            const int b = find_between(w.row, b0, b1, r), old = w.before[b], p = old + r - w.row[b];
-            if (l.positions) l.positions[r] = p;
-            if (l.slots) {
-                const int j = p >> t.shift, have = t.pages(old);
-                const int id = j < have ? t.table[(size_t)b * t.max_pages + j] : t.ring[t.place(all.head + w.take[b] + j - have)];
-                l.slots[r] = t.is_page(id) ? ((int64_t)id << t.shift) + (p & ((1 << t.shift) - 1)) : -1;
-            }
+            if (entry[u] >= 0) t.table[entry[u]] = id[u];
+            if (l.positions) l.positions[r] = p[u];
+            if (l.slots) l.slots[r] = t.is_page(id[u]) ? ((int64_t)id[u] << t.shift) + (p[u] & ((1 << t.shift) - 1)) : -1;
         }
     }
 }
@@ -296,11 +327,11 @@ __global__ __launch_bounds__(256) void paged_resize_count(Tables t, const int *l
     if ((threadIdx.x & 63) == 0) w.give[b] = n;
 }
 __global__ __launch_bounds__(kThreads) void paged_resize_plan(Tables t, const int *lengths, Lists l, Work w) { plan<true>(t, lengths, l, w); }
-__global__ __launch_bounds__(256) void paged_resize_fill(Tables t, Lists l, Work w) {
-    const int wave = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = (int)gridDim.x * 4;
-    if (blockIdx.y == 0) list_rows(t, l, w, wave, waves);
-    else if (blockIdx.y == 1) take_pages(t, w, wave, waves);
-    else give_pages(t, w, wave, waves);
+__global__ __launch_bounds__(256) void paged_resize_fill(Tables t, Lists l, Work w, int takers) {
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), block = (int)blockIdx.x;
+    if (block >= takers) give_pages(t, w, (block - takers) * 4 + wave, ((int)gridDim.x - takers) * 4);
+    else if (l.row_off) list_rows(t, l, w, block * 4 + wave, takers * 4);
+    else take_pages(t, w, block * 4 + wave, takers * 4);
 }
 // Up to kThreads sequences, all in one workgroup.
 __global__ __launch_bounds__(kThreads) void paged_resize_small(Tables t, const int *lengths, Lists l) {
@@ -310,8 +341,8 @@ __global__ __launch_bounds__(kThreads) void paged_resize_small(Tables t, const i
     plan<false>(t, lengths, l, w);
     __syncthreads();
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    take_pages(t, w, wave, kWaves);
-    list_rows(t, l, w, wave, kWaves);
+    if (l.row_off) list_rows(t, l, w, wave, kWaves);
+    else take_pages(t, w, wave, kWaves);
     give_entries(t, w);
 }
 
@@ -349,7 +380,7 @@ extern "C" int dkv_paged_resize(const dkv_paged_tables *tables, const int32_t *l
     int *arrays = reinterpret_cast<int *>(static_cast<char *>(workspace) + kTotalsBytes);
     const Work w = {static_cast<Totals *>(workspace), arrays, arrays + c.batch, arrays + 2 * (size_t)c.batch, arrays + 3 * (size_t)c.batch, arrays + 4 * (size_t)c.batch};
     hipStream_t s = static_cast<hipStream_t>(stream);
-    // rows in one launch and in three, us in a graph: 4096 4.1 and -, 8192 5.9-8.7 and 7-10, 16384 8.2-9.4 and 7.2-8.1, 65536 28.7 and 8.3
+    // rows in one launch and in three, us in a graph: 4096 4.4 and -, 8192 6.3-8.2 and 7-10, 16384 8.8-14.5 and 7.1-9.7, 65536 31-39 and 8.1-9.3
     if (c.batch <= kThreads && (!row_off || rows <= 8192)) {
         hipLaunchKernelGGL(paged_resize_small, dim3(1), dim3(kThreads), 0, s, t, lengths, l);
         DKV_LAUNCH_CHECK();
@@ -359,11 +390,11 @@ extern "C" int dkv_paged_resize(const dkv_paged_tables *tables, const int32_t *l
     DKV_LAUNCH_CHECK();
     hipLaunchKernelGGL(paged_resize_plan, dim3(1), dim3(kThreads), 0, s, t, lengths, l, w);
     DKV_LAUNCH_CHECK();
-    // a wavefront for 256 rows, 64 pages or a sequence at a time, up to what runs at once
+    // a wavefront for 256 rows or 64 pages that are taken, and for a sequence that gives some, up to what runs at once
     const int64_t pages = (int64_t)c.batch * c.max_pages < c.n_pages ? (int64_t)c.batch * c.max_pages : c.n_pages;
-    int64_t waves = row_off ? (rows + 255) / 256 : (pages + 63) / 64;
-    waves = waves > c.batch ? waves : c.batch;
-    hipLaunchKernelGGL(paged_resize_fill, dim3((unsigned)(waves < 8192 ? (waves + 3) / 4 : 2048), 3), dim3(256), 0, s, t, l, w);
+    auto blocks = [](int64_t waves) { return (int)(waves < 8192 ? (waves + 3) / 4 : 2048); };
+    const int takers = blocks(row_off ? ((int64_t)rows + 255) / 256 : (pages + 63) / 64);
+    hipLaunchKernelGGL(paged_resize_fill, dim3((unsigned)(takers + blocks(c.batch))), dim3(256), 0, s, t, l, w, takers);
     DKV_LAUNCH_CHECK();
     return DKV_OK;
 }
