@@ -100,6 +100,16 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     p.spread = best_spread(p.q_groups, heads, 1);
     p.least = kLeast;
     int want = slices_at_once(p.q_groups, heads, p.spread, 1);
+    // e2m1, few rows: two workgroups fit a unit. Slices for both where one each would leave the sequences of a long table whole, and make two of each at least (us
+    // whole and cut, one token, 8 sequences, 32 heads: up to 16384 keys 80 and 62, 32 of up to 8192, 32/8 heads, 42 and 33.7, 8192 keys each 50 and 52; up to 4096 keys 24 and 21.6, but 2048 keys each
+    // 15.7 and 18.6).
+    if (dtype == DKV_BF16 && four_bits(cache_dtype, head_dim) && p.nq == 1 && want <= c.batch && keys >= 8192) {
+        const int spread = best_spread(p.q_groups, heads, 2), more = slices_at_once(p.q_groups, heads, spread, 2);
+        if (more >= 2 * c.batch) {
+            want = more;
+            p.spread = spread;
+        }
+    }
     p.split = key_tiles > whole_tiles(dtype, head_dim) && want > c.batch;
     // Blocks of 128 query rows (paged_wide.h) where tiles of 32 would make more than one round of workgroups (128 dims; 28/4 heads, 1024 keys: 1
     // sequence of 300 rows, 264 workgroups, 29 -> 26 us, 4 of 128 rows, 448, 30 -> 27, but 4 of 64 rows, 224, 17 -> 26) or more than three (64
@@ -191,7 +201,7 @@ size_t most_partial_bytes(const PagedCache &c, int n_q_heads, int rows, int max_
         }
         return meta_bytes(c) + (size_t)n * (nq * 16) * (head_dim + 4) * sizeof(float);
     };
-    const size_t split = bytes(split_tiles(dtype, tiles), kLeast, 1);
+    const size_t split = bytes(split_tiles(dtype, tiles), kLeast, four_bits(cache_dtype, head_dim) ? 2 : 1);
     const int64_t groups = row_groups(c, rows, max_rows, G, 32), keys = (int64_t)key_tiles * PKT;
     if (!rows_for_blocks(dtype, head_dim, max_rows * G) || !keys_to_cut(head_dim, keys) ||
         !(blocks_for_rounds(cache_dtype, head_dim, groups) || blocks_for_keys(cache_dtype, head_dim, groups, keys)))
@@ -199,10 +209,18 @@ size_t most_partial_bytes(const PagedCache &c, int n_q_heads, int rows, int max_
     const size_t blocks = bytes(8, kLeastWide, block_workgroups_per_cu(head_dim));
     return blocks > split ? blocks : split;
 }
-SlicePlan slice_plan(const Plan &p) { return SlicePlan{p.least, Divisor(p.want), p.split}; }
+SlicePlan slice_plan(const Plan &p, bool longest_first) { return SlicePlan{p.least, Divisor(p.want), p.split, longest_first}; }
 GroupMap group_map(const Plan &p) { return GroupMap{Divisor(ceil_div(p.q_groups, 1 << p.spread)), p.spread, p.q_groups * p.nq * 16}; }
 int64_t split_grid(const Plan &p, const PagedCache &c) {
     return (((int64_t)p.cap * c.n_kv_heads << p.spread) + 7) / 8 * 8 * ceil_div(p.q_groups, 1 << p.spread);
+}
+// e2m1: whole sequences with the longest first where they make more than one round of a workgroup for each compute unit and up to four, over tables of 1024
+// positions and more. A workgroup then knows its sequence one look-up later (one token, us in the order of the batch and so: 32 ragged sequences of up to 4096 keys, 32 heads
+// 59 and 53, rows in fp32 237 and 182, 12 of them 30.4 and 26.6, heads of 64 38 and 32, 16 with 8 rows 33.6 and 31.3; 32 of 2048 keys each 49.7 and 49.9, 12 22.5 and 22.9; 64 of 2048 at most 56.8 and 55; 100 of 1000 at most,
+// 28/4 heads, 13.1 and 14; shorter: 300 of 500 at most, 8/8 heads 28.9 and 30, of 250 each 27.3 and 29.1). Over e4m3 and bf16 caches, one workgroup a unit, ragged batches gain as much,
+// but batches of one length lose up to 3 %: left in the order of the batch.
+template <typename C> bool longest_first(const Plan &p, const PagedCache &c) {
+    return kE2M1<C> && !p.split && (int64_t)c.max_pages << c.page_shift >= 1024 && split_grid(p, c) > kWorkgroups && split_grid(p, c) <= 4 * kWorkgroups;
 }
 
 template <typename T, int DH>
@@ -224,7 +242,7 @@ int launch_split(const PagedCache &c, const Plan &p, const void *q, int64_t q_st
         static std::atomic<uint64_t> devices{0};                                                                                 \
         const int rc = allow_lds(reinterpret_cast<const void *>(&paged_attn_split<T, C, DH, NQ, NW, ONCE>), smem, devices);      \
         if (rc) return rc;                                                                                                       \
-        hipLaunchKernelGGL((paged_attn_split<T, C, DH, NQ, NW, ONCE>), dim3((unsigned)split_grid(p, c)), dim3(64 * NW), smem, s, c, slice_plan(p), \
+        hipLaunchKernelGGL((paged_attn_split<T, C, DH, NQ, NW, ONCE>), dim3((unsigned)split_grid(p, c)), dim3(64 * NW), smem, s, c, slice_plan(p, longest_first<C>(p, c)), \
                            (const T *)q, q_stride, row_off, (T *)out, (int2 *)part, (float *)((char *)part + meta_bytes(c)), rows, max_rows, \
                            group_map(p), Divisor(c.n_kv_heads), Divisor(Hq / c.n_kv_heads), scale_log2e);                \
     } while (0)
@@ -242,7 +260,7 @@ int launch_wide(const PagedCache &c, const Plan &p, const void *q, int64_t q_str
     const int rc = allow_lds(reinterpret_cast<const void *>(&paged_attn_wide<C, DH, KS>), KS * kWideLds<DH>, devices);
     if (rc) return rc;
     hipLaunchKernelGGL((paged_attn_wide<C, DH, KS>), dim3((unsigned)(p.split ? split_grid(p, c) : p.blocks)), dim3(256 * KS), KS * kWideLds<DH>, s, c,
-                       (const bf16_t *)q, q_stride, row_off, (bf16_t *)out, rows, (int2 *)part, (float *)((char *)part + meta_bytes(c)), slice_plan(p),
+                       (const bf16_t *)q, q_stride, row_off, (bf16_t *)out, rows, (int2 *)part, (float *)((char *)part + meta_bytes(c)), slice_plan(p, false),
                        max_rows, group_map(p), Divisor(c.n_kv_heads), Divisor(Hq / c.n_kv_heads), kWorkgroups / c.n_kv_heads,
                        1.4426950408889634f / sqrtf((float)DH));
     DKV_LAUNCH_CHECK();

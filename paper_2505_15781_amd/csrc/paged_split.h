@@ -19,7 +19,7 @@
 //
 // Bound by the K/V stream where there is much of it: one token of 32 sequences of up to 4096 keys, 32 heads of 128 in e4m3 (558 MB), 95 us, 5.9
 // TB/s (a cold read of that size reaches 6.0); two sequences of 131072 keys, 28/4 heads, e4m3 (271 MB), 45 us and 4.5 us
-// of paged_merge. In e2m1 (295 MB) 53-56 us, 5.3-5.5 TB/s (K through LDS: 74), and (143 MB) 27 us and 4.5. 32 query rows of 8 sequences of 1024 keys, 32 heads, bf16 (138 MB) 25 us, 5.5 TB/s. Few keys are a chain of latencies
+// of paged_merge. In e2m1 (295 MB) 50-53 us, 5.6-5.9 TB/s (K through LDS: 74), and (143 MB) 27 us and 4.5. 32 query rows of 8 sequences of 1024 keys, 32 heads, bf16 (138 MB) 25 us, 5.5 TB/s. Few keys are a chain of latencies
 // (length, page number, first tile, join): 512 keys of 32 heads 7.6 us.
 #pragma once
 
@@ -31,7 +31,7 @@ constexpr int PKT = 32;                // keys per tile
 struct SlicePlan {
     int least;
     Divisor want;
-    bool split;
+    bool split, longest_first;         // longest_first: whole sequences in the order of `longest`
 };
 // Workgroup id -> (slice, K/V head) and query group. The groups of one (slice, K/V head) read the same keys and are on one XCD (id mod 8),
 // or in 2^shift parts on as many, where one XCD would get more of them than run at once.
@@ -92,15 +92,33 @@ __device__ __forceinline__ int slice_length(const PagedCache &c, const int *row_
         slice = max(plan.least, ceil_div(total, plan.want.d - (c.batch * quarters >> 2)));
     return slice;
 }
+// Whole wavefronts: the sequence that comes `at`-th when each 64 of them are put in the order of their lengths, in sixteen steps of the power of two that holds the table, the longest
+// first: of the sequences that are left, one bit of that number after the other says whether it is with the longer ones or how many of these are before it.
+__device__ __forceinline__ int longest(const PagedCache &c, int at) {
+    const int lane = threadIdx.x & 63, from = at & ~63, keys = from + lane < c.batch ? c.keys(from + lane) : 0;
+    const int step = min(15, keys >> max(0, 28 - __builtin_clz(c.capacity() - 1)));
+    unsigned long long left = __builtin_amdgcn_ballot_w64(from + lane < c.batch);
+    int before = at & 63;
+#pragma unroll
+    for (int bit = 3; bit >= 0; --bit) {
+        const unsigned long long longer = left & __builtin_amdgcn_ballot_w64(step >> bit & 1);
+        const int n = __popcll(longer);
+        left = before < n ? longer : left & ~longer;
+        before -= before < n ? 0 : n;
+    }
+    const int i = __builtin_amdgcn_mbcnt_hi((uint32_t)(left >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)left, 0));
+    return from + __builtin_ctzll(left & __builtin_amdgcn_ballot_w64(i == before));
+}
 // Whole wavefronts. Finds slice `at` of the batch; false if there are fewer.
 __device__ __forceinline__ bool find_slice(const PagedCache &c, const int *row_off, const SlicePlan &plan, int at, Slices &s) {
     const int lane = threadIdx.x & 63;
     if (!plan.split) {
         if (at >= c.batch) return false;
-        s.b = s.first = at;
+        s.first = at;
+        s.b = plan.longest_first ? longest(c, at) : at;
         s.n = 1;
-        rows_of_sequence(row_off, at, s.r0, s.rows);
-        s.keys = c.keys(at);
+        rows_of_sequence(row_off, s.b, s.r0, s.rows);
+        s.keys = c.keys(s.b);
         return true;
     }
     int slice = 0, before = 0;
@@ -227,7 +245,8 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
     int entry = -1, entry_ahead = -1;
     auto first_key = [&](int t_begin, int j0) { return (t_begin + wave + NW * (j0 + (lane >> 1))) * PKT + 16 * (lane & 1); };
     auto load_entry = [&](int b, int key) { return key < c.capacity() ? c.table[(size_t)b * c.max_pages + (key >> c.page_shift)] : -1; };
-    if (!plan.split && at < c.batch) entry = load_entry(at, first_key(0, 0));
+    const bool known = !plan.split && !(kE2M1<C> && plan.longest_first);      // the sequence
+    if (known && at < c.batch) entry = load_entry(at, first_key(0, 0));
     Slices sl;
     if (!find_slice(c, row_off, plan, at, sl)) return;
     // the same in every lane, which the compiler does not see behind the two ways to a slice
@@ -321,7 +340,7 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_attn_split(PagedCache c
         for (int i = 0; i < DH / 16; ++i) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     int t = t_begin + wave, j = 0;
-    if (plan.split) entry = load_entry(b, first_key(t_begin, 0));
+    if (!known) entry = load_entry(b, first_key(t_begin, 0));
     entry_ahead = load_entry(b, first_key(t_begin, 32));
     // Query operands. bf16: dims 32 ks + 8 g + [0, 8); fp32: dims 16 ks + 4 g + [0, 4), one of the four for each product. The order of the dims is
     // free as long as K has the same: where K is taken from registers, g DH / 4 + 8 ks + [0, 8) and g DH / 4 + 4 ks + [0, 4)

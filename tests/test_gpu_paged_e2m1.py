@@ -13,6 +13,7 @@ import test_gpu_paged as paged
 import test_gpu_paged_calls as calls
 from oracle import paged as O
 from paged_shapes import BLOCKS, E2M1_CALLS, plan_of
+from plans import paged_plan
 from test_gpu_paged import ATTN, TORCH, Cache, check_attn, dev, rows, workspace
 
 pytestmark = pytest.mark.gpu
@@ -176,6 +177,35 @@ def test_attention(act, case, holes):
     if R + 2 > len(counts) * max(counts):
         q = q[:R]
     check_attn(c, q, counts, most=max(counts) if case % 2 else max(counts) + 3)
+
+
+@pytest.mark.parametrize("act", ["bf16", "fp32"])
+@pytest.mark.parametrize("batch,heads,group,dh,longest,most", [(70, 4, 2, 32, 1100, 1), (20, 16, 1, 128, 1060, 3), (300, 1, 4, 64, 1500, 2), (65, 4, 1, 128, 1024, 20)])
+def test_whole_sequences_in_the_order_of_their_lengths(act, batch, heads, group, dh, longest, most):
+    """Several rounds of workgroups over a table of 1024 positions and more: lengths that are equal, zero, and as wide as the table; sequences without rows."""
+    g = np.random.default_rng(batch)
+    lens = (longest * g.random(batch) ** 6).astype(int)
+    lens[g.integers(0, batch, batch // 4)] = 0
+    lens[batch // 2], lens[batch - 1] = longest, longest
+    counts = g.integers(0, most + 1, batch) if most > 1 else np.ones(batch, int)
+    counts[[0, batch // 2, batch - 1]] = most
+    p = paged_plan(heads * group, int(counts.sum()), most, {"bf16": P.BF16, "fp32": P.FP32}[act], batch, -(-longest // 16), 16, heads, dh, P.E2M1)
+    assert p.kernel == "split" and 256 < p.cap * heads * p.q_groups <= 1024
+    c = FourBits(lens.tolist(), 16, heads, dh, seed=batch, holes=0.1).fill(act)
+    q = rows(g, (int(counts.sum()), heads * group, dh), act)
+    check_attn(c, q, counts.tolist(), most=most)
+
+
+@pytest.mark.parametrize("group,most", [(1, 1), (7, 2)])
+def test_slices_for_two_workgroups_of_a_compute_unit(group, most):
+    lens = [8200, 0, 200, 1] + [int(x) for x in np.random.default_rng(8).integers(0, 180, 27)] + [2500]
+    counts = [most] * 16 + [1] * 16
+    p = paged_plan(8 * group, sum(counts), most, P.BF16, 32, 129, 64, 8, 128, P.E2M1)
+    assert p.kernel == "split+" and p.want == 64
+    c = FourBits(lens, 64, 8, 128, seed=9, holes=0.05).fill("bf16")
+    q = rows(np.random.default_rng(10), (sum(counts), 8 * group, 128), "bf16")
+    a, b = check_attn(c, q, counts, most=most), check_attn(c, q, counts, most=most)
+    assert torch.equal(a.view(torch.int16), b.view(torch.int16))
 
 
 def make(name, types, seed, size=1.0):
