@@ -111,6 +111,18 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
         }
     }
     p.split = key_tiles > whole_tiles(dtype, head_dim) && want > c.batch;
+    // e2m1, whole sequences: groups of 16 query rows, two workgroups of which fit a compute unit, or of 32, of which one does. A round of the first, full, takes 9 / 8 of one of the
+    // second (28/4 heads, 4 sequences of 1024 keys, 64 rows 14.3 us and 12.7; 32 heads, 8 of 1024, 64 rows 25.6 and 25.0), of one workgroup a unit 5 / 8: whatever is less, up to 1024 groups (us by 32
+    // and by 16; 19 of 700 keys, 10 rows of 32/8 heads 20.3 and 12.6; 12 of 1500, 17 rows 28.5 and 18.6; one of 2700, 300 rows 44.9 and 37.5; 64 of 1000, 5 rows of 28/4 heads 25.3 and 21.2, ragged 18.2
+    // and 13.5; more groups, ragged: 16 of 2000, 40 rows 26.2 and 29.1, 20 of 2000, 17 rows of 32 heads 30.4 and 37.7, which are in the order of their lengths by 32).
+    if (!p.split && p.nq == 2 && four_bits(cache_dtype, head_dim)) {
+        const int64_t pairs = (int64_t)c.batch * heads, halves = pairs * tiles, full = halves / (2 * kWorkgroups), rest = halves % (2 * kWorkgroups);
+        const int64_t rounds = (pairs * p.q_groups + kWorkgroups - 1) / kWorkgroups;
+        if (halves <= 4 * kWorkgroups && 9 * full + (rest == 0 ? 0 : rest <= kWorkgroups ? 5 : 9) < 8 * rounds) {
+            p.nq = 1;
+            p.q_groups = tiles;
+        }
+    }
     // Blocks of 128 query rows (paged_wide.h) where tiles of 32 would make more than one round of workgroups (128 dims; 28/4 heads, 1024 keys: 1
     // sequence of 300 rows, 264 workgroups, 29 -> 26 us, 4 of 128 rows, 448, 30 -> 27, but 4 of 64 rows, 224, 17 -> 26) or more than three (64
     // dims, 32 heads, 8 ragged sequences of up to 5600 keys: bf16, 80 rows 61 -> 61, 128 rows 81 -> 70, 250 rows, 119 -> 104; e4m3 65 ->

@@ -23,6 +23,7 @@ CALLS = {
 BLOCKS = [name for name in CALLS if CALLS[name][6].startswith("wide")]
 # Over an e2m1 cache, whose blocks of 128 query rows begin later with 128 dims, the same kernels.
 E2M1_CALLS = CALLS | {
+    "split_groups_of_16": ([300, 90, 33], [90, 20, 77], 16, 32, 1, 128, "split"),
     "blocks": ([200, 90], [300, 40], 16, 16, 4, 128, "wide1"),
     "halves": ([700, 333], [300, 40], 16, 12, 4, 128, "wide2"),
     "halves_cut": ([11000], [300], 16, 4, 4, 128, "wide2+"),

@@ -119,6 +119,16 @@ def test_where_a_compute_unit_has_two_slices(batch, keys, rows, dh, dtype, kerne
     assert p.kernel == kernel and (not p.split or p.want == (64 if batch == 32 else 32))
 
 
+@pytest.mark.parametrize("batch,heads,group,rows,keys,tiles,groups", [
+    (3, 32, 1, 90, 300, 1, 6),                             # 288 groups of 32, 576 of 16: two rounds against one and a bit
+    (19, 8, 4, 10, 700, 1, 3), (12, 8, 4, 17, 1500, 1, 5), (64, 4, 7, 5, 1000, 1, 3),
+    (4, 4, 7, 64, 1024, 2, 14), (8, 32, 1, 64, 1024, 2, 2), (20, 32, 1, 17, 2000, 2, 1),
+    (16, 4, 7, 40, 2000, 8, 3)])                           # blocks of 128
+def test_where_groups_of_16_query_rows_are_taken(batch, heads, group, rows, keys, tiles, groups):
+    p = paged_plan(heads * group, batch * rows, rows, P.BF16, batch, -(-keys // 16), 16, heads, 128, P.E2M1)
+    assert p.kernel == ("split" if tiles < 8 else "wide2") and (p.q_tiles, p.q_groups) == (tiles, groups)
+
+
 def tensors():
     pages = torch.zeros((5, 2, 16, 32), dtype=torch.uint8).view(torch.float4_e2m1fn_x2)
     scale = torch.zeros((5, 2, 16, 2), dtype=torch.uint8).view(torch.float8_e8m0fnu)
