@@ -86,7 +86,8 @@ def test_the_calls_take_every_kernel():
 
 @pytest.mark.parametrize("group,heads,dh,batch,keys,dtype", [
     (7, 4, 128, 8, 4096, P.BF16), (7, 4, 128, 1, 32768, P.BF16), (1, 32, 128, 4, 2100, P.BF16), (16, 1, 64, 6, 9000, P.BF16), (4, 8, 64, 2, 100000, P.BF16),
-    (3, 8, 32, 3, 5000, P.BF16), (4, 2, 128, 5, 1000, P.FP32), (8, 24, 128, 2, 700, P.BF16), (1, 1, 128, 100, 2000, P.BF16), (16, 1, 128, 2, 50000, P.BF16)])
+    (3, 8, 32, 3, 5000, P.BF16), (4, 2, 128, 5, 1000, P.FP32), (8, 24, 128, 2, 700, P.BF16), (1, 1, 128, 100, 2000, P.BF16), (16, 1, 128, 2, 50000, P.BF16),
+    (1, 32, 128, 8, 9000, P.BF16), (7, 4, 128, 64, 8192, P.BF16)])
 def test_a_workspace_for_many_rows_is_enough_for_fewer(group, heads, dh, batch, keys, dtype):
     sizes = dict(batch=batch, max_pages=-(-keys // 16), page_size=16, n_kv_heads=heads, head_dim=dh, cache_dtype=P.E2M1)
     d = B.PagedCacheDesc(16, 16, 16, 16, 16, 16, batch, batch * sizes["max_pages"], sizes["max_pages"], 16, heads, dh, P.E2M1)
