@@ -44,7 +44,7 @@ typedef PagedAttnPlan Plan;
 // what the first does (two sequences of 131072 keys: 56 us with 256 workgroups, 67 with 512). Smaller heads would leave room for two and more, which
 // is not made use of: nothing gained over bf16 and fp32 caches but for a few calls, 10 to 30 % over e4m3 ones (two sequences of 131072 keys of 28/4 heads, one
 // workgroup and two a unit: 64 dims, bf16 47.8 us and 48.7, e4m3 33.1 and 30.5; 32 dims, e4m3 28.1 and 21.9; 16 ragged ones of 4096, 64 dims, bf16 13.2
-// and 13.9). A slice has 4 tiles of keys at least: what a compute unit
+// and 13.9; over e2m1 it is, see make_plan). A slice has 4 tiles of keys at least: what a compute unit
 // reads is bound to some 50 GB/s, so idle units cost more than wavefronts without a tile (28/4 heads, 4 sequences of 2000 keys in
 // bf16: 10.5 us with 4 tiles, 11.4 with 8, 17.2 with 32, 22.3 without slices). paged_attn_wide, whose groups take 64 keys at a time: 16
 // tiles of 32 (28/4 heads, 64 rows, 4096 keys 23.1 us with 8, 21.9 with 16, 26.7 with 32; 16384 keys 36.8, 35.4, 35.3).
@@ -100,12 +100,13 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     p.spread = best_spread(p.q_groups, heads, 1);
     p.least = kLeast;
     int want = slices_at_once(p.q_groups, heads, p.spread, 1);
-    // e2m1, few rows: two workgroups fit a unit. Slices for both where one each would leave the sequences of a long table whole, and make two of each at least (us
+    // e2m1, up to 16 query rows: two workgroups fit a unit. Slices for both where one each would leave the sequences of a long table whole, and make two of each at least (us
     // whole and cut, one token, 8 sequences, 32 heads: up to 16384 keys 80 and 62, 32 of up to 8192, 32/8 heads, 42 and 33.7, 8192 keys each 50 and 52; up to 4096 keys 24 and 21.6, but 2048 keys each
-    // 15.7 and 18.6).
-    if (dtype == DKV_BF16 && four_bits(cache_dtype, head_dim) && p.nq == 1 && want <= c.batch && keys >= 8192) {
-        const int spread = best_spread(p.q_groups, heads, 2), more = slices_at_once(p.q_groups, heads, spread, 2);
-        if (more >= 2 * c.batch) {
+    // 15.7 and 18.6; heads of 64 up to 16384 keys 61 and 37.6, 8192 each 34.4 and 30.9). Heads of 64 and 32, up to 128 slices, also where there are slices anyway (2 sequences of 131072 keys,
+    // 28/4 heads 23.2 and 21.3, 32 dims 20.7 and 17.5; 8 of 8192, 32/8 heads 15.3 and 14.3; 512 slices of one sequence 12 and 15.5); with 128 dims the two sequences take 29.8 and 31.6.
+    if (dtype == DKV_BF16 && cache_dtype == DKV_E2M1 && tiles == 1) {
+        const int spread = best_spread(1, heads, 2), more = slices_at_once(1, heads, spread, 2);
+        if (want <= c.batch ? keys >= 8192 && more >= 2 * c.batch : head_dim < 128 && more <= 128) {
             want = more;
             p.spread = spread;
         }
@@ -213,7 +214,7 @@ size_t most_partial_bytes(const PagedCache &c, int n_q_heads, int rows, int max_
         }
         return meta_bytes(c) + (size_t)n * (nq * 16) * (head_dim + 4) * sizeof(float);
     };
-    const size_t split = bytes(split_tiles(dtype, tiles), kLeast, four_bits(cache_dtype, head_dim) ? 2 : 1);
+    const size_t split = bytes(split_tiles(dtype, tiles), kLeast, cache_dtype == DKV_E2M1 ? 2 : 1);
     const int64_t groups = row_groups(c, rows, max_rows, G, 32), keys = (int64_t)key_tiles * PKT;
     if (!rows_for_blocks(dtype, head_dim, max_rows * G) || !keys_to_cut(head_dim, keys) ||
         !(blocks_for_rounds(cache_dtype, head_dim, groups) || blocks_for_keys(cache_dtype, head_dim, groups, keys)))

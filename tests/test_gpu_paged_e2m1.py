@@ -196,16 +196,25 @@ def test_whole_sequences_in_the_order_of_their_lengths(act, batch, heads, group,
     check_attn(c, q, counts.tolist(), most=most)
 
 
-@pytest.mark.parametrize("group,most", [(1, 1), (7, 2)])
-def test_slices_for_two_workgroups_of_a_compute_unit(group, most):
+@pytest.mark.parametrize("group,most,dh", [(1, 1, 128), (7, 2, 128), (7, 2, 64), (1, 3, 32)])
+def test_slices_for_two_workgroups_of_a_compute_unit(group, most, dh):
     lens = [8200, 0, 200, 1] + [int(x) for x in np.random.default_rng(8).integers(0, 180, 27)] + [2500]
     counts = [most] * 16 + [1] * 16
-    p = paged_plan(8 * group, sum(counts), most, P.BF16, 32, 129, 64, 8, 128, P.E2M1)
+    p = paged_plan(8 * group, sum(counts), most, P.BF16, 32, 129, 64, 8, dh, P.E2M1)
     assert p.kernel == "split+" and p.want == 64
-    c = FourBits(lens, 64, 8, 128, seed=9, holes=0.05).fill("bf16")
-    q = rows(np.random.default_rng(10), (sum(counts), 8 * group, 128), "bf16")
+    c = FourBits(lens, 64, 8, dh, seed=9, holes=0.05).fill("bf16")
+    q = rows(np.random.default_rng(10), (sum(counts), 8 * group, dh), "bf16")
     a, b = check_attn(c, q, counts, most=most), check_attn(c, q, counts, most=most)
     assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+@pytest.mark.parametrize("dh", [64, 32])
+def test_slices_of_small_heads(dh):
+    lens, counts = [5000, 0, 1300], [1, 1, 2]
+    p = paged_plan(4 * 7, 4, 2, P.BF16, 3, 157, 32, 4, dh, P.E2M1)
+    assert p.kernel == "split+" and p.want == 128
+    c = FourBits(lens, 32, 4, dh, seed=11, holes=0.1).fill("bf16")
+    check_attn(c, rows(np.random.default_rng(12), (4, 28, dh), "bf16"), counts, most=2)
 
 
 def make(name, types, seed, size=1.0):

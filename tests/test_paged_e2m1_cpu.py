@@ -113,7 +113,7 @@ def test_where_blocks_of_128_rows_begin(heads, rows, keys, kernel):
 
 @pytest.mark.parametrize("batch,keys,rows,dh,dtype,kernel", [
     (32, 8192, 1, 128, P.BF16, "split+"), (32, 8160, 1, 128, P.BF16, "split"), (33, 8192, 1, 128, P.BF16, "split"), (32, 8192, 17, 128, P.BF16, "split"),
-    (32, 8192, 1, 64, P.BF16, "split"), (32, 8192, 1, 128, P.FP32, "split"), (31, 8160, 1, 128, P.BF16, "split+")])
+    (32, 8192, 1, 64, P.BF16, "split+"), (32, 8192, 1, 128, P.FP32, "split"), (31, 8160, 1, 128, P.BF16, "split+")])
 def test_where_a_compute_unit_has_two_slices(batch, keys, rows, dh, dtype, kernel):
     """8 K/V heads: 32 slices of each with one workgroup a unit, 64 with two, which serve up to 32 sequences of at least 8192 positions."""
     p = paged_plan(8, batch * rows, rows, dtype, batch, keys // 32, 32, 8, dh, P.E2M1)
