@@ -149,3 +149,5 @@ struct PagedAttnPlan {
 // What both entry points of the attention refuse, and the plan of what they do not.
 int dkv_paged_attn_plan(const dkv_paged_cache *cache, PagedCache &view, PagedAttnPlan &plan, int n_q_heads, int rows, int max_rows_per_seq,
                         int dtype);
+// Launches that dkv_paged_resize makes: one, or three. listed: whether it lists the new positions, `rows` of them at most.
+int dkv_paged_resize_launches(const dkv_paged_tables &tables, bool listed, int rows);

@@ -353,6 +353,21 @@ size_t work_bytes(int batch) { return kTotalsBytes + 5 * sizeof(int) * (size_t)b
 
 }  // namespace
 
+// By what the host knows, rows of the lists and entries of the tables that can move, in one launch and in three, us in a graph:
+//   rows: 4096 4.4 and -, 8192 6.3-8.2 and 7-10, 16384 8.8-14.5 and 7.1-9.7, 65536 31-39 and 8.1-9.3.
+//   entries without lists, where moving many is what a call is for. 64 sequences that leave: 64 pages each 5.3 and 7.7, 128 8.1 and 7.7, 256 13.4 and
+//     8.0; that take them 4.8 and 7.4, 6.7 and 7.4, 10.8 and 7.2. 512 sequences: 4 pages 5.6 and 8.1 (4.4 and 7.6), 16 11.4 and 7.9 (9.8 and 8.2), 256
+//     119 and 8.4 (92 and 8.4); 1024 of 2048 pages 2088 and 23.
+//   entries with a list of a few rows, a server's step, which seldom moves more than a page for each sequence (4.0 and 7.1, with 512 sequences 6.1 and
+//     10.6, however wide the tables) but can give all back: 64 sequences of 1024 pages 46 and 13, of 4096 176 and 28; 512 of 64 32 and 8.6, of 256
+//     119 and 8.6; 1024 of 64 69 and 9.4.
+// A sequence gives its pages back by one wavefront in the three-launch form, 4 us for 1024 of them and 0.65 in the other (one of 4096 pages 4.4 and 20,
+// 16 of 4096 45 and 24): the pages of six sequences do not count.
+int dkv_paged_resize_launches(const dkv_paged_tables &c, bool listed, int rows) {
+    const int64_t entries = (int64_t)c.batch * c.max_pages, move = (entries < c.n_pages ? entries : c.n_pages) - 6 * (int64_t)c.max_pages;
+    return c.batch <= kThreads && (!listed || rows <= 8192) && move <= (listed ? 65536 : 6144) ? 1 : 3;
+}
+
 extern "C" size_t dkv_paged_resize_workspace_bytes(int32_t batch) {
     if (batch < 1 || batch > kMostSequences) { dkv_set_error("%d sequences: 1 to %d are expected", batch, kMostSequences); return 0; }
     return work_bytes(batch);
@@ -380,8 +395,7 @@ extern "C" int dkv_paged_resize(const dkv_paged_tables *tables, const int32_t *l
     int *arrays = reinterpret_cast<int *>(static_cast<char *>(workspace) + kTotalsBytes);
     const Work w = {static_cast<Totals *>(workspace), arrays, arrays + c.batch, arrays + 2 * (size_t)c.batch, arrays + 3 * (size_t)c.batch, arrays + 4 * (size_t)c.batch};
     hipStream_t s = static_cast<hipStream_t>(stream);
-    // rows in one launch and in three, us in a graph: 4096 4.4 and -, 8192 6.3-8.2 and 7-10, 16384 8.8-14.5 and 7.1-9.7, 65536 31-39 and 8.1-9.3
-    if (c.batch <= kThreads && (!row_off || rows <= 8192)) {
+    if (dkv_paged_resize_launches(c, row_off != nullptr, rows) == 1) {
         hipLaunchKernelGGL(paged_resize_small, dim3(1), dim3(kThreads), 0, s, t, lengths, l);
         DKV_LAUNCH_CHECK();
         return DKV_OK;

@@ -139,3 +139,11 @@ def paged_plan(n_q_heads, rows, most, dtype, batch, max_pages, page_size, n_kv_h
     view, plan = C.create_string_buffer(256), PagedAttnPlan()           # the kernels' view of the cache is not looked at
     b._check(f(C.byref(d), view, C.byref(plan), n_q_heads, rows, most, dtype))
     return plan
+
+
+def resize_launches(batch, max_pages, n_pages, rows=None, page_size=16):
+    """Launches of dkv_paged_resize for tables of these sizes; rows: of the lists of new positions (None: no lists)."""
+    from paper_2505_15781_amd import binding as b
+    f = b.lib._Z25dkv_paged_resize_launchesRK16dkv_paged_tablesbi
+    f.restype, f.argtypes = C.c_int, [C.POINTER(b.PagedTablesDesc), C.c_bool, C.c_int]
+    return f(C.byref(b.PagedTablesDesc(16, 16, 16, 16, batch, n_pages, max_pages, page_size)), rows is not None, rows or 0)

@@ -5,6 +5,7 @@ import torch
 
 import paper_2505_15781_amd as P
 from oracle import tables as O
+from plans import resize_launches
 from test_gpu_paged import dev
 
 pytestmark = pytest.mark.gpu
@@ -168,3 +169,77 @@ def test_two_tables_on_two_streams(batch):
         for w in ws:
             O.resize(b.table, b.len, b.ring, b.at, 16, [int(x) for x in w])
         b.same()
+
+
+# batch, pages of a table, holes: on both sides of the border between one launch and three, for calls without lists and for those with a short one
+MOVES = [(1, 1500, 0.0), (7, 900, 0.2), (40, 180, 0.2), (40, 181, 0.2), (512, 13, 0.0), (1024, 7, 0.3), (75, 940, 0.1), (75, 960, 0.1), (1024, 65, 0.0)]
+
+
+@pytest.mark.parametrize("case", MOVES, ids=[str(m) for m in MOVES])
+def test_many_pages_move_for_few_rows_or_none(case):
+    """All pages taken without lists, given back with a list of a few rows, taken and given back without, and in parts."""
+    batch, width, holes = case
+    b = Both(batch, width, batch * width, 16, seed=width, first=3)
+    full, none = np.full(batch, 16 * width), np.zeros(batch, int)
+    b.resize(full, lists="none")
+    if holes:
+        b.holes(holes)
+    b.resize(none)                                         # with a list of 8 rows
+    b.resize(b.g.integers(0, 16 * width + 1, batch), lists="none")
+    b.resize(np.where(np.arange(batch) % 3 == 0, np.array(b.len) + 1, 0), room=0)
+    b.resize(full, lists="none")
+    b.resize(none, lists="none")
+
+
+def test_the_moves_lie_on_both_sides_of_the_borders():
+    forms = {(rows, resize_launches(batch, width, batch * width, rows)) for batch, width, _ in MOVES for rows in (None, 8)}
+    assert forms == {(None, 1), (None, 3), (8, 1), (8, 3)}
+    assert [resize_launches(40, w, 40 * w) for w in (180, 181)] == [1, 3]
+
+
+@pytest.mark.parametrize("batch,width", [(60, 40), (1000, 5)])
+def test_two_small_tables_on_two_streams(batch, width):
+    """One launch each."""
+    both = [Both(batch, width, batch * width - 7, 16, seed=i) for i in range(2)]
+    assert resize_launches(batch, width, batch * width - 7) == 1
+    wants = [[b.g.integers(0, 16 * width + 1, batch) for _ in range(8)] for b in both]
+    streams = [torch.cuda.Stream() for _ in both]
+    dev_wants = [[dev(w) for w in ws] for ws in wants]
+    torch.cuda.synchronize()
+    for i in range(8):
+        for b, s, w in zip(both, streams, dev_wants):
+            with torch.cuda.stream(s):
+                P.paged_resize(b.t, w[i], b.ws)
+    torch.cuda.synchronize()
+    for b, ws in zip(both, wants):
+        for w in ws:
+            O.resize(b.table, b.len, b.ring, b.at, 16, [int(x) for x in w])
+        b.same()
+
+
+@pytest.mark.parametrize("batch,rows", [(500, 300), (900, 9)])
+def test_captured_calls_that_move_many_pages(batch, rows):
+    """A captured call with a short list over tables that take three launches for it, and one without lists, replayed in turn."""
+    width = 160
+    b = Both(batch, width, width * batch, 16, seed=4)
+    assert resize_launches(batch, width, width * batch, rows) == resize_launches(batch, width, width * batch) == 3
+    want, bulk = dev(np.zeros(batch)), dev(np.zeros(batch))
+    off, pos, slots = dev(np.zeros(batch + 1)), dev(np.full(rows, -3)), torch.full((rows,), -3, dtype=torch.int64, device="cuda")
+    b.resize(np.full(batch, 7), lists="none")
+    first, second = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(first):
+        P.paged_resize(b.t, want, b.ws, off, pos, slots)
+    with torch.cuda.graph(second):
+        P.paged_resize(b.t, bulk, b.ws)
+    for i in range(4):
+        lengths = b.g.integers(0, 16 * width + 1, batch)
+        bulk.copy_(dev(lengths))
+        second.replay()
+        O.resize(b.table, b.len, b.ring, b.at, 16, lengths.tolist())
+        b.same()
+        lengths = np.where(b.g.random(batch) < 0.7, 0, np.array(b.len) + b.g.integers(0, 3, batch))
+        want.copy_(dev(lengths))
+        first.replay()
+        o, p, s = O.resize(b.table, b.len, b.ring, b.at, 16, lengths.tolist(), rows)
+        b.same()
+        assert off.tolist() == o and pos[:o[-1]].tolist() == p and slots[:o[-1]].tolist() == s

@@ -8,6 +8,7 @@ import torch
 import paper_2505_15781_amd as P
 from oracle import tables as O
 from paper_2505_15781_amd import binding as B
+from plans import resize_launches
 
 
 def test_the_oracle_keeps_every_page_in_one_place():
@@ -96,3 +97,25 @@ def test_the_binding_refuses_tensors_that_are_not_what_a_call_reads():
         P.paged_resize(tuple(t)[:4], i(3), ws)
     with pytest.raises(TypeError):
         P.paged_resize(t._replace(page_size=None), i(3), ws)
+
+
+def test_the_launches_go_by_the_pages_that_can_move_too():
+    """One workgroup moves 4096 entries at a time: tables and pools of which many entries can move are not left to it."""
+    for rows in (0, 8, 8192):                              # a server's step over ordinary tables
+        assert resize_launches(64, 257, 8500, rows) == resize_launches(64, 1024, 65536, rows) == resize_launches(1024, 64, 65536, rows) == 1
+        assert resize_launches(512, 256, 512 * 256, rows) == resize_launches(1024, 2048, 1 << 21, rows) == resize_launches(64, 4096, 64 * 4096, rows) == 3
+    assert resize_launches(64, 100, 6400) == resize_launches(512, 8, 4096) == resize_launches(1, 256, 256) == 1
+    assert resize_launches(64, 256, 64 * 256) == resize_launches(512, 256, 512 * 256) == resize_launches(1024, 2048, 1 << 21) == 3
+    # wide tables over a small pool, and few sequences whatever they hold
+    assert resize_launches(1000, 1 << 14, 1 << 15) == resize_launches(1000, 1 << 14, 1 << 15, 5) == 1
+    assert resize_launches(1, 1 << 16, 1 << 16) == resize_launches(6, 1 << 16, 6 << 16) == 1
+    # rows of the lists and sequences as before
+    assert resize_launches(20, 30, 600, 8193) == resize_launches(1025, 4, 3000, 9) == resize_launches(1025, 4, 3000) == 3
+
+
+@pytest.mark.parametrize("rows,most", [(None, 6144), (9, 65536)])
+def test_the_border_between_the_forms(rows, most):
+    for batch in (7, 40, 300, 1024):
+        width = most // (batch - 6)
+        assert resize_launches(batch, width, batch * width, rows) == 1 and resize_launches(batch, width + 1, batch * (width + 1), rows) == 3
+        assert resize_launches(batch, width + 1, most + 6 * (width + 1), rows) == 1       # a smaller pool
