@@ -243,3 +243,37 @@ def test_captured_calls_that_move_many_pages(batch, rows):
         o, p, s = O.resize(b.table, b.len, b.ring, b.at, 16, lengths.tolist(), rows)
         b.same()
         assert off.tolist() == o and pos[:o[-1]].tolist() == p and slots[:o[-1]].tolist() == s
+
+
+def test_sums_beyond_32_bits_of_many_sequences():
+    """2100 sequences, three groups of 1024 in the sums, that want 2^30 positions each: sums that end at their largest number go on from group to group,
+    and so does the place where the first sequence did not fit, which is in the first group or in a later one."""
+    batch, page, width = 2100, 65536, 1 << 14
+    table = torch.full((batch, width), -1, dtype=torch.int32, device="cuda")
+    ws = torch.empty(P.paged_resize_workspace_bytes(batch), dtype=torch.uint8, device="cuda")
+
+    def call(want, n, rows):
+        t = P.PagedTables(table.fill_(-1), dev(np.zeros(batch)), torch.arange(n, dtype=torch.int32, device="cuda"), dev([0, n]), page)
+        lists = () if rows is None else (dev(np.full(batch + 1, -3)), dev(np.full(rows, -3)), torch.full((rows,), -3, dtype=torch.int64, device="cuda"))
+        P.paged_resize(t, dev(want), ws, *lists)
+        return t, lists
+
+    # more pages than are asked for, ten rows: the first sequence stops all, those of the third group that want a single row among them
+    want = np.full(batch, 1 << 30)
+    want[2048:] = 1
+    t, (off, pos, slots) = call(want, 1 << 26, 10)
+    assert int(off.abs().max()) == 0 and int(t.seq_len.abs().max()) == 0 and (pos == -3).all() and (slots == -3).all()
+    assert t.free_at.tolist() == [0, 1 << 26] and int(table.max()) == -1
+    # 1500 single rows fit, the next sequence stops the rest
+    want[:1500] = 1
+    t, (off, pos, slots) = call(want, 1 << 26, 2000)
+    assert off.tolist() == list(range(1501)) + [1500] * 600 and t.seq_len.tolist() == [1] * 1500 + [0] * 600 and t.free_at.tolist() == [1500, (1 << 26) - 1500]
+    assert (pos[:1500] == 0).all() and slots[:1500].tolist() == [page * b for b in range(1500)] and (pos[1500:] == -3).all() and (slots[1500:] == -3).all()
+    assert table[:1500, 0].tolist() == list(range(1500)) and int(table[:1500, 1:].max()) == int(table[1500:].max()) == -1
+    # too few pages, without lists: 1500 of one page, one of 2^14, and no further one
+    t, _ = call(want, 1 << 15, None)
+    assert t.seq_len.tolist() == [1] * 1500 + [1 << 30] + [0] * 599 and t.free_at.tolist() == [1500 + width, (1 << 15) - 1500 - width]
+    assert torch.equal(table[1500], torch.arange(1500, 1500 + width, dtype=torch.int32, device="cuda")) and int(table[1501:].max()) == -1
+    # the first two of the first group
+    t, _ = call(np.full(batch, 1 << 30), 1 << 15, None)
+    assert t.seq_len.tolist() == [1 << 30] * 2 + [0] * (batch - 2) and t.free_at.tolist() == [0, 0]
