@@ -56,13 +56,6 @@ template <typename T> __device__ __forceinline__ Piece<16> load_piece(const T *p
 }
 __device__ __forceinline__ void store_piece(float *p, Piece<4> x) { *reinterpret_cast<f32x4_el *>(p) = x; }
 __device__ __forceinline__ void store_piece(bf16_t *p, Piece<8> x) { store8(p, x); }
-// with the non-temporal hint
-__device__ __forceinline__ void store_piece_nt(float *p, Piece<4> x) { __builtin_nontemporal_store((f32x4)x, reinterpret_cast<f32x4_el *>(p)); }
-__device__ __forceinline__ void store_piece_nt(bf16_t *p, Piece<8> x) {
-    u32x4 y;
-    store8(reinterpret_cast<bf16_t *>(&y), x);
-    __builtin_nontemporal_store(y, reinterpret_cast<bf16x8_el *>(p));
-}
 
 // Maximum over the 2, 4 or 8 neighbouring lanes that hold a row.
 template <int LANES> __device__ __forceinline__ float row_max(float x) {
@@ -208,11 +201,13 @@ __global__ __launch_bounds__(512) void paged_store_e2m1(PagedCache c, const T *_
     }
 }
 
-// A lane writes N times 16 bytes. Its loads are short where the cache is e4m3 (8 bytes for bf16 rows, 4 for fp32) or e2m1 (half of that), and wait for the
-// row's place: with many rows four at once are ahead. They meet at 4096 wavefronts of four pieces a lane (32 heads of 128 from e4m3 to bf16: 512 rows 5.6
-// against 4.9, 1024 rows 7.3 and 7.5, 2048 rows 14.2 and 16.4). From bf16 and fp32 caches one is. So many rows are more than the caches hold until somebody reads
-// them: four pieces are written with the non-temporal hint (6144 rows of 32 heads from e2m1 to bf16 38.4 -> 26.5 us, 4.8 TB/s, to fp32 62.6 -> 39.0, 5.8; from e4m3 to bf16
-// 35 -> 25.2, 6.0; 2048 rows 14.2 -> 11.3). From bf16 to bf16 42 (4.8 TB/s), to fp32 75 (4.0), from fp32 to fp32 72 (5.6).
+// A lane writes N times 16 bytes. Its loads are short where the cache is e4m3 (8 bytes for bf16 rows, 4 for fp32) or e2m1 (half of that), and
+// wait for the row's place: with many rows four at once are ahead. They meet at 4096 wavefronts of four pieces a lane (32 heads of 128 from
+// e4m3 to bf16: 512 rows 5.6 against 4.9, 1024 rows 7.3 and 7.5, 2048 rows 14.2 and 16.4). From bf16 and fp32 caches one is. 6144 rows of 32
+// heads from e4m3 to bf16 35.7 us (4.2 TB/s), to fp32 61 (4.2), from e2m1 37.7 (3.4) and 62 (3.7), from bf16 to bf16 42 (4.8), to fp32 75 (4.0),
+// from fp32 to fp32 72 (5.6). The results are written into the caches, where whoever reads them next finds a part: with the non-temporal hint
+// the e4m3 and e2m1 loads of 6144 rows take 26 to 28 us (fp32 40), but with a copy of the results behind them 75 instead of 72 and 78 instead of 73
+// (e2m1 to fp32 136 and 134), 2048 rows 26.0 instead of 22.6, with their sum 20.4 instead of 19.3.
 template <typename T, typename C, int DH, int N>
 __global__ __launch_bounds__(256) void paged_load_kernel(PagedCache c, T *__restrict__ k_out, T *__restrict__ v_out,
                                                          const int *__restrict__ positions, const int *__restrict__ row_off, int rows,
@@ -239,8 +234,7 @@ __global__ __launch_bounds__(256) void paged_load_kernel(PagedCache c, T *__rest
         if constexpr (kRowScales<C, DH> > 0) x[u] *= scale[u];
         if (page < 0) x[u] = 0.f;
         T *to = (i / P % 2 ? v_out : k_out) + ((size_t)w.r * c.n_kv_heads + i / (2 * P)) * DH + E * (i % P);
-        if constexpr (N > 1) store_piece_nt(to, x[u]);
-        else store_piece(to, x[u]);
+        store_piece(to, x[u]);
     }
 }
 
