@@ -151,3 +151,5 @@ int dkv_paged_attn_plan(const dkv_paged_cache *cache, PagedCache &view, PagedAtt
                         int dtype);
 // Launches that dkv_paged_resize makes: one, or three. listed: whether it lists the new positions, `rows` of them at most.
 int dkv_paged_resize_launches(const dkv_paged_tables &tables, bool listed, int rows);
+// Heads that a lane of dkv_rope has at once, one or four, with pieces of v elements (one: a pair); 0 where the call has too many rows.
+int dkv_rope_lane_heads(int dtype, int v, int head_dim, int heads, int rows);

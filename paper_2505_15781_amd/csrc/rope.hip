@@ -6,9 +6,15 @@
 // positions at one radian each: an fp32 product is off by 2^-4): position times frequency, in quarter turns, and what is left of it in the
 // quarter are formed in 64 bits, sine and cosine of that from their Taylor series in 32.
 //
-// 6144 rows of 64 heads of 128 in bf16 (201 MB) 33.6 us, 6.0 TB/s (a large copy 4.46); 4099 rows of 32 heads in fp32, neighbouring pairs of 64 dims, into other memory (134 MB)
-// 20.2 us. With stores that stay in the caches 39.3 and 27.0: so many rows are more than the caches hold until somebody reads them. Neighbouring pairs in one piece of
-// 32 bytes a lane, every other 16 to a load, took 30.1 instead of 27.0. 64 rows 3.4 us; the call is 5.5 us of the host.
+// 6144 rows of 64 heads of 128 in bf16 (201 MB) 35.7 us in place, 39.4 into other memory (5.1 TB/s; a large copy 4.46), 3072 in fp32 34.5 and 38;
+// 64 rows 3.4 us, the call is 5.5 us of the host. Part of a head moves what a whole one does: in place 64 and 32 dims of 128 take 26 and 24 us
+// (all are read, those that are turned written). Where the pairs of a head are no multiple of 4 (neighbouring ones: of 2) a lane has one pair, and
+// these rows take 45 to 58.
+//
+// The results are written into the caches: the next launches of a layer read them. With the non-temporal hint rope alone is faster in some
+// calls (6144 rows in bf16 into other memory 39.8 -> 35.3 us, in place 35.7 -> 34.4, but 3072 rows 17.0 -> 18.9, 32 of 128 dims into other memory
+// 41 -> 47), not with its readers: stored into a cache and attended to 242 -> 246, in place 241.5 -> 242.5, 1024 rows 55.2 -> 55.3 and
+// 54.7 -> 55.0, 512 rows 47.0 -> 48.0 and 46.9 -> 47.0; with a copy of the results 57 -> 61.
 #include <math.h>
 
 #include <type_traits>
@@ -125,32 +131,24 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs<T> a) {
         }
         if (turn_lo) narrow(m, x[i]);
         if (turn_hi) narrow(n, y[i]);
-        // many rows: with the non-temporal hint
-        auto put = [&](typename B::type v, T *to) {
-            if constexpr (H > 1) __builtin_nontemporal_store(v, reinterpret_cast<typename B::at *>(to));
-            else *reinterpret_cast<typename B::at *>(to) = v;
-        };
-        if (turn_lo || moves) put(x[i], p + lo);
-        if (turn_hi || moves) put(y[i], p + hi);
+        if (turn_lo || moves) *reinterpret_cast<typename B::at *>(p + lo) = x[i];
+        if (turn_hi || moves) *reinterpret_cast<typename B::at *>(p + hi) = y[i];
     }
 }
 
 template <typename T, int V> int launch(RopeArgs<T> &a, bool pairs, hipStream_t s) {
     a.lanes = __builtin_ctz((unsigned)(a.head_dim / (2 * V)));
-    const int at_once = 64 >> a.lanes;
-    // four heads of a lane at once where that leaves 512 wavefronts (32 and 32 heads of 128, one head and four: 128 rows 3.6 and 4.2 us, 256 rows 5.0 and 4.4, 2048 rows 15.3
-    // and 12.5; 28 and 4: 256 rows 3.6 and 4.2, 512 rows 4.9 and 4.4; 8 and 2 of 64 in fp32: 512 rows 3.0 and 3.2, 1024 rows 3.5 and 3.4)
-    const bool many = (int64_t)a.rows * ((a.heads + 4 * at_once - 1) / (4 * at_once)) >= 512;
-    const int64_t parts = (a.heads + (many ? 4 : 1) * at_once - 1) / ((many ? 4 : 1) * at_once), groups = (parts * a.rows + 3) / 4;
-    if (groups >= 1 << 23) { dkv_set_error("%d rows of %d heads are too many for one call", a.rows, a.heads); return DKV_E_UNSUPPORTED; }
-    a.parts = Divisor((int)parts);
+    const int n = dkv_rope_lane_heads(sizeof(T) == 2 ? DKV_BF16 : DKV_FP32, V, a.head_dim, a.heads, a.rows);
+    if (!n) { dkv_set_error("%d rows of %d heads are too many for one call", a.rows, a.heads); return DKV_E_UNSUPPORTED; }
+    const int parts = ceil_div(a.heads, n * (64 >> a.lanes));
+    a.parts = Divisor(parts);
     auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, s, a);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(((int64_t)parts * a.rows + 3) / 4)), dim3(256), 0, s, a);
         DKV_LAUNCH_CHECK();
         return DKV_OK;
     };
-    if (pairs) return many ? go(rope_kernel<T, V, true, 4>) : go(rope_kernel<T, V, true, 1>);
-    return many ? go(rope_kernel<T, V, false, 4>) : go(rope_kernel<T, V, false, 1>);
+    if (pairs) return n == 4 ? go(rope_kernel<T, V, true, 4>) : go(rope_kernel<T, V, true, 1>);
+    return n == 4 ? go(rope_kernel<T, V, false, 4>) : go(rope_kernel<T, V, false, 1>);
 }
 
 bool rope_ok(const dkv_rope_desc &d) {
@@ -160,6 +158,22 @@ bool rope_ok(const dkv_rope_desc &d) {
 }
 
 }  // namespace
+
+// Four heads at once, so that a lane's cosines cost less (us with one head and with four):
+//   bf16 in pieces of 4 and 8, from 1024 wavefronts on: 32 and 32 heads of 128 in place 256 rows 4.2 and 4.4, 512 rows 6.1 and 5.2, 2048 rows 15.9 and
+//     12.0, 6144 rows 39.4 and 35.7; 28 and 4: 512 rows 4.2 and 4.4, 1024 rows 6.1 and 5.2
+//   one pair to a lane, from 2048 on: bf16, 32 and 32 heads 128 rows 3.6 and 3.5, 2048 rows 26 and 15; 28 and 4: 128 rows 3.1 and 3.2; fp32, 32 and 32:
+//     2048 rows 24 and 15
+//   fp32 in pieces of 4 does not: 32 and 32 heads of 128 in place 1024 rows 12.7 and 12.0, 6144 rows 71 and 76; neighbouring pairs into other memory
+//     512 rows 7.3 and 8.2, 1024 rows 12.0 and 12.1, 6144 rows 69 and 75
+// and only where one wavefront has not all heads anyway (8 and 2 heads of 64 in bf16, 6144 rows 6.6 and 7.3). Also where workgroups would be too many.
+int dkv_rope_lane_heads(int dtype, int v, int head_dim, int heads, int rows) {
+    const int at_once = 64 / (head_dim / (2 * v));
+    const int64_t ones = (int64_t)ceil_div(heads, at_once) * rows, fours = (int64_t)ceil_div(heads, 4 * at_once) * rows, most = 4ll << 23;      // wavefronts
+    if (fours > most - 4) return 0;
+    const bool gains = heads > at_once && (v == 1 ? fours >= 2048 : dtype == DKV_BF16 && fours >= 1024);
+    return gains || ones > most - 4 ? 4 : 1;
+}
 
 extern "C" int dkv_rope_init(dkv_rope_desc *rope, int32_t head_dim, int32_t rot_dim, int32_t interleaved, double theta, int32_t scaling,
                              double factor, double original, double slow, double fast) {

@@ -147,3 +147,11 @@ def resize_launches(batch, max_pages, n_pages, rows=None, page_size=16):
     f = b.lib._Z25dkv_paged_resize_launchesRK16dkv_paged_tablesbi
     f.restype, f.argtypes = C.c_int, [C.POINTER(b.PagedTablesDesc), C.c_bool, C.c_int]
     return f(C.byref(b.PagedTablesDesc(16, 16, 16, 16, batch, n_pages, max_pages, page_size)), rows is not None, rows or 0)
+
+
+def rope_lane_heads(dtype, piece, head_dim, heads, rows):
+    """Heads that a lane of dkv_rope has at once with pieces of this many elements (0: refused)."""
+    from paper_2505_15781_amd import binding as b
+    f = b.lib._Z19dkv_rope_lane_headsiiiii
+    f.restype, f.argtypes = C.c_int, [C.c_int] * 5
+    return f(dtype, piece, head_dim, heads, rows)

@@ -167,3 +167,12 @@ def test_two_streams_and_a_captured_call():
         torch.cuda.synchronize()
         P.rope(P.Rope(128), xs[0], None, pos, q_out=want[0])
         assert torch.equal(want[0], got[0])
+
+
+@pytest.mark.parametrize("act", ["bf16", "fp32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("shape", [(1100, 9, 4, 128, 120), (1100, 9, 4, 128, 124), (2100, 3, 2, 64, 30), (2048, 1, 4, 64, 62), (2047, 1, 4, 64, 62),
+                                   (1024, 5, 4, 128, 128), (1023, 5, 4, 128, 64), (1030, 5, 3, 128, 128)], ids=str)
+def test_heads_of_a_lane_one_or_four(act, interleaved, shape):
+    """Both sides of where a lane works on four heads at once, in pieces of 8 and 4 elements and of one."""
+    test_rows_are_rotated(act, interleaved, shape)

@@ -6,7 +6,7 @@ import pytest
 from test_device_code_cpu import device_code      # noqa: F401 (a fixture)
 
 
-@pytest.mark.parametrize("kernel,kinds", [("paged_load_kernel", 36)])
+@pytest.mark.parametrize("kernel,kinds", [("paged_load_kernel", 36), ("rope_kernel", 20)])
 def test_results_stay_in_the_caches_for_their_reader(device_code, kernel, kinds):      # noqa: F811
     """No store with the non-temporal hint: it ends the launch earlier, and whoever reads the rows next waits for memory instead."""
     functions, stores = set(), 0

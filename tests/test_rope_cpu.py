@@ -11,6 +11,7 @@ import torch
 import paper_2505_15781_amd as P
 from oracle import rotary as O
 from paper_2505_15781_amd import binding as B
+from plans import rope_lane_heads
 
 
 @pytest.mark.parametrize("scaling,factor", [("none", 1.0), ("linear", 4.0), ("base", 8.0), ("parts", 16.0), ("parts", 0.5)])
@@ -142,3 +143,15 @@ def test_the_oracle_turns_pairs_by_their_angles():
         assert np.array_equal(z[..., 48:], x[..., 48:])
         back, _ = O.rotate(y, pos, freq, 1.5, pairs, inverse=True)
         assert np.sum(z[..., :48] * y[..., :48]) == pytest.approx(np.sum(x[..., :48] * back[..., :48]))
+
+
+def test_heads_of_a_lane():
+    """Four where that gains; calls of the most workgroups, also of those that would be too many with one."""
+    assert [rope_lane_heads(P.BF16, 8, 128, 64, n) for n in (1, 511, 512, 6144)] == [1, 1, 4, 4]
+    assert [rope_lane_heads(P.BF16, 4, 128, 13, n) for n in (1023, 1024)] == [1, 4]
+    assert [rope_lane_heads(t, 1, 64, 5, n) for t in (P.BF16, P.FP32) for n in (2047, 2048)] == [1, 4, 1, 4]
+    assert {rope_lane_heads(P.FP32, 4, 128, 64, n) for n in (1, 512, 6144, 100000)} == {1}
+    assert rope_lane_heads(P.BF16, 8, 64, 10, 6144) == rope_lane_heads(P.FP32, 1, 32, 4, 6144) == 1      # all heads in one wavefront
+    # 64 heads of 128 in fp32, 16 wavefronts a row or 4: up to 2^25 of them
+    assert [rope_lane_heads(P.FP32, 4, 128, 64, n) for n in ((1 << 21) - 1, 1 << 21, (1 << 23) - 1, 1 << 23)] == [1, 4, 4, 0]
+    assert [rope_lane_heads(P.BF16, 8, 128, 64, n) for n in ((1 << 24) - 3, 1 << 24)] == [4, 0]
