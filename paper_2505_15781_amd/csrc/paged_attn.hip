@@ -201,7 +201,7 @@ size_t partial_bytes(const Plan &p, const PagedCache &c, int head_dim) {
 }
 // What no plan of this many rows and fewer exceeds, so that one workspace serves an active set that shrinks (fewer rows can have more slices: 28/4
 // heads, 8 sequences of 4096 keys, none with 128 rows each, 17 MB with 64, 4 with 8). The slices of a plan times its K/V heads and query groups are
-// one round of workgroups at most (slices_at_once; e2m1: of two to a compute unit), and no sequence has slices of less than `least` tiles.
+// one round of workgroups at most (slices_at_once; bf16 rows over e2m1: of two to a compute unit), and no sequence has slices of less than `least` tiles.
 size_t most_partial_bytes(const PagedCache &c, int n_q_heads, int rows, int max_rows, int dtype, int cache_dtype, int head_dim) {
     max_rows = max_rows < rows ? max_rows : rows;
     const int G = n_q_heads / c.n_kv_heads, tiles = ceil_div(max_rows > 0 ? max_rows * G : 1, 16), key_tiles = ceil_div(c.max_pages << c.page_shift, PKT);
@@ -214,7 +214,7 @@ size_t most_partial_bytes(const PagedCache &c, int n_q_heads, int rows, int max_
         }
         return meta_bytes(c) + (size_t)n * (nq * 16) * (head_dim + 4) * sizeof(float);
     };
-    const size_t split = bytes(split_tiles(dtype, tiles), kLeast, cache_dtype == DKV_E2M1 ? 2 : 1);
+    const size_t split = bytes(split_tiles(dtype, tiles), kLeast, dtype == DKV_BF16 && cache_dtype == DKV_E2M1 ? 2 : 1);
     const int64_t groups = row_groups(c, rows, max_rows, G, 32), keys = (int64_t)key_tiles * PKT;
     if (!rows_for_blocks(dtype, head_dim, max_rows * G) || !keys_to_cut(head_dim, keys) ||
         !(blocks_for_rounds(cache_dtype, head_dim, groups) || blocks_for_keys(cache_dtype, head_dim, groups, keys)))

@@ -157,3 +157,20 @@ def test_the_binding_refuses_tensors_that_are_not_what_a_call_reads():
     refused(("attn",), c, "q", q=torch.zeros((6, 4, 32), dtype=torch.bfloat16))
     huge = torch.empty((1, 1, 1, 2 ** 31 - 1), dtype=torch.uint8, device="meta").view(torch.float4_e2m1fn_x2)
     refused(ALL, c._replace(k_pages=huge, v_pages=huge), "32 bits")
+
+
+@pytest.mark.parametrize("heads,group,dh,batch,keys", [(8, 4, 128, 4, 9000), (32, 1, 64, 8, 16384), (4, 7, 32, 2, 100000), (1, 16, 128, 100, 2000)])
+def test_fp32_rows_need_no_more_workspace_than_over_e4m3(heads, group, dh, batch, keys):
+    """Their slices are those of one workgroup to a compute unit, whatever the cache; and enough for every call of fewer rows."""
+    pages = -(-keys // 16)
+
+    def bytes_for(dtype, m):
+        d = B.PagedCacheDesc(16, 16, 16, 16, 16, 16, batch, batch * pages, pages, 16, heads, dh, dtype)
+        return B.lib.dkv_paged_attn_workspace_bytes(C.byref(d), group * heads, batch * m, m, P.FP32)
+
+    for m in (1, 2, 7, 33, 150):
+        have = bytes_for(P.E2M1, m)
+        assert have == bytes_for(P.E4M3, m) > 0
+        for fewer in {1, m // 2, m} - {0}:
+            plan = paged_plan(group * heads, batch * fewer, fewer, P.FP32, batch, pages, 16, heads, dh, P.E2M1)
+            assert need(plan, batch, heads, dh) <= have
