@@ -145,6 +145,7 @@ struct PagedAttnPlan {
     int spread;             // log2 of the XCDs that the query groups of one (slice, K/V head) are on
     int least, want;        // see SlicePlan
     bool split;             // whether a sequence can have several slices
+    bool longest_first;     // whole sequences of paged_attn_split in the order of their lengths
 };
 // What both entry points of the attention refuse, and the plan of what they do not.
 int dkv_paged_attn_plan(const dkv_paged_cache *cache, PagedCache &view, PagedAttnPlan &plan, int n_q_heads, int rows, int max_rows_per_seq,

@@ -88,6 +88,10 @@ bool keys_to_cut(int head_dim, int64_t keys) { return keys >= (head_dim == 64 ? 
 int block_workgroups_per_cu(int head_dim) { return head_dim == 64 ? 3 : 1; }
 int split_tiles(int dtype, int tiles) { return dtype == DKV_BF16 && tiles > 1 ? 2 : 1; }
 
+int64_t split_grid(const Plan &p, const PagedCache &c) {
+    return (((int64_t)p.cap * c.n_kv_heads << p.spread) + 7) / 8 * 8 * ceil_div(p.q_groups, 1 << p.spread);
+}
+
 Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int dtype, int cache_dtype, int head_dim) {
     Plan p;
     max_rows = max_rows < rows ? max_rows : rows;
@@ -191,6 +195,18 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     p.want = p.split ? want : 1;
     const int64_t most = (int64_t)c.batch * ceil_div(key_tiles, p.least);
     p.cap = !p.split ? c.batch : (int)(most < want ? most : want);      // see slice_length
+    // e2m1: whole sequences with the longest first where they make more than one round of a workgroup for each compute unit and up to four, over tables
+    // of 1024 positions and more, batches of up to 64 sequences, which a wavefront orders. A workgroup then knows its sequence one look-up later
+    // (one token of ragged sequences, us in the order of the batch and so: 32 of up to 4096 keys, 32 heads 59-62 and 53, rows in fp32 237 and 182, 12 of
+    // them 30.4 and 26.6, heads of 64 38 and 32; 16 with 8 rows 33.6 and 31.3; 64 of up to 2048, 32/8 heads 22.1 and 18.9; of one length: 32 of 2048
+    // keys 49.7 and 49.9, 12 22.5 and 22.9). Beyond four rounds the gain is less and batches of one length lose (40, 48 and 64 of up to 4096 keys 68 and
+    // 64, 77 and 75, 99 and 94, of 2048 keys each 60.4 and 61.6, 72 and 74, 92 and 93; heads of 64, 64 of up to 4096 65 and 59, of 2048 each 57 and 60).
+    // In batches of more than 64, each 64 in order, it is as often a loss (28/4 heads, up to 4096 keys: 100 sequences 33.0 and 37.4, 128 38.9 and
+    // 40.3, 256 66.7 and 59.5; 16/2 heads 150 31.1 and 35.9, 300 42.2 and 40.5; 16/1 heads 1000 65 and 73; 32/8 heads 100 51.1 and 51.6, 128 65 and
+    // 54), also with every other 64 the shortest first (128 of 28/4 39.5 and 31.3, of 32/8 60.6 and 62.5). Over e4m3 and bf16 caches, one workgroup a
+    // unit, ragged batches gain as much, but batches of one length lose up to 3 %: left in the order of the batch.
+    p.longest_first = cache_dtype == DKV_E2M1 && !p.wide && !p.split && c.batch <= 64 && (int64_t)c.max_pages << c.page_shift >= 1024 &&
+                      split_grid(p, c) > kWorkgroups && split_grid(p, c) <= 4 * kWorkgroups;
     return p;
 }
 
@@ -222,20 +238,8 @@ size_t most_partial_bytes(const PagedCache &c, int n_q_heads, int rows, int max_
     const size_t blocks = bytes(8, kLeastWide, block_workgroups_per_cu(head_dim));
     return blocks > split ? blocks : split;
 }
-SlicePlan slice_plan(const Plan &p, bool longest_first) { return SlicePlan{p.least, Divisor(p.want), p.split, longest_first}; }
+SlicePlan slice_plan(const Plan &p) { return SlicePlan{p.least, Divisor(p.want), p.split, p.longest_first}; }
 GroupMap group_map(const Plan &p) { return GroupMap{Divisor(ceil_div(p.q_groups, 1 << p.spread)), p.spread, p.q_groups * p.nq * 16}; }
-int64_t split_grid(const Plan &p, const PagedCache &c) {
-    return (((int64_t)p.cap * c.n_kv_heads << p.spread) + 7) / 8 * 8 * ceil_div(p.q_groups, 1 << p.spread);
-}
-// e2m1: whole sequences with the longest first where they make more than one round of a workgroup for each compute unit and up to four, over tables of 1024
-// positions and more. A workgroup then knows its sequence one look-up later (one token, us in the order of the batch and so: 32 ragged sequences of up to 4096 keys, 32 heads
-// 59 and 53, rows in fp32 237 and 182, 12 of them 30.4 and 26.6, heads of 64 38 and 32, 16 with 8 rows 33.6 and 31.3; 32 of 2048 keys each 49.7 and 49.9, 12 22.5 and 22.9; 64 of 2048 at most 56.8 and 55; 100 of 1000 at most,
-// 28/4 heads, 13.1 and 14; shorter: 300 of 500 at most, 8/8 heads 28.9 and 30, of 250 each 27.3 and 29.1). Over e4m3 and bf16 caches, one workgroup a unit, ragged batches gain as much,
-// but batches of one length lose up to 3 %: left in the order of the batch.
-template <typename C> bool longest_first(const Plan &p, const PagedCache &c) {
-    return kE2M1<C> && !p.split && (int64_t)c.max_pages << c.page_shift >= 1024 && split_grid(p, c) > kWorkgroups && split_grid(p, c) <= 4 * kWorkgroups;
-}
-
 template <typename T, int DH>
 int launch_merge(const PagedCache &c, const Plan &p, const int *row_off, void *out, void *part, int rows, int max_rows, int Hq, hipStream_t s) {
     hipLaunchKernelGGL((paged_merge<T, DH>), dim3((unsigned)(rows * Hq)), dim3(256), 0, s, row_off, c.batch, (const int2 *)part,
@@ -255,7 +259,7 @@ int launch_split(const PagedCache &c, const Plan &p, const void *q, int64_t q_st
         static std::atomic<uint64_t> devices{0};                                                                                 \
         const int rc = allow_lds(reinterpret_cast<const void *>(&paged_attn_split<T, C, DH, NQ, NW, ONCE>), smem, devices);      \
         if (rc) return rc;                                                                                                       \
-        hipLaunchKernelGGL((paged_attn_split<T, C, DH, NQ, NW, ONCE>), dim3((unsigned)split_grid(p, c)), dim3(64 * NW), smem, s, c, slice_plan(p, longest_first<C>(p, c)), \
+        hipLaunchKernelGGL((paged_attn_split<T, C, DH, NQ, NW, ONCE>), dim3((unsigned)split_grid(p, c)), dim3(64 * NW), smem, s, c, slice_plan(p), \
                            (const T *)q, q_stride, row_off, (T *)out, (int2 *)part, (float *)((char *)part + meta_bytes(c)), rows, max_rows, \
                            group_map(p), Divisor(c.n_kv_heads), Divisor(Hq / c.n_kv_heads), scale_log2e);                \
     } while (0)
@@ -273,7 +277,7 @@ int launch_wide(const PagedCache &c, const Plan &p, const void *q, int64_t q_str
     const int rc = allow_lds(reinterpret_cast<const void *>(&paged_attn_wide<C, DH, KS>), KS * kWideLds<DH>, devices);
     if (rc) return rc;
     hipLaunchKernelGGL((paged_attn_wide<C, DH, KS>), dim3((unsigned)(p.split ? split_grid(p, c) : p.blocks)), dim3(256 * KS), KS * kWideLds<DH>, s, c,
-                       (const bf16_t *)q, q_stride, row_off, (bf16_t *)out, rows, (int2 *)part, (float *)((char *)part + meta_bytes(c)), slice_plan(p, false),
+                       (const bf16_t *)q, q_stride, row_off, (bf16_t *)out, rows, (int2 *)part, (float *)((char *)part + meta_bytes(c)), slice_plan(p),
                        max_rows, group_map(p), Divisor(c.n_kv_heads), Divisor(Hq / c.n_kv_heads), kWorkgroups / c.n_kv_heads,
                        1.4426950408889634f / sqrtf((float)DH));
     DKV_LAUNCH_CHECK();

@@ -92,13 +92,14 @@ __device__ __forceinline__ int slice_length(const PagedCache &c, const int *row_
         slice = max(plan.least, ceil_div(total, plan.want.d - (c.batch * quarters >> 2)));
     return slice;
 }
-// Whole wavefronts: the sequence that comes `at`-th when each 64 of them are put in the order of their lengths, in sixteen steps of the power of two that holds the table, the longest
-// first: of the sequences that are left, one bit of that number after the other says whether it is with the longer ones or how many of these are before it.
+// Whole wavefronts, up to 64 sequences: the one that comes `at`-th in the order of their lengths, in sixteen steps of the power of two that holds
+// the table, the longest first: of the sequences that are left, one bit of that number after the other says whether it is with the longer ones or how
+// many of these are before it.
 __device__ __forceinline__ int longest(const PagedCache &c, int at) {
-    const int lane = threadIdx.x & 63, from = at & ~63, keys = from + lane < c.batch ? c.keys(from + lane) : 0;
+    const int lane = threadIdx.x & 63, keys = lane < c.batch ? c.keys(lane) : 0;
     const int step = min(15, keys >> max(0, 28 - __builtin_clz(c.capacity() - 1)));
-    unsigned long long left = __builtin_amdgcn_ballot_w64(from + lane < c.batch);
-    int before = at & 63;
+    unsigned long long left = __builtin_amdgcn_ballot_w64(lane < c.batch);
+    int before = at;
 #pragma unroll
     for (int bit = 3; bit >= 0; --bit) {
         const unsigned long long longer = left & __builtin_amdgcn_ballot_w64(step >> bit & 1);
@@ -107,7 +108,7 @@ __device__ __forceinline__ int longest(const PagedCache &c, int at) {
         before -= before < n ? 0 : n;
     }
     const int i = __builtin_amdgcn_mbcnt_hi((uint32_t)(left >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)left, 0));
-    return from + __builtin_ctzll(left & __builtin_amdgcn_ballot_w64(i == before));
+    return __builtin_ctzll(left & __builtin_amdgcn_ballot_w64(i == before));
 }
 // Whole wavefronts. Finds slice `at` of the batch; false if there are fewer.
 __device__ __forceinline__ bool find_slice(const PagedCache &c, const int *row_off, const SlicePlan &plan, int at, Slices &s) {

@@ -122,7 +122,7 @@ def gather_rows(src, picks, counts, dst):
 
 
 class PagedAttnPlan(C.Structure):
-    _fields_ = [(n, C.c_int) for n in ("q_tiles", "q_groups", "wide", "blocks", "cap", "spread", "least", "want")] + [("split", C.c_bool)]
+    _fields_ = [(n, C.c_int) for n in ("q_tiles", "q_groups", "wide", "blocks", "cap", "spread", "least", "want")] + [(n, C.c_bool) for n in ("split", "longest_first")]
 
     @property
     def kernel(self):

@@ -337,3 +337,20 @@ def test_positions_behind_four_gigabytes():
     ref = (w[..., None] * hv).sum(0) / total[:, None]
     bar = 2.0 ** -7 * np.abs(ref) + 2.0 ** -7 * (w[..., None] * np.abs(hv)).sum(0) / total[:, None]
     assert (np.abs(out.double().cpu().numpy()[0] - ref) <= bar).all()
+
+
+@pytest.mark.parametrize("act", ["bf16", "fp32"])
+@pytest.mark.parametrize("batch,heads,group,dh,longest,most", [(64, 8, 2, 64, 1100, 2), (64, 16, 1, 32, 1024, 1), (64, 5, 1, 128, 1700, 3), (2, 140, 1, 32, 1100, 1)])
+def test_a_wavefront_of_sequences_in_the_order_of_their_lengths(act, batch, heads, group, dh, longest, most):
+    """Up to 64 sequences, all in order; lengths that are equal, zero, and as wide as the table."""
+    g = np.random.default_rng(batch + heads)
+    lens = (longest * g.random(batch) ** 4).astype(int)
+    lens[g.integers(0, batch, batch // 4)] = 0
+    lens[batch - 1], lens[0] = longest, lens[batch // 2]
+    counts = g.integers(0, most + 1, batch) if most > 1 else np.ones(batch, int)
+    counts[[0, batch - 1]] = most
+    p = paged_plan(heads * group, int(counts.sum()), most, {"bf16": P.BF16, "fp32": P.FP32}[act], batch, -(-longest // 16), 16, heads, dh, P.E2M1)
+    assert p.kernel == "split" and p.longest_first
+    c = FourBits(lens.tolist(), 16, heads, dh, seed=batch, holes=0.1, wider=0).fill(act)
+    q = rows(g, (int(counts.sum()), heads * group, dh), act)
+    check_attn(c, q, counts.tolist(), most=most)

@@ -174,3 +174,16 @@ def test_fp32_rows_need_no_more_workspace_than_over_e4m3(heads, group, dh, batch
         for fewer in {1, m // 2, m} - {0}:
             plan = paged_plan(group * heads, batch * fewer, fewer, P.FP32, batch, pages, 16, heads, dh, P.E2M1)
             assert need(plan, batch, heads, dh) <= have
+
+
+def test_sequences_are_ordered_by_their_lengths_where_that_gains():
+    """Whole sequences in two to four rounds of workgroups over tables of 1024 positions and more: up to 64 of them, which are in order as a whole."""
+    def ordered(batch, heads, max_pages=32, cache_dtype=P.E2M1, dtype=P.BF16, group=1, page=64, dh=128):
+        p = paged_plan(heads * group, batch, 1, dtype, batch, max_pages, page, heads, dh, cache_dtype)
+        assert p.kernel == "split"
+        return p.longest_first
+
+    assert ordered(32, 32) and ordered(64, 8) and ordered(64, 16, max_pages=16) and ordered(12, 32) and ordered(32, 32, dtype=P.FP32)
+    assert not ordered(33, 32) and not ordered(8, 32, max_pages=8) and not ordered(64, 8, max_pages=15)
+    assert not ordered(65, 8) and not ordered(100, 4, group=7) and not ordered(1000, 1, group=16) and not ordered(128, 8, group=4)
+    assert not ordered(32, 32, cache_dtype=P.E4M3) and not ordered(32, 32, cache_dtype=P.BF16)
