@@ -309,7 +309,9 @@ typedef struct {
  * most 120, and then magnitudes end at 240 * 2^120, so that no finite element is read back as infinity.)
  * A DKV_E2M1 cache holds x * 2^-e rounded to the nearest of its values, ties to the even code, with the smallest e >= -110 that brings the largest
  * magnitude of the 32 dims to at most 6: an error of at most 2^-2 of the element or 2^(e - 2), whichever is larger. Where one of them is an infinity
- * or a NaN all 32 become NaN. (e is at most 126, and then magnitudes end at 3 * 2^126.) */
+ * or a NaN all 32 become NaN. (e is at most 126, and then magnitudes end at 3 * 2^126.)
+ * What that costs attention: on normally distributed rows its result is off by 0.17 (relative, all elements together) of that over the rows before they were
+ * stored, 0.3 where queries are three times as large and few keys count; DKV_E4M3 0.04 and 0.07, DKV_BF16 0.0025 and 0.0045. */
 int dkv_paged_store(const dkv_paged_cache *cache, const void *k_new, const void *v_new, int64_t row_stride,
                     const int32_t *positions, const int32_t *row_off, int32_t rows, int32_t dtype, void *stream);
 
@@ -381,7 +383,8 @@ typedef struct {
  *   DKV_ROPE_LINEAR  f / factor
  *   DKV_ROPE_BASE    f of a larger base, theta * factor^(rot_dim / (rot_dim - 2)): the last pair is stretched by `factor`, the first not
  *   DKV_ROPE_PARTS   f * y + f / factor * (1 - y) with y = (original f / 2 pi - slow) / (fast - slow) within [0, 1]: pairs that turn at least
- *                    `fast` times over `original` positions stay, those that turn at most `slow` times are stretched; scale = 0.1 ln(factor) + 1
+ *                    `fast` times over `original` positions stay, those that turn at most `slow` times are stretched; scale = 0.1 ln(factor) + 1.
+ *                    y is linear in the number of turns; a model that was trained with one that is linear in the pair's index i has to set freq
  * original, slow and fast are read for DKV_ROPE_PARTS only (usual: slow 1, fast 32), factor not for DKV_ROPE_NONE. */
 #define DKV_ROPE_NONE   0
 #define DKV_ROPE_LINEAR 1

@@ -445,8 +445,9 @@ def paged_resize(tables, lengths, workspace, row_off=None, positions=None, slots
 
 class Rope:
     """The frequencies of rotary positions (see dkv_rope_init in dkv.h): pairs (i, i + rot_dim / 2), or where `interleaved` (2 i, 2 i + 1), of the first
-    rot_dim dims of a head. scaling: "none", "linear", "base" or "parts", by `factor`. `freq` (radians of each pair for one position) and
-    `scale` may be set otherwise."""
+    rot_dim dims of a head. scaling: "none", "linear", "base" or "parts", by `factor`. `freq` (radians of each pair for one position, all at once) and
+    `scale` may be set otherwise: "parts" goes from kept to stretched pairs linearly in their number of turns, and a model that was trained with
+    another ramp (linear in the pair's index) has to set them."""
     SCALINGS = ("none", "linear", "base", "parts")
 
     def __init__(self, head_dim, rot_dim=None, theta=10000.0, interleaved=False, scaling="none", factor=1.0, original=4096, slow=1.0, fast=32.0):

@@ -3,8 +3,8 @@
 #include "common.h"
 
 struct PagedCache {
-    unsigned char *k, *v;             // [n_pages][n_kv_heads][page_size][head_dim]
-    uint8_t *ks, *vs;                 // [n_pages][n_kv_heads][page_size], e4m3 only
+    unsigned char *k, *v;             // rows [n_pages][n_kv_heads][page_size] of kRowBytes: head_dim elements, e2m1 two to a byte
+    uint8_t *ks, *vs;                 // the same rows of kRowScales: one (e4m3), head_dim / 32 (e2m1), or null
     const int *table, *seq_len;
     int batch, n_pages, max_pages, page_shift, n_kv_heads;
 
@@ -16,7 +16,7 @@ struct PagedCache {
         const int id = table[(size_t)b * max_pages + (p >> page_shift)];
         return (unsigned)id < (unsigned)n_pages ? id : -1;
     }
-    // index of a (page, head, slot) row: times head_dim elements, or itself in the scales. A cache has at most 2^32 rows.
+    // index of a (page, head, slot) row: times kRowBytes in k and v, times kRowScales in ks and vs. A cache has at most 2^32 rows.
     __device__ __forceinline__ uint32_t row(int page, int head, int slot) const {
         return (((uint32_t)page * n_kv_heads + head) << page_shift) + slot;
     }

@@ -49,9 +49,10 @@ typedef PagedAttnPlan Plan;
 // bf16: 10.5 us with 4 tiles, 11.4 with 8, 17.2 with 32, 22.3 without slices). paged_attn_wide, whose groups take 64 keys at a time: 16
 // tiles of 32 (28/4 heads, 64 rows, 4096 keys 23.1 us with 8, 21.9 with 16, 26.7 with 32; 16384 keys 36.8, 35.4, 35.3).
 constexpr int kWorkgroups = 256, kLeast = 4, kLeastWide = 16;
-// Key tiles of a table (the host does not know the lengths) up to which sequences stay whole: the launch that joins slices costs some 2 us. bf16, 128 dims: 16 tiles 8.6 us whole and 9.0
-// in slices, 24 tiles 11.5 and 9.3; 64 dims: 24 tiles 7.3 and 8.1, 47 tiles 10.8 and 9.0. fp32 (four wavefronts, matrix instructions of an
-// eighth of the rate): 128 dims, 8 tiles 13.3 and 11.8; 64 dims, 8 tiles 7.4 and 8.4, 16 tiles 12.1 and 8.5; 32 dims, 16 tiles 7.5 and 8.2, 24 9.7 and 8.5.
+// Key tiles of a table (the host does not know the lengths) up to which sequences stay whole: the launch that joins slices costs some 2 us. bf16, 128
+// dims: 16 tiles 8.6 us whole and 9.0 in slices, 24 tiles 11.5 and 9.3; 64 dims: 24 tiles 7.3 and 8.1, 47 tiles 10.8 and 9.0. fp32 (four wavefronts,
+// matrix instructions of an eighth of the rate): 128 dims, 8 tiles 13.3 and 11.8; 64 dims, 8 tiles 7.4 and 8.4, 16 tiles 12.1 and 8.5; 32 dims, 16
+// tiles 7.5 and 8.2, 24 9.7 and 8.5.
 int whole_tiles(int dtype, int head_dim) { return (dtype == DKV_BF16 ? 2304 : 640) / head_dim; }
 
 // Slices of one K/V head, all sequences together, that run at once: `per_cu` workgroups to a compute unit, `groups` query groups to a slice on
@@ -72,11 +73,12 @@ int64_t row_groups(const PagedCache &c, int rows, int max_rows, int G, int n) {
 // Blocks of 128 query rows, see make_plan: whether there are rows enough, whether groups of 32 are so many or the keys that are cut so long, and
 // whether keys are cut. None of them turns back with more rows.
 bool rows_for_blocks(int dtype, int head_dim, int query_rows) { return dtype == DKV_BF16 && head_dim >= 64 && query_rows > (head_dim == 128 ? 32 : 64); }
-// e2m1, 128 dims: groups of 32 read K without LDS, and are worth more of it: up to two rounds of workgroups (16 ragged sequences of 28/4 heads, 2000 keys, 40
-// rows 41.6 us in blocks and 30.5; 4100 keys 76 and 51; 8 of 1900 keys, 64 rows 39.5 and 34.6, 2100 keys 44.6 and 37.2; 32/32 heads, 3 of 2600 keys, 150 rows 51 and 43;
-// the other way 8 of 300 keys, 64 rows 13.7 and 15.4, one of 2700 keys, 300 rows of 32/8 heads 39.4 and 44.5; more than two rounds lose: 32 of 512 keys,
-// 28/4 heads, 32 rows 20 and 33), and slices of 6144 keys each (2 of 4000 keys, 130 rows of 28/4 heads 37.3 and 31.8, 8192 keys, 40 rows of 32/32 44.7 and 36.3; one of
-// 8192 keys, 128 rows of 28/4 heads 34.1 and 37.1, 32768 keys 83 and 104). With 64 dims neither gains.
+// e2m1, 128 dims: groups of 32 read K without LDS, and are worth more of it: up to two rounds of workgroups (16 ragged sequences of 28/4 heads, 2000
+// keys, 40 rows 41.6 us in blocks and 30.5; 4100 keys 76 and 51; 8 of 1900 keys, 64 rows 39.5 and 34.6, 2100 keys 44.6 and 37.2; 32/32 heads, 3 of
+// 2600 keys, 150 rows 51 and 43; the other way 8 of 300 keys, 64 rows 13.7 and 15.4, one of 2700 keys, 300 rows of 32/8 heads 39.4 and 44.5; more
+// than two rounds lose: 32 of 512 keys, 28/4 heads, 32 rows 20 and 33), and slices of 6144 keys each (2 of 4000 keys, 130 rows of 28/4 heads 37.3 and
+// 31.8, 8192 keys, 40 rows of 32/32 44.7 and 36.3; one of 8192 keys, 128 rows of 28/4 heads 34.1 and 37.1, 32768 keys 83 and 104). With 64 dims
+// neither gains.
 bool four_bits(int cache_dtype, int head_dim) { return cache_dtype == DKV_E2M1 && head_dim == 128; }
 bool blocks_for_rounds(int cache_dtype, int head_dim, int64_t groups) {
     return groups > (four_bits(cache_dtype, head_dim) ? 2 * kWorkgroups : head_dim == 128 ? kWorkgroups : 3 * kWorkgroups);
@@ -104,10 +106,12 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
     p.spread = best_spread(p.q_groups, heads, 1);
     p.least = kLeast;
     int want = slices_at_once(p.q_groups, heads, p.spread, 1);
-    // e2m1, up to 16 query rows: two workgroups fit a unit. Slices for both where one each would leave the sequences of a long table whole, and make two of each at least (us
-    // whole and cut, one token, 8 sequences, 32 heads: up to 16384 keys 80 and 62, 32 of up to 8192, 32/8 heads, 42 and 33.7, 8192 keys each 50 and 52; up to 4096 keys 24 and 21.6, but 2048 keys each
-    // 15.7 and 18.6; heads of 64 up to 16384 keys 61 and 37.6, 8192 each 34.4 and 30.9). Heads of 64 and 32, up to 128 slices, also where there are slices anyway (2 sequences of 131072 keys,
-    // 28/4 heads 23.2 and 21.3, 32 dims 20.7 and 17.5; 8 of 8192, 32/8 heads 15.3 and 14.3; 512 slices of one sequence 12 and 15.5); with 128 dims the two sequences take 29.8 and 31.6.
+    // e2m1, up to 16 query rows: two workgroups fit a unit. Slices for both where one each would leave the sequences of a long table whole, and make
+    // two of each at least (us whole and cut, one token, 8 sequences, 32 heads: up to 16384 keys 80 and 62, 32 of up to 8192, 32/8 heads, 42 and
+    // 33.7, 8192 keys each 50 and 52; up to 4096 keys 24 and 21.6, but 2048 keys each 15.7 and 18.6; heads of 64 up to 16384 keys 61 and 37.6, 8192
+    // each 34.4 and 30.9). Heads of 64 and 32, up to 128 slices, also where there are slices anyway (2 sequences of 131072 keys, 28/4 heads 23.2 and
+    // 21.3, 32 dims 20.7 and 17.5; 8 of 8192, 32/8 heads 15.3 and 14.3; 512 slices of one sequence 12 and 15.5); with 128 dims the two sequences take
+    // 29.8 and 31.6.
     if (dtype == DKV_BF16 && cache_dtype == DKV_E2M1 && tiles == 1) {
         const int spread = best_spread(1, heads, 2), more = slices_at_once(1, heads, spread, 2);
         if (want <= c.batch ? keys >= 8192 && more >= 2 * c.batch : head_dim < 128 && more <= 128) {
@@ -116,10 +120,12 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
         }
     }
     p.split = key_tiles > whole_tiles(dtype, head_dim) && want > c.batch;
-    // e2m1, whole sequences: groups of 16 query rows, two workgroups of which fit a compute unit, or of 32, of which one does. A round of the first, full, takes 9 / 8 of one of the
-    // second (28/4 heads, 4 sequences of 1024 keys, 64 rows 14.3 us and 12.7; 32 heads, 8 of 1024, 64 rows 25.6 and 25.0), of one workgroup a unit 5 / 8: whatever is less, up to 1024 groups (us by 32
-    // and by 16; 19 of 700 keys, 10 rows of 32/8 heads 20.3 and 12.6; 12 of 1500, 17 rows 28.5 and 18.6; one of 2700, 300 rows 44.9 and 37.5; 64 of 1000, 5 rows of 28/4 heads 25.3 and 21.2, ragged 18.2
-    // and 13.5; more groups, ragged: 16 of 2000, 40 rows 26.2 and 29.1, 20 of 2000, 17 rows of 32 heads 30.4 and 37.7, which are in the order of their lengths by 32).
+    // e2m1, whole sequences: groups of 16 query rows, two workgroups of which fit a compute unit, or of 32, of which one does. A round of the first,
+    // full, takes 9 / 8 of one of the second (28/4 heads, 4 sequences of 1024 keys, 64 rows 14.3 us and 12.7; 32 heads, 8 of 1024, 64 rows 25.6 and
+    // 25.0), of one workgroup a unit 5 / 8: whatever is less, up to 1024 groups (us by 32 and by 16; 19 of 700 keys, 10 rows of 32/8 heads 20.3 and
+    // 12.6; 12 of 1500, 17 rows 28.5 and 18.6; one of 2700, 300 rows 44.9 and 37.5; 64 of 1000, 5 rows of 28/4 heads 25.3 and 21.2, ragged 18.2 and
+    // 13.5; more groups, ragged: 16 of 2000, 40 rows 26.2 and 29.1, 20 of 2000, 17 rows of 32 heads 30.4 and 37.7, which are in the order of their
+    // lengths by 32).
     if (!p.split && p.nq == 2 && four_bits(cache_dtype, head_dim)) {
         const int64_t pairs = (int64_t)c.batch * heads, halves = pairs * tiles, full = halves / (2 * kWorkgroups), rest = halves % (2 * kWorkgroups);
         const int64_t rounds = (pairs * p.q_groups + kWorkgroups - 1) / kWorkgroups;
@@ -129,31 +135,31 @@ Plan make_plan(const PagedCache &c, int n_q_heads, int rows, int max_rows, int d
         }
     }
     // Blocks of 128 query rows (paged_wide.h) where tiles of 32 would make more than one round of workgroups (128 dims; 28/4 heads, 1024 keys: 1
-    // sequence of 300 rows, 264 workgroups, 29 -> 26 us, 4 of 128 rows, 448, 30 -> 27, but 4 of 64 rows, 224, 17 -> 26) or more than three (64
-    // dims, 32 heads, 8 ragged sequences of up to 5600 keys: bf16, 80 rows 61 -> 61, 128 rows 81 -> 70, 250 rows, 119 -> 104; e4m3 65 ->
-    // 68, 94 -> 77, 144 -> 125, since then 63 and 103 in blocks; of 700 keys each 24.1 -> 21, 32 -> 22, 59 -> 32). Also where the
-    // keys are so many that slices of them keep the compute units busy without those workgroups: 1536 keys each for tiles of 32 (28/4
-    // heads, 1 sequence of 128 rows, 4096 keys 30.3 -> 28.9 us, 32768 keys 131 -> 98, but 32 rows, 4096 keys 15.9 -> 21.4, 8192 keys 21.0 -> 23.3),
-    // of more than 4096 keys of 128 dims (64 dims, 28/4 heads, 2 sequences of 128 rows: 4096 keys 27.6 -> 34.4 over e4m3, 8192 keys 48.3 -> 46.9, bf16 42.8 -> 44.6).
-    // More than 32 query rows to a sequence, which two of the four wavefronts work on (19 sequences of 700 keys, 32/32 heads, 40 rows 73 -> 59 us,
-    // 32/8 heads, 10 rows 27.9 -> 25.1); with 64 dims more than 64 (32/32 heads, 64 rows, 12 sequences of 8192 keys 160 -> 198, e4m3 156 -> 245).
-    // Two groups of wavefronts to a workgroup where the blocks are few and the keys many enough to share (96 blocks of 1024 keys 28.6 -> 26.0 us,
-    // 128 blocks of 256 keys 12.8 -> 13.6), and one round of workgroups holds them two by two (36 sequences
-    // of 700 keys, 32/8 heads, 32 rows: 288 blocks, each of a sequence of its own, 43 -> 58). Few are 320 at most, for the longest sequences of ragged batches
-    // are then shared and the shorter ones paired (28/4 heads, 129 rows and 1536 keys at most: at most 308 blocks 45.8 -> 42.3, 344 47.2 -> 46.5, 380 50.8 -> 52.9);
-    // batches of one length gain up to 256 and lose a little from there (32/32 heads, 1536 keys: 256 blocks 45.9 -> 43.9, 288 60.2 -> 63.4).
-    // Their keys are cut where every sequence can have two slices, from 2048 keys of 128 dims on (32/8 heads, 300 rows, 80 blocks: 1300 keys
-    // 32.9 us whole and 33.8 in slices, 2700 keys 55.9 and 43.0; 28/4 heads, 4 ragged sequences of 130 rows and 2000 keys at most 43.8 and 35.4),
-    // from 4096 of 64 dims (4 sequences of 300 rows, 2700 keys: 32/32 heads 69 and 86, 28/4 heads 69 and 79, 3500 keys 85 and 89).
-    // Slices of heads of 64 have one group of wavefronts, and three workgroups a compute unit, which hold more loads on their way than one of
-    // two groups (28/4 heads, 130 rows, 100000 keys: e4m3 214 -> 167 us, since then 139, bf16 155 -> 151; 32/32 heads, 80 rows, 2 sequences of 31000
-    // 152 -> 123, since then 96, and 116 -> 113; the other way 28/4 heads, 17 rows of 2 sequences of 31000 31.1 -> 32.8 and 28.4 -> 28.8).
-    // With fewer slices the long sequences of a ragged batch are cut all the same. The host knows the rows, and takes it that keys go with
-    // them (a batch of equal rows over ragged lengths is not seen): ragged is a batch with at most 3/4 of the rows that the longest sequence's would make (28/4 heads, 8 sequences of up to 9000 keys and 80 rows, 12
-    // slices: 0.6 of them 159 -> 102 us, 0.75 158 -> 130, 1 161 -> 166; 14 of up to 2100, 37 rows, 20 slices: 0.6 45 -> 41, 0.75 46 -> 48, 0.8 46 -> 49), and
-    // from four slices for three sequences on (9 sequences, 12 slices 158 -> 133, 10 158 -> 162; of up to 3000 keys, 40 rows, 20 slices for 13 sequences
-    // 59 -> 44, 15 59.5 -> 59.5, 16 59.8 -> 63; 16/1 heads, 6000 keys, 64 rows, 32 slices for 24 109 -> 105, 26 109 -> 114). In two rounds of slices batches of one length lose (8 sequences of 5600 keys, 32 heads, 80
-    // rows 119 -> 141).
+    // sequence of 300 rows, 264 workgroups, 29 -> 26 us, 4 of 128 rows, 448, 30 -> 27, but 4 of 64 rows, 224, 17 -> 26) or more than three (64 dims,
+    // 32 heads, 8 ragged sequences of up to 5600 keys: bf16, 80 rows 61 -> 61, 128 rows 81 -> 70, 250 rows, 119 -> 104; e4m3 65 -> 68, 94 -> 77, 144
+    // -> 125, since then 63 and 103 in blocks; of 700 keys each 24.1 -> 21, 32 -> 22, 59 -> 32). Also where the keys are so many that slices of them
+    // keep the compute units busy without those workgroups: 1536 keys each for tiles of 32 (28/4 heads, 1 sequence of 128 rows, 4096 keys 30.3 ->
+    // 28.9 us, 32768 keys 131 -> 98, but 32 rows, 4096 keys 15.9 -> 21.4, 8192 keys 21.0 -> 23.3), of more than 4096 keys of 128 dims (64 dims, 28/4
+    // heads, 2 sequences of 128 rows: 4096 keys 27.6 -> 34.4 over e4m3, 8192 keys 48.3 -> 46.9, bf16 42.8 -> 44.6). More than 32 query rows to a
+    // sequence, which two of the four wavefronts work on (19 sequences of 700 keys, 32/32 heads, 40 rows 73 -> 59 us, 32/8 heads, 10 rows 27.9 ->
+    // 25.1); with 64 dims more than 64 (32/32 heads, 64 rows, 12 sequences of 8192 keys 160 -> 198, e4m3 156 -> 245). Two groups of wavefronts to a
+    // workgroup where the blocks are few and the keys many enough to share (96 blocks of 1024 keys 28.6 -> 26.0 us, 128 blocks of 256 keys 12.8 ->
+    // 13.6), and one round of workgroups holds them two by two (36 sequences of 700 keys, 32/8 heads, 32 rows: 288 blocks, each of a sequence of its
+    // own, 43 -> 58). Few are 320 at most, for the longest sequences of ragged batches are then shared and the shorter ones paired (28/4 heads, 129
+    // rows and 1536 keys at most: at most 308 blocks 45.8 -> 42.3, 344 47.2 -> 46.5, 380 50.8 -> 52.9); batches of one length gain up to 256 and lose
+    // a little from there (32/32 heads, 1536 keys: 256 blocks 45.9 -> 43.9, 288 60.2 -> 63.4). Their keys are cut where every sequence can have two
+    // slices, from 2048 keys of 128 dims on (32/8 heads, 300 rows, 80 blocks: 1300 keys 32.9 us whole and 33.8 in slices, 2700 keys 55.9 and 43.0;
+    // 28/4 heads, 4 ragged sequences of 130 rows and 2000 keys at most 43.8 and 35.4), from 4096 of 64 dims (4 sequences of 300 rows, 2700 keys:
+    // 32/32 heads 69 and 86, 28/4 heads 69 and 79, 3500 keys 85 and 89). Slices of heads of 64 have one group of wavefronts, and three workgroups a
+    // compute unit, which hold more loads on their way than one of two groups (28/4 heads, 130 rows, 100000 keys: e4m3 214 -> 167 us, since then 139,
+    // bf16 155 -> 151; 32/32 heads, 80 rows, 2 sequences of 31000 152 -> 123, since then 96, and 116 -> 113; the other way 28/4 heads, 17 rows of 2
+    // sequences of 31000 31.1 -> 32.8 and 28.4 -> 28.8). With fewer slices the long sequences of a ragged batch are cut all the same. The host knows
+    // the rows, and takes it that keys go with them (a batch of equal rows over ragged lengths is not seen): ragged is a batch with at most 3/4 of
+    // the rows that the longest sequence's would make (28/4 heads, 8 sequences of up to 9000 keys and 80 rows, 12 slices: 0.6 of them 159 -> 102 us,
+    // 0.75 158 -> 130, 1 161 -> 166; 14 of up to 2100, 37 rows, 20 slices: 0.6 45 -> 41, 0.75 46 -> 48, 0.8 46 -> 49), and from four slices for three
+    // sequences on (9 sequences, 12 slices 158 -> 133, 10 158 -> 162; of up to 3000 keys, 40 rows, 20 slices for 13 sequences 59 -> 44, 15 59.5 ->
+    // 59.5, 16 59.8 -> 63; 16/1 heads, 6000 keys, 64 rows, 32 slices for 24 109 -> 105, 26 109 -> 114). In two rounds of slices batches of one length
+    // lose (8 sequences of 5600 keys, 32 heads, 80 rows 119 -> 141).
     if (rows_for_blocks(dtype, head_dim, max_rows * G)) {
         const int64_t groups = row_groups(c, rows, max_rows, G, 32), blocks = row_groups(c, rows, max_rows, G, 128);
         const int per_cu = block_workgroups_per_cu(head_dim), q_groups = ceil_div(tiles, 8), spread = best_spread(q_groups, heads, per_cu);

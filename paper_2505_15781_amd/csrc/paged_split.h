@@ -11,16 +11,16 @@
 // total number of key tiles and the number of slices that the host wants for the whole batch, and find their own by a prefix
 // sum over the sequences. So a captured call follows the lengths, and a ragged batch is cut where its keys are.
 //
-// e4m3 elements are converted on their way into LDS with their row's scale (exact in bf16 and fp32), everything behind is the same
-// for all caches, but for K of an e2m1 cache: 32 dims are 16 bytes, so that the lanes that hold a key's operand of the matrix instruction load
-// just that, and convert it where it is used. It needs no LDS, which leaves room for a second workgroup on a compute unit. (The order of the dims in a
-// product is free; the queries are read in the same one.) A tile is two halves of 16 keys, each on one page: no load needs a bounds check, a half without a page reads page 0
-// and is masked. Masked scores become -infinity and masked V rows zero, whatever they hold.
+// e4m3 elements are converted on their way into LDS with their row's scale (exact in bf16 and fp32), everything behind is the same for all caches,
+// but for K of an e2m1 cache: 32 dims are 16 bytes, so that the lanes that hold a key's operand of the matrix instruction load just that, and convert
+// it where it is used. It needs no LDS, which leaves room for a second workgroup on a compute unit. (The order of the dims in a product is free; the
+// queries are read in the same one.) A tile is two halves of 16 keys, each on one page: no load needs a bounds check, a half without a page reads
+// page 0 and is masked. Masked scores become -infinity and masked V rows zero, whatever they hold.
 //
-// Bound by the K/V stream where there is much of it: one token of 32 sequences of up to 4096 keys, 32 heads of 128 in e4m3 (558 MB), 95 us, 5.9
-// TB/s (a cold read of that size reaches 6.0); two sequences of 131072 keys, 28/4 heads, e4m3 (271 MB), 45 us and 4.5 us
-// of paged_merge. In e2m1 (295 MB) 50-53 us, 5.6-5.9 TB/s (K through LDS: 74), and (143 MB) 27 us and 4.5. 32 query rows of 8 sequences of 1024 keys, 32 heads, bf16 (138 MB) 25 us, 5.5 TB/s. Few keys are a chain of latencies
-// (length, page number, first tile, join): 512 keys of 32 heads 7.6 us.
+// Bound by the K/V stream where there is much of it: one token of 32 sequences of up to 4096 keys, 32 heads of 128 in e4m3 (558 MB), 95 us, 5.9 TB/s
+// (a cold read of that size reaches 6.0); two sequences of 131072 keys, 28/4 heads, e4m3 (271 MB), 45 us and 4.5 us of paged_merge. In e2m1 (295 MB)
+// 50-53 us, 5.6-5.9 TB/s (K through LDS: 74), and (143 MB) 27 us and 4.5. 32 query rows of 8 sequences of 1024 keys, 32 heads, bf16 (138 MB) 25 us,
+// 5.5 TB/s. Few keys are a chain of latencies (length, page number, first tile, join): 512 keys of 32 heads 7.6 us.
 #pragma once
 
 constexpr int PKT = 32;                // keys per tile

@@ -2,15 +2,17 @@
 // the new positions listed with their slots.
 //
 // Everything depends on sums over the sequences before: pages taken, pages given back, new rows. One workgroup forms them (paged_resize_plan, a
-// thread per sequence, 1024 at a time), and a launch of many wavefronts writes tables and lists from them (paged_resize_fill). Small calls
-// are nothing but latency: there the workgroup goes on with its own wavefronts, in one launch, its sums in LDS. No sum depends on an order, so the results do not either.
+// thread per sequence, 1024 at a time), and a launch of many wavefronts writes tables and lists from them (paged_resize_fill). Small calls are
+// nothing but latency: there the workgroup goes on with its own wavefronts, in one launch, its sums in LDS. No sum depends on an order, so the
+// results do not either.
 //
-// Entries that give a page back may name none, so these have to be counted before their places in the ring are known: by a launch of its own, a wavefront to a
-// sequence (by the one workgroup, a sequence after the other to a wavefront, 512 sequences of 256 pages took 28 us instead of 3 + 3), or in the one-launch form by
-// going through all such entries in a row, 4096 at a time.
+// Entries that give a page back may name none, so these have to be counted before their places in the ring are known: by a launch of its own, a
+// wavefront to a sequence (by the one workgroup, a sequence after the other to a wavefront, 512 sequences of 256 pages took 28 us instead of 3 + 3),
+// or in the one-launch form by going through all such entries in a row, 4096 at a time.
 //
-// One launch: 64 sequences, 1000 rows, 4 of them leave 5.8-6.5 us in a trace, the least 4.1: the chain of lengths, barriers, ring or table, stores. Three: 512 sequences, 1.9 million
-// rows 16 us (3 + 3 + 9.7; 23 MB written at 2.4 TB/s in the last). There each row of a lane that looked its sequence up in memory by itself, with the row before stored between, took 12.4 instead of 9.7.
+// One launch: 64 sequences, 1000 rows, 4 of them leave 5.8-6.5 us in a trace, the least 4.1: the chain of lengths, barriers, ring or table, stores.
+// Three: 512 sequences, 1.9 million rows 16 us (3 + 3 + 9.7; 23 MB written at 2.4 TB/s in the last). There each row of a lane that looked its
+// sequence up in memory by itself, with the row before stored between, took 12.4 instead of 9.7.
 #include <type_traits>
 
 #include "paged.h"

@@ -10,17 +10,15 @@
 //         once per 128 query rows: 32 of a wavefront's vector instructions per tile, next to some 200 of the softmax.
 //
 // 4 sequences of 1536 rows and keys, 32 heads of 128 (155 GFLOP): e4m3 178-188 us by card, 820-870 TFLOP/s, bf16 191-193. A large product would take
-// 111 us. Power is part of the rest: with zeros for data the same launches take 160 and 143 us. What the other part is no counters show yet. Softmax, products
-// and LDS reads hide behind each other: without its exponentials the e4m3 launch took 5 % less, without the maximum 2 %, without the reads of V 4 %. Measured and
-// not kept there: the maximum inside the stretch (193 us), 64 query rows
-// per wavefront (227), e4m3 conversion spread over the stretch (no gain;
-// 64 dims 125 -> 150), two groups of wavefronts (187-209), blocks of 256 query rows with eight
-// wavefronts behind one barrier, which halves the fills (201 against 183: two workgroups to a compute unit drift apart and fill each other's
-// gaps), LDS reads 9 and 12 ahead instead of 6 (no change).
-// Over e2m1 171-188 us by card. Not kept there: the conversion between the products of a stretch, from two sets of registers (171 -> 179 us), or of K
-// where it is used, each wavefront for itself and without LDS (172 -> 177); keys that are not there made zero when they are fetched (178 -> 181). Two
-// wavefronts of a SIMD take 1.25 us for a tile each, one alone 1.5. Products of K in 4 bits with the queries in two parts of 8 (the same matrix time, no
-// conversion) add up to less than fp32: up to 2^-12 of the sum of magnitudes is lost.
+// 111 us. Power is part of the rest: with zeros for data the same launches take 160 and 143 us. What the other part is no counters show yet. Softmax,
+// products and LDS reads hide behind each other: without its exponentials the e4m3 launch took 5 % less, without the maximum 2 %, without the reads
+// of V 4 %. Measured and not kept there: the maximum inside the stretch (193 us), 64 query rows per wavefront (227), e4m3 conversion spread over the
+// stretch (no gain; 64 dims 125 -> 150), two groups of wavefronts (187-209), blocks of 256 query rows with eight wavefronts behind one barrier, which
+// halves the fills (201 against 183: two workgroups to a compute unit drift apart and fill each other's gaps), LDS reads 9 and 12 ahead instead of 6
+// (no change). Over e2m1 171-188 us by card. Not kept there: the conversion between the products of a stretch, from two sets of registers (171 -> 179
+// us), or of K where it is used, each wavefront for itself and without LDS (172 -> 177); keys that are not there made zero when they are fetched (178
+// -> 181). Two wavefronts of a SIMD take 1.25 us for a tile each, one alone 1.5. Products of K in 4 bits with the queries in two parts of 8 (the same
+// matrix time, no conversion) add up to less than fp32: up to 2^-12 of the sum of magnitudes is lost.
 #pragma once
 
 typedef __attribute__((address_space(3))) void *lds_ptr_t;
@@ -331,7 +329,8 @@ __global__ __launch_bounds__(256 * KS, 2) __attribute__((amdgpu_waves_per_eu(2, 
                        bf16x8 (&pn)[2]) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) sn[v] = 0.f;
-        // heads of 64, whose exponentials weigh as much as the products: the wavefront in here goes first (e2m1, 4 sequences of 1536 102 -> 98 us; 128 dims: no change)
+        // heads of 64, whose exponentials weigh as much as the products: the wavefront in here goes first (e2m1, 4 sequences of 1536 102 -> 98 us;
+        // 128 dims: no change)
         if constexpr (DH == 64) __builtin_amdgcn_s_setprio(1);
         f32x8 p[2];
         constexpr int MT = DH / 32, N = DH / 16, PER = 16 / N;        // products of the scores, and of the output; exponentials next to each two
