@@ -6,14 +6,15 @@
 // positions at one radian each: an fp32 product is off by 2^-4): position times frequency, in quarter turns, and what is left of it in the
 // quarter are formed in 64 bits, sine and cosine of that from their Taylor series in 32.
 //
-// 6144 rows of 64 heads of 128 in bf16 (201 MB) 35.7 us in place, 39.4 into other memory (5.1 TB/s; a large copy 4.46), 3072 in fp32 34.5 and 38;
-// 64 rows 3.4 us, the call is 5.5 us of the host. Part of a head moves what a whole one does: in place 64 and 32 dims of 128 take 26 and 24 us
-// (all are read, those that are turned written). Where the pairs of a head are no multiple of 4 (neighbouring ones: of 2) a lane has one pair, and
-// these rows take 45 to 58.
+// 6144 rows of 64 heads of 128 in bf16 (201 MB) 35.7 us in place, 39.4 into other memory (5.1 TB/s; a large copy 4.46), 2048 in fp32 21.9 and 25.8;
+// 64 rows 3.4 us, the call is 5.5 us of the host. Neighbouring pairs in one piece of 32 bytes a lane, every other 16 to a load, took 30.1 us instead of
+// 27.0 (4099 rows of 32 heads in fp32, 64 dims). Part of a head into other memory moves all of it, in place all is read and what turns is written: 64
+// and 32 dims of 128 26 and 24 us. Where the pairs of a head are no multiple of 4 (neighbouring ones: of 2) a lane has one pair, and these rows take 41
+// to 58.
 //
-// The results are written into the caches: the next launches of a layer read them. With the non-temporal hint rope alone is faster in some
-// calls (6144 rows in bf16 into other memory 39.8 -> 35.3 us, in place 35.7 -> 34.4, but 3072 rows 17.0 -> 18.9, 32 of 128 dims into other memory
-// 41 -> 47), not with its readers: stored into a cache and attended to 242 -> 246, in place 241.5 -> 242.5, 1024 rows 55.2 -> 55.3 and
+// The results are written into the caches: the next launches of a layer read them. With the non-temporal hint rope alone is faster in some calls
+// (6144 rows in bf16 into other memory 39.8 -> 35.3 us, in place 35.7 -> 34.4, but with 28 and 4 heads 17.1 -> 19.2, 32 of 128 dims into other
+// memory 41 -> 47), not with its readers: stored into a cache and attended to 242 -> 246, in place 241.5 -> 242.5, 1024 rows 55.2 -> 55.3 and
 // 54.7 -> 55.0, 512 rows 47.0 -> 48.0 and 46.9 -> 47.0; with a copy of the results 57 -> 61.
 #include <math.h>
 
